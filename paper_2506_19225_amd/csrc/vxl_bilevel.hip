@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "vxl_internal.h"
+#include "vxl_rows.h"
 
 namespace vxl {
 
@@ -485,12 +486,6 @@ __global__ __launch_bounds__(256, 8) void pool_sparse_kernel(const T* __restrict
 // map the in-place decode reads the dense and sparse rows through).
 // ------------------------------------------------------------------------------------------
 constexpr long long kPastCaches = 160ll << 20;
-// Chunks up to which a block keeps where a chunk's rows come from in LDS beside the offsets: more would leave room for
-// fewer than the eight blocks per compute unit that the heads one after the other run at (FOUR, at four, always does).
-// Beyond, a row asks memory for it.  Eight queries, one head, 3,000 chunks of 40 tokens 55.0 -> 42.3 us, three, two heads
-// of D = 64, 4,096 of 40, 2,000 dense 74.9 -> 56.7; one query, one head, 4,096 of 32 22.3 -> 23.0.
-constexpr int kTableChunks = 2500;
-
 template <int ROW_BYTES, bool FOUR, bool ONCE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR ? 4 : 8, FOUR ? 4 : 8))) void gather_kernel(
     const uint4* __restrict__ K, const uint4* __restrict__ V, const uint8_t* __restrict__ dense_mask,
@@ -504,54 +499,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR ? 4 : 
     extern __shared__ int off[];                              // [n_chunks] first mixed row of every chunk, top bit: dense; then
     int* from = off + n_chunks;                               // (table) [n_chunks] its first token, or -1 - its first kept row
     const bool table = FOUR || n_chunks <= kTableChunks;
-    constexpr int DENSE = INT32_MIN;
     __shared__ int wave_tot[4][4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x;
     const int b = ONCE ? blockIdx.x % batch : blockIdx.y, block = ONCE ? blockIdx.x / batch : blockIdx.x;
     const uint8_t* mask = dense_mask + (size_t)b * n_chunks;
-    int len = n_prefix;                                       // rows of the chunks so far
-    // The rows every chunk contributes, four 256-chunk passes at a time: their loads are all requested before the
-    // first scan and do not wait for the mask (one memory round trip and one barrier per 1,024 chunks).
-    for (int base4 = 0; base4 < n_chunks; base4 += 1024) {
-        int rows[4], inc[4], flag[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int c = base4 + u * 256 + tid;
-            rows[u] = flag[u] = 0;
-            if (c < n_chunks) {
-                const int lo = bounds[c], hi = bounds[c + 1], s_lo = soff[c], s_hi = soff[c + 1];
-                const bool dense = mask[c] != 0;
-                rows[u] = dense ? hi - lo : s_hi - s_lo;
-                flag[u] = dense ? DENSE : 0;
-                if (table) from[c] = dense ? lo : -1 - s_lo;
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (base4 + u * 256 >= n_chunks) break;           // (uniform)
-            inc[u] = rows[u];                                 // inclusive scan inside the wave
-            for (int o = 1; o < 64; o <<= 1) {
-                const int t = __shfl_up(inc[u], o);
-                if (lane >= o) inc[u] += t;
-            }
-            if (lane == 63) wave_tot[u][wave] = inc[u];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (base4 + u * 256 >= n_chunks) break;
-            const int c = base4 + u * 256 + tid;
-            int before = len;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const int t = wave_tot[u][w];
-                before += w < wave ? t : 0;
-                len += t;
-            }
-            if (c < n_chunks) off[c] = (before + inc[u] - rows[u]) | flag[u];
-        }
-        __syncthreads();                                      // off is there; wave_tot may be written again
-    }
+    const int len = scan_mixed_rows(mask, bounds, soff, n_chunks, n_prefix, off, from, table, wave_tot);
     // a mixed set that does not fit l_cap is reported, not truncated: minus the rows it needs
     if (block == 0 && tid == 0) mix_len[b] = len <= l_cap ? len : -len;
     if (len > l_cap) return;
@@ -560,23 +512,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR ? 4 : 
     for (int gi = 0; gi < groups; ++gi) {
         const int r = (block * groups + gi) * ROWS + tid / LPR;
         if (r >= len) break;                                  // (rows ascend with gi; the lanes of a row together)
-        int src;                                              // token id, or -1 - pooled row
-        if (r < n_prefix) {
-            src = r;
-        } else {
-            int c = 0;                                        // last chunk with off[c] <= r: it lies in [c, c + span)
-            for (int span = n_chunks; span > 1;) {
-                const int step = (span + LPR - 1) / LPR;
-                const unsigned long long hit = __ballot(part * step < span && (off[min(c + part * step, n_chunks - 1)] & ~DENSE) <= r);
-                const int last = __popcll((hit >> (lane & ~(LPR - 1))) & ((1ull << LPR) - 1)) - 1;
-                c += last * step;
-                span = min(step, span - last * step);
-            }
-            const int at = off[c], o = r - (at & ~DENSE);
-            const int first = table ? from[c] : at < 0 ? bounds[c] : -1 - soff[c];
-            if (first >= 0) src = first + o;
-            else src = Ksp ? first - o : sidx[-1 - first + o];
-        }
+        const int src = mixed_row_source<LPR>(r, n_prefix, n_chunks, off, from, table, bounds, soff, sidx, Ksp != nullptr);
         if (src_idx && part == 0) src_idx[(size_t)b * l_cap + r] = src;
         if (!Kmix) continue;                                  // index-only call: no rows are copied
         const uint4* ks = src >= 0 ? K : Ksp;
