@@ -62,7 +62,8 @@ typedef enum {
     VXL_OP_GATHER = 2,
     VXL_OP_DECODE = 3,
     VXL_OP_SCORE_MASS = 4,
-    VXL_OP_DECODE_INPLACE = 5
+    VXL_OP_DECODE_INPLACE = 5,
+    VXL_OP_DECODE_KVQ = 6
 } vxl_op;
 
 /*
@@ -370,6 +371,71 @@ vxl_status vxl_kv_store_offload(vxl_kv_store* store, const void* K, const void* 
 vxl_status vxl_kv_store_reload(vxl_kv_store* store, const uint8_t* dense_mask, int32_t batch,
                                void* Kmix, void* Vmix, int32_t l_cap, int32_t* mix_len_host,
                                int32_t* mix_len, vxl_stream stream);
+
+/*
+ * Quantised KV cache: the keys and values of one layer in 8 or 4 bits, for the same bi-level decoding ("Bi-level KVs
+ * Decoding" keeps the dense KVs of a whole video; in 4 bits 136 bytes per row and KV head of 128 dimensions instead of 512).
+ * A block is 32 consecutive elements x of a key or value row.  With a = max |x| its scale is 2^e,
+ *   e = floor(log2 a) - emax, one more where a / 2^floor(log2 a) >= 1.75;   emax = 8 (FP8) or 2 (FP4), e >= -110 (also of a = 0)
+ * and its codes are x / 2^e rounded to the nearest number of the element type, ties to even (FP4: at most to its largest, 6).
+ * A value reads back as code * 2^e, exactly, in BF16 and in F32.  A block with an infinity, a NaN or a magnitude of 1.75 * 2^127
+ * or more reads back as NaN.
+ *   rows      device [n_kv_heads, capacity, 2, head_dim * bits / 8]: the codes of a row's key, then of its value; FP4: two
+ *             per byte, the element with the even index in the low half
+ *   scales    device uint8 [n_kv_heads, capacity, 2, head_dim / 32]: e + 127 of the key's blocks, then of the value's; 255: NaN
+ *   format    VXL_KVQ_FP8: e4m3 (4 significant bits, largest number 448); VXL_KVQ_FP4: e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6)
+ *   capacity  rows per KV head; row i of the cache of a prompt is token i
+ * Both buffers 16-byte aligned.  What the calls below read has been written by vxl_kvq_write, or holds codes and scale bytes
+ * of 17 to 252 or 255.  The descriptor gives heads, head_dim and the type and strides of the plain tensors.
+ */
+typedef enum { VXL_KVQ_FP8 = 0, VXL_KVQ_FP4 = 1 } vxl_kvq_format;
+typedef struct {
+    void* rows;
+    void* scales;
+    int32_t format;          /* vxl_kvq_format */
+    int32_t capacity;
+} vxl_kvq_cache;
+
+/* Bytes of the codes of one row of one KV head; *scale_bytes (may be NULL): of its scales.  0 on invalid arguments. */
+size_t vxl_kvq_row_bytes(const vxl_attn_desc* desc, int32_t format, size_t* scale_bytes);
+
+/*
+ * Writes rows [first_row, first_row + n_rows) of the cache from K and V; other rows are left as they are.
+ *   K, V   device, n_rows rows of every KV head in the descriptor's layout (strides 0: dense [n_kv_heads, n_rows, head_dim];
+ *          a part of a longer tensor is its first row and the strides of the whole)
+ * n_rows == 0 does nothing.  No workspace.  Errors: VXL_ERR_INVALID_ARG (null, misaligned or aliasing buffers, rows outside the
+ * capacity), VXL_ERR_UNSUPPORTED, VXL_ERR_HIP.
+ */
+vxl_status vxl_kvq_write(const vxl_attn_desc* desc, const void* K, const void* V, int32_t n_rows, const vxl_kvq_cache* cache,
+                         int32_t first_row, vxl_stream stream);
+/* The inverse: K and V (written, in the layout above) from rows [first_row, first_row + n_rows) of the cache. */
+vxl_status vxl_kvq_read(const vxl_attn_desc* desc, const vxl_kvq_cache* cache, int32_t first_row, int32_t n_rows, void* K, void* V,
+                        vxl_stream stream);
+
+/*
+ * vxl_gather_bilevel_kv from a quantised cache: the mixed KV sets in the descriptor's type, ready for vxl_bilevel_decode.
+ *   cache    the dense rows of the layout's tokens (capacity >= n_tokens)
+ *   sparse   quantised sparse rows in chunk order (capacity >= S_total, the format of `cache`): the pooled rows of
+ *            vxl_pool_sparse_kv, or the kept rows compacted; NULL: the kept rows are read where they lie in `cache`
+ * Other arguments, capacity, report of an overflow and src_idx as vxl_gather_bilevel_kv (sparse == NULL) or
+ * vxl_gather_bilevel_kv_pooled.  No workspace.
+ */
+vxl_status vxl_gather_bilevel_kvq(const vxl_layout* layout, const vxl_attn_desc* desc, const vxl_kvq_cache* cache,
+                                  const vxl_kvq_cache* sparse, const uint8_t* dense_mask, int32_t batch, void* Kmix, void* Vmix,
+                                  int32_t l_cap, int32_t* mix_len, int32_t* src_idx, vxl_stream stream);
+
+/*
+ * vxl_bilevel_decode_inplace over a quantised cache: every query token attends to the quantised rows of its mixed set where
+ * they lie.  cache and sparse as above, other arguments as vxl_bilevel_decode_inplace (map_ready too: the row map is the same),
+ * the workspace sized by vxl_workspace_bytes(VXL_OP_DECODE_KVQ, layout, desc, batch, n_q_tokens, l_cap), never less.
+ * O and LSE are those of the attention over the values that the cache reads back as, within the tolerance of the path; the
+ * same call gives the same bits.  A row whose logits include NaN or +inf, or are all -inf, and one that attends to a NaN
+ * value, are NaN; what a query does not attend to never matters.
+ */
+vxl_status vxl_bilevel_decode_kvq(const vxl_layout* layout, const vxl_attn_desc* desc, const void* Qd, int32_t batch,
+                                  int32_t n_q_tokens, const vxl_kvq_cache* cache, const vxl_kvq_cache* sparse,
+                                  const uint8_t* dense_mask, int32_t l_cap, int32_t map_ready, void* O, float* LSE,
+                                  int32_t* mix_len, void* workspace, size_t workspace_bytes, vxl_stream stream);
 
 const char* vxl_status_string(vxl_status s);
 const char* vxl_last_error(void);   /* text of the last failing HIP call on this thread */

@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 #include <numeric>
 
@@ -192,7 +193,7 @@ extern "C" int vxl_debug_decode_plan(const vxl_attn_desc* d, int batch, int n_q_
 }
 
 // Workspace of the in-place decode: split-KV partial results, then the row map and the lengths.
-InplaceWorkspace inplace_workspace(const vxl_attn_desc* d, int batch, int T, int l_cap) {
+InplaceWorkspace inplace_workspace(int batch, int l_cap, size_t partials) {
     InplaceWorkspace w{};
     // The row map and the lengths come first: their places do not depend on the number of query
     // tokens, so a map survives calls with another n_q_tokens on the same workspace.
@@ -202,7 +203,7 @@ InplaceWorkspace inplace_workspace(const vxl_attn_desc* d, int batch, int T, int
     w.mix_len = off;
     off += align_up((size_t)batch * sizeof(int32_t), 256);
     w.partials = off;
-    off += align_up(std::max<size_t>(256, decode_plan(d, batch, T, l_cap, false).total), 256);
+    off += align_up(std::max<size_t>(256, partials), 256);
     w.total = off;
     return w;
 }
@@ -456,7 +457,10 @@ size_t vxl_workspace_bytes(vxl_op op, const vxl_layout* L, const vxl_attn_desc* 
             return std::max<size_t>(256, mass_plan(L, d, batch, n_q_tokens).total);
         case VXL_OP_DECODE_INPLACE:
             if (batch <= 0 || n_q_tokens <= 0 || l_cap <= 0) return 0;
-            return inplace_workspace(d, batch, n_q_tokens, l_cap).total;
+            return inplace_workspace(batch, l_cap, decode_plan(d, batch, n_q_tokens, l_cap, false).total).total;
+        case VXL_OP_DECODE_KVQ:
+            if (batch <= 0 || n_q_tokens <= 0 || l_cap <= 0) return 0;
+            return inplace_workspace(batch, l_cap, kvq_plan(d, batch, n_q_tokens, l_cap).total).total;
     }
     return 0;
 }
@@ -616,7 +620,7 @@ vxl_status vxl_bilevel_decode_inplace(const vxl_layout* L, const vxl_attn_desc* 
     if (!aligned16(Qd) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(Ksp) || !aligned16(Vsp))
         return VXL_ERR_INVALID_ARG;
     if (l_cap < vxl_mixed_kv_capacity(L, 0)) return VXL_ERR_INVALID_ARG;
-    const InplaceWorkspace w = inplace_workspace(d, batch, n_q_tokens, l_cap);
+    const InplaceWorkspace w = inplace_workspace(batch, l_cap, decode_plan(d, batch, n_q_tokens, l_cap, false).total);
     // (fp32: the row map is needed, room for partial results is not)
     const DecodePlan p = decode_plan(d, batch, n_q_tokens, l_cap, false, workspace_bytes > w.partials ? workspace_bytes - w.partials : 0);
     const size_t need = w.partials + (d->dtype == VXL_F32 ? 256 : align_up(std::max<size_t>(256, p.total), 256));
@@ -640,6 +644,96 @@ vxl_status vxl_bilevel_decode_inplace(const vxl_layout* L, const vxl_attn_desc* 
                                                      decode_f32_plan(d, batch, n_q_tokens, l_cap).total), s);
     return launch_decode_inplace_simple(L, d, scale, Qd, batch, n_q_tokens, K, V, Ksp, Vsp, src_idx, l_cap, len, O,
                                         LSE, s);
+}
+
+static bool cache_ok(const vxl_kvq_cache* c, vxl_status* st) {
+    *st = VXL_ERR_INVALID_ARG;
+    if (!c || !c->rows || !c->scales || !aligned16(c->rows) || !aligned16(c->scales) || c->capacity <= 0) return false;
+    if (c->format != VXL_KVQ_FP8 && c->format != VXL_KVQ_FP4) { *st = VXL_ERR_UNSUPPORTED; return false; }
+    return true;
+}
+
+// Arguments that a gather and a decode of quantised rows share; *sp: the sparse rows where there are any.
+static vxl_status kvq_sets_ok(const vxl_layout* L, const vxl_kvq_cache* cache, const vxl_kvq_cache* sparse,
+                              const uint8_t* dense_mask, int32_t batch, int32_t l_cap, const vxl_kvq_cache** sp) {
+    vxl_status st;
+    *sp = sparse && L->s_total > 0 ? sparse : nullptr;
+    if (!cache_ok(cache, &st) || (*sp && !cache_ok(*sp, &st))) return st;
+    if (cache->capacity < L->n_tokens || (*sp && ((*sp)->capacity < L->s_total || (*sp)->format != cache->format)))
+        return VXL_ERR_INVALID_ARG;
+    if (batch <= 0 || l_cap <= 0 || (L->n_chunks > 0 && !dense_mask) || l_cap < vxl_mixed_kv_capacity(L, 0)) return VXL_ERR_INVALID_ARG;
+    return VXL_OK;
+}
+
+size_t vxl_kvq_row_bytes(const vxl_attn_desc* d, int32_t format, size_t* scale_bytes) {
+    vxl_status st;
+    const bool ok = desc_ok(d, &st) && (format == VXL_KVQ_FP8 || format == VXL_KVQ_FP4);
+    if (scale_bytes) *scale_bytes = ok ? 2 * d->head_dim / 32 : 0;
+    return ok ? 2 * d->head_dim / (format == VXL_KVQ_FP4 ? 2 : 1) : 0;
+}
+
+// Arguments of the calls between plain rows and rows of a quantised cache.
+static vxl_status kvq_rows_ok(const vxl_attn_desc* d, const void* K, const void* V, int32_t n_rows, const vxl_kvq_cache* cache,
+                              int32_t first_row) {
+    vxl_status st;
+    if (!desc_ok(d, &st) || !cache_ok(cache, &st)) return st;
+    if (n_rows < 0 || first_row < 0 || n_rows > cache->capacity - first_row) return VXL_ERR_INVALID_ARG;
+    if (n_rows > 0 && (!K || !V || !aligned16(K) || !aligned16(V))) return VXL_ERR_INVALID_ARG;
+    for (const void* p : {K, V})
+        if (p && (p == cache->rows || p == cache->scales)) return VXL_ERR_INVALID_ARG;
+    return VXL_OK;
+}
+
+vxl_status vxl_kvq_write(const vxl_attn_desc* d, const void* K, const void* V, int32_t n_rows, const vxl_kvq_cache* cache,
+                         int32_t first_row, vxl_stream stream) {
+    const vxl_status st = kvq_rows_ok(d, K, V, n_rows, cache, first_row);
+    if (st != VXL_OK || n_rows == 0) return st;
+    return launch_kvq_write(d, K, V, n_rows, cache, first_row, (hipStream_t)stream);
+}
+
+vxl_status vxl_kvq_read(const vxl_attn_desc* d, const vxl_kvq_cache* cache, int32_t first_row, int32_t n_rows, void* K, void* V,
+                        vxl_stream stream) {
+    const vxl_status st = kvq_rows_ok(d, K, V, n_rows, cache, first_row);
+    if (st != VXL_OK || n_rows == 0) return st;
+    if (K == V) return VXL_ERR_INVALID_ARG;
+    return launch_kvq_read(d, cache, first_row, n_rows, K, V, (hipStream_t)stream);
+}
+
+vxl_status vxl_gather_bilevel_kvq(const vxl_layout* L, const vxl_attn_desc* d, const vxl_kvq_cache* cache,
+                                  const vxl_kvq_cache* sparse, const uint8_t* dense_mask, int32_t batch, void* Kmix,
+                                  void* Vmix, int32_t l_cap, int32_t* mix_len, int32_t* src_idx, vxl_stream stream) {
+    vxl_status st;
+    const vxl_kvq_cache* sp;
+    if (!L) return VXL_ERR_INVALID_ARG;
+    if (!desc_ok(d, &st)) return st;
+    if ((st = kvq_sets_ok(L, cache, sparse, dense_mask, batch, l_cap, &sp)) != VXL_OK) return st;
+    if (!Kmix || !Vmix || !mix_len || !aligned16(Kmix) || !aligned16(Vmix) || Kmix == Vmix) return VXL_ERR_INVALID_ARG;
+    return launch_kvq_gather(L, d, cache, sp, dense_mask, batch, Kmix, Vmix, l_cap, mix_len, src_idx, (hipStream_t)stream);
+}
+
+vxl_status vxl_bilevel_decode_kvq(const vxl_layout* L, const vxl_attn_desc* d, const void* Qd, int32_t batch, int32_t n_q_tokens,
+                                  const vxl_kvq_cache* cache, const vxl_kvq_cache* sparse, const uint8_t* dense_mask,
+                                  int32_t l_cap, int32_t map_ready, void* O, float* LSE, int32_t* mix_len, void* workspace,
+                                  size_t workspace_bytes, vxl_stream stream) {
+    vxl_status st;
+    const vxl_kvq_cache* sp;
+    if (!L) return VXL_ERR_INVALID_ARG;
+    if (!desc_ok(d, &st)) return st;
+    if ((st = kvq_sets_ok(L, cache, sparse, dense_mask, batch, l_cap, &sp)) != VXL_OK) return st;
+    if (!Qd || !O || n_q_tokens <= 0 || !aligned16(Qd) || !aligned16(O) || O == Qd) return VXL_ERR_INVALID_ARG;
+    const KvqPlan p = kvq_plan(d, batch, n_q_tokens, l_cap);
+    const InplaceWorkspace w = inplace_workspace(batch, l_cap, p.total);
+    if (!workspace || workspace_bytes < w.total || !aligned16(workspace)) return VXL_ERR_WORKSPACE;
+    hipStream_t s = (hipStream_t)stream;
+    int32_t* src_idx = (int32_t*)((char*)workspace + w.src_idx);
+    int32_t* len = mix_len ? mix_len : (int32_t*)((char*)workspace + w.mix_len);
+    if (!map_ready) {           // the row map and the lengths: the gather's index pass, which reads no row
+        st = launch_gather(L, d, nullptr, nullptr, sp ? sp->rows : nullptr, sp ? sp->rows : nullptr, dense_mask, batch, nullptr,
+                           nullptr, l_cap, len, src_idx, s);
+        if (st != VXL_OK) return st;
+    }
+    return launch_kvq_decode(p, d, resolve_scale(d), Qd, batch, n_q_tokens, cache, sp, src_idx, l_cap, len, O, LSE,
+                             (char*)workspace + w.partials, s);
 }
 
 vxl_status vxl_bilevel_decode_static(const vxl_attn_desc* d, const void* Qd, int32_t batch,

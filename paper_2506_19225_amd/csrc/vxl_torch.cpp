@@ -20,19 +20,21 @@ namespace {
 // copy in the process called the first copy's library, and one of another path than its own was never called.
 #define VXL_PATH(X)                                                                                               \
     X(chunk_prefill) X(chunk_score_topk) X(chunk_score_topk_mass) X(gather_bilevel_kv) X(pool_sparse_kv)          \
-    X(gather_bilevel_kv_pooled) X(bilevel_decode) X(bilevel_decode_inplace)
+    X(gather_bilevel_kv_pooled) X(bilevel_decode) X(bilevel_decode_inplace) X(kvq_write) X(kvq_read)              \
+    X(gather_bilevel_kvq) X(bilevel_decode_kvq)
 
 // Of one module object: a vxl.py that is loaded twice has two.
 struct State {
-    PyObject *desc_type, *handle_type, *stream_of;
+    PyObject *desc_type, *handle_type, *stream_of, *cache_type;
 #define VXL_DECLARE(name) decltype(&vxl_##name) name;
     VXL_PATH(VXL_DECLARE)
 };
 
-// Kinds of an argument: a layout's c_void_p (or a number or None, the library's to refuse); the descriptor; a tensor (its
+// Kinds of an argument: a layout's c_void_p (or a number or None, the library's to refuse); the descriptor; a quantised cache
+// or None, a null pointer; a tensor (its
 // data pointer; a contiguous CUDA tensor or AssertionError) or None, a null pointer; a number.  Python does not pass
 // kNumel, the number of elements of the tensor before it (0 for None), and size(i, d), dimension d of its argument i.
-enum Kind { kLayout, kDesc, kTensor, kInt, kNumel, kSize };
+enum Kind { kLayout, kDesc, kCache, kTensor, kInt, kNumel, kSize };
 constexpr int size(int arg, int dim) { return kSize | arg << 8 | dim << 16; }
 
 // A number that an object answers with (a new reference, or null where it raised).
@@ -133,6 +135,15 @@ bool layout_of(const State& st, PyObject* o, long long* out) {
     return true;
 }
 
+bool cache_of(const State& st, PyObject* o, long long* out) {
+    void* p = nullptr;
+    if (o == Py_None) { *out = 0; return true; }
+    if (!st.cache_type || !PyObject_TypeCheck(o, (PyTypeObject*)st.cache_type)) return refuse(o, "a quantised cache");
+    if (!memory_of(o, &p)) return false;
+    *out = (long long)p;
+    return true;
+}
+
 constexpr bool passed(int kind) { return kind < kNumel; }
 
 // The argument of this kind: the next of Python's, or a number read off one.
@@ -142,6 +153,7 @@ bool convert(const State& st, PyObject* const* args, int* next, long long* out) 
     else if constexpr (KIND == kNumel) return numel_of(args[*next - 1], out);
     else if constexpr (KIND == kLayout) return layout_of(st, args[(*next)++], out);
     else if constexpr (KIND == kDesc) return desc_of(st, args[(*next)++], out);
+    else if constexpr (KIND == kCache) return cache_of(st, args[(*next)++], out);
     else if constexpr (KIND == kTensor) return tensor_of(args[(*next)++], out);
     else return int_of(args[(*next)++], out);
 }
@@ -176,6 +188,14 @@ PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n, F f) {
 template <typename T> T* ptr(long long a) { return (T*)a; }
 const vxl_layout* lay(long long a) { return (const vxl_layout*)a; }
 const vxl_attn_desc* desc(long long a) { return (const vxl_attn_desc*)a; }
+const vxl_kvq_cache* cache(long long a) { return (const vxl_kvq_cache*)a; }
+
+// Whether a tensor of so many elements holds the rows that a call takes off it, by the descriptor's layout.
+bool holds(const vxl_attn_desc* d, long long n_rows, long long numel) {
+    if (n_rows <= 0) return true;                             // (for the library to refuse, or nothing to do)
+    const long long head = d->kv_stride_head ? d->kv_stride_head : n_rows * d->head_dim, tok = d->kv_stride_tok ? d->kv_stride_tok : d->head_dim;
+    return (d->n_kv_heads - 1) * head + (n_rows - 1) * tok + d->head_dim <= numel;
+}
 
 PyObject* chunk_prefill(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     return call<kLayout, kDesc, kTensor, kTensor, kTensor, kTensor, kTensor, kTensor, kNumel>(
@@ -242,6 +262,34 @@ PyObject* bilevel_decode_inplace(PyObject* self, PyObject* const* args, Py_ssize
                                           ptr<void>(a[15]), (size_t)a[16], (vxl_stream)a[17]);
     });
 }
+PyObject* kvq_write(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    return call<kDesc, kTensor, kNumel, kTensor, kNumel, kInt, kCache, kInt>(self, args, n, [](const State& lib, const long long* a) {
+        if (!holds(desc(a[0]), a[5], a[2]) || !holds(desc(a[0]), a[5], a[4])) return VXL_ERR_INVALID_ARG;
+        return lib.kvq_write(desc(a[0]), ptr<void>(a[1]), ptr<void>(a[3]), (int32_t)a[5], cache(a[6]), (int32_t)a[7], (vxl_stream)a[8]);
+    });
+}
+PyObject* kvq_read(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    return call<kDesc, kCache, kInt, kInt, kTensor, kNumel, kTensor, kNumel>(self, args, n, [](const State& lib, const long long* a) {
+        if (!holds(desc(a[0]), a[3], a[5]) || !holds(desc(a[0]), a[3], a[7])) return VXL_ERR_INVALID_ARG;
+        return lib.kvq_read(desc(a[0]), cache(a[1]), (int32_t)a[2], (int32_t)a[3], ptr<void>(a[4]), ptr<void>(a[6]), (vxl_stream)a[8]);
+    });
+}
+PyObject* gather_bilevel_kvq(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    return call<kLayout, kDesc, kCache, kCache, kTensor, size(5, 0), kTensor, kTensor, size(5, 2), kTensor, kTensor>(
+        self, args, n, [](const State& lib, const long long* a) {
+        return lib.gather_bilevel_kvq(lay(a[0]), desc(a[1]), cache(a[2]), cache(a[3]), ptr<uint8_t>(a[4]), (int32_t)a[5], ptr<void>(a[6]),
+                                      ptr<void>(a[7]), (int32_t)a[8], ptr<int32_t>(a[9]), ptr<int32_t>(a[10]), (vxl_stream)a[11]);
+    });
+}
+PyObject* bilevel_decode_kvq(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    return call<kLayout, kDesc, kTensor, size(2, 0), size(2, 1), kCache, kCache, kTensor, kInt, kInt, kTensor, kTensor, kTensor,
+                kTensor, kNumel>(
+        self, args, n, [](const State& lib, const long long* a) {
+        return lib.bilevel_decode_kvq(lay(a[0]), desc(a[1]), ptr<void>(a[2]), (int32_t)a[3], (int32_t)a[4], cache(a[5]), cache(a[6]),
+                                      ptr<uint8_t>(a[7]), (int32_t)a[8], (int32_t)a[9], ptr<void>(a[10]), ptr<float>(a[11]),
+                                      ptr<int32_t>(a[12]), ptr<void>(a[13]), (size_t)a[14], (vxl_stream)a[15]);
+    });
+}
 // setup(type of the descriptor, type of a layout's handle, vxl._stream, the addresses of VXL_PATH)
 PyObject* setup(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 #define VXL_COUNT(name) + 1
@@ -265,12 +313,21 @@ PyObject* setup(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     }
     Py_RETURN_NONE;
 }
+// setup_cache(type of a quantised cache)
+PyObject* setup_cache(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    if (n != 1 || !PyType_Check(args[0])) { PyErr_SetString(PyExc_TypeError, "a type expected"); return nullptr; }
+    State& st = *(State*)PyModule_GetState(self);
+    Py_INCREF(args[0]);
+    Py_XSETREF(st.cache_type, args[0]);
+    Py_RETURN_NONE;
+}
 
 int traverse(PyObject* self, visitproc visit, void* arg) {
     const State* st = (const State*)PyModule_GetState(self);
     if (!st) return 0;
     Py_VISIT(st->desc_type);
     Py_VISIT(st->handle_type);
+    Py_VISIT(st->cache_type);
     Py_VISIT(st->stream_of);
     return 0;
 }
@@ -279,6 +336,7 @@ int clear(PyObject* self) {
     if (!st) return 0;
     Py_CLEAR(st->desc_type);
     Py_CLEAR(st->handle_type);
+    Py_CLEAR(st->cache_type);
     Py_CLEAR(st->stream_of);
     return 0;
 }
@@ -286,7 +344,7 @@ int clear(PyObject* self) {
 int exec(PyObject* self) { return PyModule_AddStringConstant(self, "torch_version", VXL_TORCH_VERSION); }
 
 #define VXL_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr},
-PyMethodDef methods[] = {VXL_METHOD(setup) VXL_PATH(VXL_METHOD){nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {VXL_METHOD(setup) VXL_METHOD(setup_cache) VXL_PATH(VXL_METHOD){nullptr, nullptr, 0, nullptr}};
 PyModuleDef_Slot slots[] = {{Py_mod_exec, (void*)exec}, {0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_vxl_torch", nullptr, sizeof(State), methods, slots, traverse, clear, nullptr};
 

@@ -19,7 +19,8 @@ BINDING_PATH = os.path.join(_PKG, "_vxl_torch" + (sysconfig.get_config_var("EXT_
 
 VXL_OK, VXL_ERR_INVALID_ARG, VXL_ERR_UNSUPPORTED, VXL_ERR_WORKSPACE, VXL_ERR_HIP, VXL_ERR_ALLOC = range(6)
 VXL_F32, VXL_BF16 = 0, 1
-OP_PREFILL, OP_SCORE_TOPK, OP_GATHER, OP_DECODE, OP_SCORE_MASS, OP_DECODE_INPLACE = range(6)
+OP_PREFILL, OP_SCORE_TOPK, OP_GATHER, OP_DECODE, OP_SCORE_MASS, OP_DECODE_INPLACE, OP_DECODE_KVQ = range(7)
+KVQ_FP8, KVQ_FP4 = range(2)
 MAX_CHUNKS = 4096
 
 
@@ -28,6 +29,11 @@ class AttnDesc(C.Structure):
                 ("dtype", C.c_int32), ("softmax_scale", C.c_float), ("reserved", C.c_int32),
                 ("q_stride_head", C.c_int64), ("q_stride_tok", C.c_int64),
                 ("kv_stride_head", C.c_int64), ("kv_stride_tok", C.c_int64)]
+
+
+class KvqCacheArg(C.Structure):
+    """vxl_kvq_cache"""
+    _fields_ = [("rows", C.c_void_p), ("scales", C.c_void_p), ("format", C.c_int32), ("capacity", C.c_int32)]
 
 
 class VxlError(RuntimeError):
@@ -42,7 +48,8 @@ _lib = None
 _native = None
 # The calls of the path, in the order in which the binding takes their addresses.
 _PATH = ("chunk_prefill", "chunk_score_topk", "chunk_score_topk_mass", "gather_bilevel_kv", "pool_sparse_kv",
-         "gather_bilevel_kv_pooled", "bilevel_decode", "bilevel_decode_inplace")
+         "gather_bilevel_kv_pooled", "bilevel_decode", "bilevel_decode_inplace", "kvq_write", "kvq_read", "gather_bilevel_kvq",
+         "bilevel_decode_kvq")
 
 
 def lib() -> C.CDLL:
@@ -100,6 +107,17 @@ def lib() -> C.CDLL:
     L.vxl_bilevel_decode_inplace.argtypes = [vp, dp, vp, i32, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
     L.vxl_bilevel_decode_static.restype = C.c_int
     L.vxl_bilevel_decode_static.argtypes = [dp, vp, i32, i32, vp, vp, i32, vp, vp, vp, vp]
+    cp = C.POINTER(KvqCacheArg)
+    L.vxl_kvq_row_bytes.restype = sz
+    L.vxl_kvq_row_bytes.argtypes = [dp, i32, C.POINTER(sz)]
+    L.vxl_kvq_write.restype = C.c_int
+    L.vxl_kvq_write.argtypes = [dp, vp, vp, i32, cp, i32, vp]
+    L.vxl_kvq_read.restype = C.c_int
+    L.vxl_kvq_read.argtypes = [dp, cp, i32, i32, vp, vp, vp]
+    L.vxl_gather_bilevel_kvq.restype = C.c_int
+    L.vxl_gather_bilevel_kvq.argtypes = [vp, dp, cp, cp, vp, i32, vp, vp, i32, vp, vp, vp]
+    L.vxl_bilevel_decode_kvq.restype = C.c_int
+    L.vxl_bilevel_decode_kvq.argtypes = [vp, dp, vp, i32, i32, cp, cp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
     L.vxl_debug_force_simple.argtypes = [C.c_int]
     L.vxl_debug_prefill_variant.argtypes = [C.c_int]
     L.vxl_debug_prefill_events.argtypes = [vp, vp]
@@ -142,6 +160,7 @@ def native():
             raise RuntimeError(f"{BINDING_PATH} was built for torch {module.torch_version}, this is {torch.__version__}: "
                                f"{build} again")
         module.setup(AttnDesc, C.c_void_p, _stream, *(C.cast(getattr(L, "vxl_" + n), C.c_void_p).value for n in _PATH))
+        module.setup_cache(KvqCacheArg)
         _native = module
     return _native
 
@@ -304,6 +323,64 @@ def bilevel_decode_inplace(layout: Layout, desc: AttnDesc, qd, k, v, ksp, vsp, d
     st = (_native or native()).bilevel_decode_inplace(layout.handle, desc, qd, k, v, ksp, vsp, dense_mask, int(l_cap),
                                                       int(bool(map_ready)), out, lse, mix_len, workspace, stream)
     _check(st, "vxl_bilevel_decode_inplace")
+    return out
+
+
+class KvqCache:
+    """A quantised KV cache of one layer (vxl_kvq_cache) and the tensors that hold it: rows uint8 [Hkv, capacity, 2,
+    D * bits / 8] and scales uint8 [Hkv, capacity, 2, D / 32], allocated (uninitialised) unless given."""
+
+    def __init__(self, desc: AttnDesc, format, capacity: Optional[int] = None, rows=None, scales=None, device="cuda"):
+        code = {"fp8": KVQ_FP8, "fp4": KVQ_FP4}.get(format, format)
+        scale_bytes = C.c_size_t()
+        row_bytes = lib().vxl_kvq_row_bytes(C.byref(desc), code, C.byref(scale_bytes)) if isinstance(code, int) else 0
+        if not row_bytes:
+            raise ValueError(f"unsupported descriptor or format {format!r}")
+        if (rows is None) != (scales is None) or (rows is None) == (capacity is None):
+            raise ValueError("either a capacity or both tensors of a cache")
+        if rows is None:
+            rows = torch.empty((desc.n_kv_heads, int(capacity), 2, row_bytes // 2), dtype=torch.uint8, device=device)
+            scales = torch.empty((desc.n_kv_heads, int(capacity), 2, scale_bytes.value // 2), dtype=torch.uint8, device=device)
+        for t, last in ((rows, row_bytes // 2), (scales, scale_bytes.value // 2)):
+            if t.dtype != torch.uint8 or tuple(t.shape) != (desc.n_kv_heads, rows.shape[1], 2, last):
+                raise ValueError(f"a uint8 tensor of shape {(desc.n_kv_heads, rows.shape[1], 2, last)} expected, "
+                                 f"not {t.dtype} of {tuple(t.shape)}")
+        self.rows, self.scales, self.format, self.capacity = rows, scales, code, int(rows.shape[1])
+        self.arg = KvqCacheArg(_ptr(rows), _ptr(scales), code, self.capacity)
+
+
+def kvq_write(desc: AttnDesc, k, v, cache: KvqCache, first_row: int = 0, n_rows: Optional[int] = None, stream=None):
+    """vxl_kvq_write: rows [first_row, first_row + n_rows) of the cache from k / v, contiguous tensors that start at the first
+    of these rows (n_rows None: all they hold in dense storage)."""
+    if n_rows is None:
+        n_rows = k.numel() // (desc.n_kv_heads * desc.head_dim)
+    st = (_native or native()).kvq_write(desc, k, v, int(n_rows), cache.arg, int(first_row), stream)
+    _check(st, "vxl_kvq_write")
+
+
+def kvq_read(desc: AttnDesc, cache: KvqCache, k, v, first_row: int = 0, n_rows: Optional[int] = None, stream=None):
+    """vxl_kvq_read: k / v from rows [first_row, first_row + n_rows) of the cache; tensors as kvq_write's."""
+    if n_rows is None:
+        n_rows = k.numel() // (desc.n_kv_heads * desc.head_dim)
+    st = (_native or native()).kvq_read(desc, cache.arg, int(first_row), int(n_rows), k, v, stream)
+    _check(st, "vxl_kvq_read")
+
+
+def gather_bilevel_kvq(layout: Layout, desc: AttnDesc, cache: KvqCache, sparse: Optional[KvqCache], dense_mask, kmix, vmix,
+                       mix_len, src_idx=None, stream=None):
+    """vxl_gather_bilevel_kvq: as gather_bilevel_kv, rows read back from the quantised cache (sparse: quantised sparse rows
+    [Hkv, S_total], or None: the kept rows of the cache)."""
+    st = (_native or native()).gather_bilevel_kvq(layout.handle, desc, cache.arg, sparse.arg if sparse is not None else None,
+                                                  dense_mask, kmix, vmix, mix_len, src_idx, stream)
+    _check(st, "vxl_gather_bilevel_kvq")
+
+
+def bilevel_decode_kvq(layout: Layout, desc: AttnDesc, qd, cache: KvqCache, sparse: Optional[KvqCache], dense_mask, l_cap: int, out,
+                       lse=None, mix_len=None, workspace=None, map_ready: bool = False, stream=None):
+    """vxl_bilevel_decode_kvq: as bilevel_decode_inplace, over the rows of the quantised cache."""
+    st = (_native or native()).bilevel_decode_kvq(layout.handle, desc, qd, cache.arg, sparse.arg if sparse is not None else None,
+                                                  dense_mask, int(l_cap), int(bool(map_ready)), out, lse, mix_len, workspace, stream)
+    _check(st, "vxl_bilevel_decode_kvq")
     return out
 
 

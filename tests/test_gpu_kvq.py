@@ -1,0 +1,558 @@
+"""The quantised KV cache on the device: codes and values bit for bit against the oracle's definition, gathered sets exactly,
+the decode in place against float64 attention over the values that the cache stands for, with bounds counted from the
+roundings that the path makes."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2506_19225_amd import vxl, workloads as wl
+
+from gpu_util import gpu_decode, kept_rows, make_layout
+from kvq_util import FORMATS, device_cache, pack, quantised, random_rows
+
+pytestmark = pytest.mark.gpu
+DTYPE = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def same_bits(a, b):
+    return a.dtype == b.dtype and a.shape == b.shape and torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+
+# ---- write and read ------------------------------------------------------------------------------
+def write_and_read(k, v, dtype, fmt, token_major=False, first=0, capacity=None):
+    """k, v float32 [Hkv, n, D]: written at `first`, compared with the oracle, read back and compared again."""
+    hkv, n, d = k.shape
+    capacity = first + n if capacity is None else capacity
+    desc = vxl.make_desc(hkv, hkv, d, dtype, token_major=token_major)
+    cache = vxl.KvqCache(desc, fmt, capacity)
+    cache.rows.fill_(0x5a)
+    cache.scales.fill_(0xa5)
+    order = (lambda x: x.transpose(1, 0, 2)) if token_major else (lambda x: x)
+    dk, dv = vxl.to_device(order(k), dtype), vxl.to_device(order(v), dtype)
+    vxl.kvq_write(desc, dk, dv, cache, first)
+    rows, scales, wk, wv = quantised(k, v, fmt)
+    want_rows, want_scales = np.full(cache.rows.shape, 0x5a, np.uint8), np.full(cache.scales.shape, 0xa5, np.uint8)
+    want_rows[:, first:first + n], want_scales[:, first:first + n] = rows, scales
+    got_rows, got_scales = cache.rows.cpu().numpy(), cache.scales.cpu().numpy()
+    assert np.array_equal(got_scales, want_scales)
+    assert np.array_equal(got_rows, want_rows)
+    k2, v2 = torch.full_like(dk, 3.0), torch.full_like(dv, 3.0)
+    vxl.kvq_read(desc, cache, k2, v2, first)
+    for got, want in ((k2, wk), (v2, wv)):
+        got, want = got.double().cpu().numpy(), order(want)
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        assert np.array_equal(got[~np.isnan(want)], want[~np.isnan(want)])
+        assert np.array_equal(np.signbit(got[~np.isnan(want)]), np.signbit(want[~np.isnan(want)]))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hkv,n,d,token_major,first,spare", [
+    (4, 1, 128, True, 37, 5), (2, 3, 64, False, 0, 0), (1, 130, 128, False, 1, 0), (3, 67, 64, True, 9, 1), (8, 33, 128, True, 0, 3)])
+def test_rows_written_and_read(fmt, dtype, hkv, n, d, token_major, first, spare):
+    rng = np.random.default_rng(n * d + hkv)
+    k, v = random_rows(rng, (hkv, n, d), dtype), random_rows(rng, (hkv, n, d), dtype)
+    write_and_read(k, v, dtype, fmt, token_major, first, first + n + spare)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_every_bf16_number(fmt):
+    """All 65,536 bit patterns: in blocks of 32 neighbours, and each beside a larger one, so that every number is the largest of
+    a block once and is rounded against other scales too."""
+    bits = np.arange(65536, dtype=np.uint32)
+    x = (bits << 16).view(np.float32)
+    with np.errstate(invalid="ignore"):
+        y = np.where(np.isfinite(x), x, 1.0).astype(np.float32).reshape(-1, 32)
+    mixed = y[np.argsort((bits * 40503) % 65536).reshape(-1, 32) // 32, np.arange(32)]
+    mixed[:, 0] = np.abs(mixed[:, 0])
+    near = np.concatenate([y.reshape(-1, 64), (y * np.float32(0.5)).reshape(-1, 64)], 0)
+    near[:, 5] = wl.round_to_bf16((near[:, 6].astype(np.float64) * 5).clip(-2.0e38, 2.0e38).astype(np.float32))
+    for rows in (x.reshape(1, -1, 64), mixed.reshape(1, -1, 64), wl.round_to_bf16(near)[None]):
+        write_and_read(rows, rows[:, ::-1].copy(), "bf16", fmt)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_fp32_numbers_at_the_borders(fmt):
+    """Ties, numbers a step to either side of them, the bound of a block's scale, subnormals, the largest, zeros, NaN."""
+    numbers = oracle.kvq_numbers(fmt)
+    ties = np.concatenate([numbers, (numbers[1:] + numbers[:-1]) / 2]).astype(np.float32)
+    around = np.concatenate([ties, np.nextafter(ties, np.float32(9e9)), np.nextafter(ties, np.float32(-9e9))])
+    around = np.concatenate([around, -around])
+    rng = np.random.default_rng(8)
+    blocks = []
+    for e in (-149, -126, -112, -110, -60, -1, 0, 40, 110):
+        for top in (numbers[-1], 1.75 * 2.0 ** np.floor(np.log2(numbers[-1]) - 1), 3.5):
+            row = rng.choice(around, size=128).astype(np.float64) * 2.0 ** e
+            row[rng.integers(0, 4) * 32:][:32][3] = top * 2.0 ** e
+            blocks.append(row.astype(np.float32))
+    special = np.zeros((8, 128), np.float32)
+    special[0, 3:5] = np.inf, 1.0
+    special[1, 40] = np.nan
+    special[2, 70] = np.float32(1.75 * 2.0 ** 127)
+    special[3, 70] = np.nextafter(np.float32(1.75 * 2.0 ** 127), np.float32(0))
+    special[4] = -0.0
+    special[5, ::7] = 1.0e-45
+    special[6, 100] = np.finfo(np.float32).max
+    x = np.concatenate([np.stack(blocks), special])[None]
+    write_and_read(x, x[:, ::-1].copy(), "f32", fmt)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_part_of_a_longer_tensor(dtype):
+    """Rows 11..50 of a head-major tensor, by its strides, into rows 100..139; then one row, and none."""
+    rng = np.random.default_rng(77)
+    hkv, n, d = 3, 90, 64
+    k, v = random_rows(rng, (hkv, n, d), dtype), random_rows(rng, (hkv, n, d), dtype)
+    desc = vxl.make_desc(hkv, hkv, d, dtype)
+    desc.q_stride_head = desc.kv_stride_head = n * d
+    desc.q_stride_tok = desc.kv_stride_tok = d
+    cache = vxl.KvqCache(desc, "fp4", 150)
+    cache.rows.zero_(), cache.scales.zero_()
+    dk, dv = vxl.to_device(k, dtype), vxl.to_device(v, dtype)
+    at = lambda t, r: t.view(-1)[r * d:]                                        # noqa: E731
+    vxl.kvq_write(desc, at(dk, 11), at(dv, 11), cache, 100, 40)
+    vxl.kvq_write(desc, at(dk, 89), at(dv, 89), cache, 149, 1)
+    vxl.kvq_write(desc, at(dk, 0), at(dv, 0), cache, 0, 0)
+    rows, scales, wk, _ = quantised(k, v, "fp4")
+    got = cache.rows.cpu().numpy()
+    assert np.array_equal(got[:, 100:140], rows[:, 11:51]) and np.array_equal(got[:, 149], rows[:, 89])
+    assert not got[:, :100].any() and not got[:, 140:149].any()
+    assert np.array_equal(cache.scales.cpu().numpy()[:, 100:140], scales[:, 11:51])
+    for start, count in ((51, 40), (89, 2), (0, 91)):                           # rows that the tensors do not hold
+        with pytest.raises(vxl.VxlError) as e:
+            vxl.kvq_write(desc, at(dk, start), at(dv, start), cache, 0, count)
+        assert e.value.status == vxl.VXL_ERR_INVALID_ARG
+        with pytest.raises(vxl.VxlError) as e:
+            vxl.kvq_read(desc, cache, at(dk, start), at(dv, start), 0, count)
+        assert e.value.status == vxl.VXL_ERR_INVALID_ARG
+    back = torch.zeros_like(dk)
+    vxl.kvq_read(desc, cache, at(back, 20), at(torch.zeros_like(dk), 20), 100, 40)
+    got = back.double().cpu().numpy()
+    assert np.array_equal(got[:, 20:60], wk[:, 11:51]) and not got[:, :20].any() and not got[:, 60:].any()
+
+
+# ---- prompts -------------------------------------------------------------------------------------
+def prompt(rng, dtype, hkv, d, fmt, lay, pooled):
+    """Plain rows of a prompt, its caches on the device and the values that they stand for (dense, sparse)."""
+    k, v = random_rows(rng, (hkv, lay.n_tokens, d), dtype), random_rows(rng, (hkv, lay.n_tokens, d), dtype)
+    desc = vxl.make_desc(hkv, hkv, d, dtype)
+    rows, scales, wk, wv = quantised(k, v, fmt)
+    cache = device_cache(desc, fmt, rows, scales, spare=3)
+    if not pooled:
+        return cache, None, (wk, wv), None
+    ksp, vsp = (random_rows(rng, (hkv, max(int(lay.sparse_offsets[-1]), 1), d), dtype) for _ in range(2))
+    rows, scales, wks, wvs = quantised(ksp, vsp, fmt)
+    return cache, device_cache(desc, fmt, rows, scales, spare=2), (wk, wv), (wks, wvs)
+
+
+def mixed(values, sparse, masks, lay, l_cap):
+    args = lay.n_prefix, lay.chunk_bounds, lay.sparse_offsets
+    if sparse is None:
+        return oracle.gather_bilevel(*values, masks, *args, lay.sparse_idx, l_cap=l_cap)
+    return oracle.gather_bilevel_pooled(*values, *sparse, masks, *args, l_cap=l_cap)
+
+
+def some_masks(rng, bsz, n_chunks):
+    masks = rng.integers(0, 2, size=(bsz, n_chunks)).astype(np.uint8)
+    masks[0] = 0
+    if bsz > 1:
+        masks[1] = 1
+    return masks
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("pooled", [False, True])
+@pytest.mark.parametrize("dtype,hkv,d,bsz,chunks,prefix", [
+    ("bf16", 4, 128, 3, 11, 17), ("f32", 1, 64, 2, 5, 0), ("bf16", 3, 64, 1, 1, 300), ("f32", 2, 128, 1, 40, 5),
+    ("bf16", 2, 128, 2, 0, 33), ("bf16", 8, 64, 9, 130, 1)])
+def test_gather(fmt, pooled, dtype, hkv, d, bsz, chunks, prefix):
+    rng = np.random.default_rng(d + 13 * chunks)
+    lay = wl.random_layout(rng, prefix, chunks, 1, 60) if chunks else wl.layout_from_lists(prefix, [], [])
+    cache, sparse, values, sparse_values = prompt(rng, dtype, hkv, d, fmt, lay, pooled)
+    masks = some_masks(rng, bsz, max(chunks, 1))[:, :chunks]
+    l_cap = lay.n_tokens + 7
+    wk, wv, wlen, wsrc = mixed(values, sparse_values, masks, lay, l_cap)
+    desc = vxl.make_desc(hkv, hkv, d, dtype)
+    kmix = torch.full((bsz, hkv, l_cap, d), 7.0, dtype=DTYPE[dtype], device="cuda")
+    vmix = torch.full_like(kmix, 7.0)
+    lens, src = torch.full((bsz,), -1, dtype=torch.int32, device="cuda"), torch.full((bsz, l_cap), -5, dtype=torch.int32, device="cuda")
+    dm = torch.from_numpy(np.ascontiguousarray(masks)).cuda() if chunks else None
+    gl = make_layout(lay)
+    for want_src in (True, False):
+        kmix.fill_(7.0), vmix.fill_(7.0), lens.fill_(-1)
+        vxl.gather_bilevel_kvq(gl, desc, cache, sparse, dm, kmix, vmix, lens, src if want_src else None)
+        assert np.array_equal(lens.cpu().numpy(), wlen)
+        for b in range(bsz):
+            n = int(wlen[b])
+            for got, want in ((kmix, wk), (vmix, wv)):
+                got = got[b].double().cpu().numpy()
+                assert np.array_equal(got[:, :n], want[b, :, :n]) and (got[:, n:] == 7.0).all()
+            assert np.array_equal(src[b, :n].cpu().numpy(), wsrc[b, :n]) and (src[b, n:] == -5).all()
+
+
+def test_gather_reports_an_overflow():
+    rng = np.random.default_rng(3)
+    lay = wl.random_layout(rng, 9, 6, 20, 50)
+    cache, _, values, _ = prompt(rng, "bf16", 2, 64, "fp4", lay, False)
+    masks = np.ones((2, lay.n_chunks), np.uint8)
+    masks[0] = 0
+    few = 9 + len(lay.sparse_idx)
+    desc, gl = vxl.make_desc(2, 2, 64, "bf16"), make_layout(lay)
+    kmix = torch.full((2, 2, few, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    vmix, lens = torch.full_like(kmix, 7.0), torch.zeros(2, dtype=torch.int32, device="cuda")
+    vxl.gather_bilevel_kvq(gl, desc, cache, None, torch.from_numpy(masks).cuda(), kmix, vmix, lens)
+    assert lens.tolist() == [few, -lay.n_tokens] and (kmix[1] == 7.0).all() and not (kmix[0] == 7.0).all()
+    qd = torch.ones(2, 1, 2, 64, dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.full_like(qd, 5.0), torch.zeros(2, 1, 2, device="cuda")
+    ws = vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, 2, 1, few))
+    vxl.bilevel_decode_kvq(gl, desc, qd, cache, None, torch.from_numpy(masks).cuda(), few, out, lse, lens, ws)
+    assert lens.tolist() == [few, -lay.n_tokens] and not out[1].any() and (lse[1] == -np.inf).all() and out[0].any()
+
+
+# ---- decode --------------------------------------------------------------------------------------
+def attention(qd, k, v, n, scale):
+    """float64 (O, LSE) [T, Hq, ...] over n rows, and sum p |v| and the largest sum |q k| and |logit| of a row."""
+    t, hq, d = qd.shape
+    g = hq // k.shape[0]
+    o, lse, av, aq = (np.zeros(s) for s in ((t, hq, d), (t, hq), (t, hq, d), (t, hq)))
+    for h in range(hq):
+        kk, vv = k[h // g, :n], v[h // g, :n]
+        s = scale * (qd[:, h].astype(np.float64) @ kk.T)
+        m = s.max(1, keepdims=True)
+        e = np.exp(s - m)
+        p = e / e.sum(1, keepdims=True)
+        o[:, h], av[:, h] = p @ vv, p @ np.abs(vv)
+        lse[:, h] = (m + np.log(e.sum(1, keepdims=True)))[:, 0]
+        aq[:, h] = scale * (np.abs(qd[:, h].astype(np.float64)) @ np.abs(kk).T).max(1)
+    return o, lse, av, aq
+
+
+def check_decode(rng, dtype, fmt, hq, hkv, d, t, lay, masks, pooled, q_gain=1.0, scale=0.0, l_cap=None):
+    cache, sparse, values, sparse_values = prompt(rng, dtype, hkv, d, fmt, lay, pooled)
+    bsz = masks.shape[0]
+    l_cap = lay.n_tokens if l_cap is None else l_cap
+    qd = (rng.standard_normal((bsz, t, hq, d)) * q_gain).astype(np.float32)
+    qd = wl.round_to_bf16(qd) if dtype == "bf16" else qd
+    wk, wv, wlen, _ = mixed(values, sparse_values, masks, lay, l_cap)
+    gl, desc = make_layout(lay), vxl.make_desc(hq, hkv, d, dtype, scale)
+    dq = vxl.to_device(qd, dtype)
+    dm = torch.from_numpy(np.ascontiguousarray(masks)).cuda() if lay.n_chunks else None
+    out, lse = torch.full_like(dq, np.nan), torch.full(dq.shape[:3], np.nan, device="cuda")
+    lens = torch.full((bsz,), -77, dtype=torch.int32, device="cuda")
+    ws = vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, bsz, t, l_cap))
+    ws.fill_(0xff)
+    vxl.bilevel_decode_kvq(gl, desc, dq, cache, sparse, dm, l_cap, out, lse, lens, ws)
+    assert np.array_equal(lens.cpu().numpy(), wlen)
+    again, only = torch.full_like(dq, np.nan), torch.full_like(dq, np.nan)
+    vxl.bilevel_decode_kvq(gl, desc, dq, cache, sparse, dm, l_cap, again, None, lens, ws, map_ready=True)
+    assert same_bits(out, again)                                    # the map reused, no LSE, no lengths asked for
+    vxl.bilevel_decode_kvq(gl, desc, dq, cache, sparse, dm, l_cap, only, None, None, ws)
+    assert same_bits(out, only)
+    got, got_lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    scale = scale or d ** -0.5
+    for b in range(bsz):
+        n = int(wlen[b])
+        if n == 0:
+            assert not got[b].any() and (got_lse[b] == -np.inf).all()
+            continue
+        o, wlse, av, aq = attention(qd[b], wk[b], wv[b], n, scale)
+        # A logit: fp32 sums of at most 12 steps of 32 products, its product with log2(e) and the subtraction from the
+        # reference, all of magnitude up to sum |q k|; an exponential 2 steps.  The sum over n keys in lanes, waves and
+        # splits: n / 16 + 100 steps.  bf16: every weight and the result are rounded by half a step, 2^-8.  The weights are
+        # exponentials against a reference that is a logit of the row, so that their sum is at least 1, and one below the
+        # smallest normal number, 2^-126, is 0: up to n times 2^-126 |v| is missing from the result.
+        logit = (44 + 4) * 2.0 ** -24 * aq * 1.5 + 2.0 ** -22
+        sums = (n / 16 + 100) * 2.0 ** -24
+        bound = av * (2 * logit + 2 * sums)[..., None] + n * 2.0 ** -126 * np.abs(wv[b, :, :n]).max()
+        if dtype == "bf16":
+            bound = bound + 1.01 * 2.0 ** -8 * (av + np.abs(o))
+        assert (np.abs(got[b] - o) <= bound).all(), float((np.abs(got[b] - o) / bound).max())
+        assert (np.abs(got_lse[b] - wlse) <= logit + sums + np.abs(wlse) * 2.0 ** -22).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("pooled", [False, True])
+@pytest.mark.parametrize("dtype,hq,hkv,d,t,bsz", [
+    ("bf16", 14, 2, 128, 1, 2), ("bf16", 14, 2, 64, 4, 1), ("bf16", 8, 1, 128, 2, 3), ("bf16", 4, 4, 64, 1, 9),
+    ("bf16", 28, 4, 128, 5, 2), ("bf16", 14, 2, 128, 18, 2), ("bf16", 14, 2, 64, 40, 1), ("bf16", 28, 4, 128, 64, 1),
+    ("bf16", 16, 1, 64, 1, 2), ("bf16", 17, 1, 128, 1, 2), ("f32", 2, 1, 64, 8, 1), ("f32", 14, 2, 128, 1, 2), ("f32", 6, 3, 64, 21, 3)])
+def test_decode(fmt, pooled, dtype, hq, hkv, d, t, bsz):
+    rng = np.random.default_rng(hq * 1000 + d + t)
+    lay = wl.random_layout(rng, 17, 11, 1, 150)
+    check_decode(rng, dtype, fmt, hq, hkv, d, t, lay, some_masks(rng, bsz, lay.n_chunks), pooled)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 130, 257])
+def test_decode_of_short_sets(dtype, n):
+    """A prefix alone, in buffers of its own size and in larger ones."""
+    rng = np.random.default_rng(n)
+    lay = wl.layout_from_lists(n, [], [])
+    masks = np.zeros((1, 0), np.uint8)
+    check_decode(rng, dtype, "fp4", 14, 2, 128, 1, lay, masks, False)
+    check_decode(rng, dtype, "fp8", 4, 2, 64, 3, lay, masks, False, l_cap=n + 1000)
+
+
+def test_decode_of_empty_sets():
+    """No prefix and no kept rows: a query without dense chunks attends to nothing."""
+    rng = np.random.default_rng(4)
+    lay = wl.layout_from_lists(0, [40, 3, 90], [[], [], []])
+    masks = np.array([[0, 0, 0], [0, 1, 0], [1, 1, 1]], np.uint8)
+    for dtype in ("bf16", "f32"):
+        for pooled in (False, True):
+            check_decode(rng, dtype, "fp4", 6, 2, 64, 2, lay, masks, pooled)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype,d,t,tokens,bsz", [("bf16", 128, 1, 20000, 1), ("bf16", 64, 3, 30001, 2), ("f32", 128, 2, 9000, 1),
+                                                  ("bf16", 128, 33, 9001, 2), ("bf16", 128, 1, 40000, 8)])
+def test_decode_of_long_sets(fmt, dtype, d, t, tokens, bsz):
+    """Many splits and many tiles per wave; two heads, values of wide range, logits of a few units and of dozens."""
+    rng = np.random.default_rng(tokens + t)
+    lens = [tokens // 7] * 7
+    lay = wl.layout_from_lists(130, lens, [np.arange(130 + i * lens[0], 130 + (i + 1) * lens[0], 5) for i in range(7)])
+    check_decode(rng, dtype, fmt, 4, 2, d, t, lay, some_masks(rng, bsz, 7), False, q_gain=0.02)
+    if bsz < 8:
+        check_decode(rng, dtype, fmt, 4, 1, d, t, lay, some_masks(rng, bsz, 7), True, q_gain=0.5)
+
+
+def test_decode_with_a_scale_of_its_own_and_steep_logits():
+    rng = np.random.default_rng(21)
+    lay = wl.random_layout(rng, 30, 5, 50, 200)
+    for dtype in ("bf16", "f32"):
+        check_decode(rng, dtype, "fp8", 6, 2, 64, 2, lay, some_masks(rng, 2, 5), False, scale=0.9)
+        check_decode(rng, dtype, "fp4", 6, 2, 128, 1, lay, some_masks(rng, 2, 5), False, scale=1e-3)
+        check_decode(rng, dtype, "fp4", 6, 2, 128, 1, lay, some_masks(rng, 2, 5), False, q_gain=20.0)
+
+
+def test_many_chunks():
+    """More chunks than a block's table of first rows holds."""
+    rng = np.random.default_rng(6)
+    lay = wl.random_layout(rng, 3, 4000, 1, 3)
+    masks = some_masks(rng, 3, 4000)
+    check_decode(rng, "bf16", "fp4", 4, 1, 64, 1, lay, masks, True)
+    cache, _, values, _ = prompt(rng, "bf16", 1, 64, "fp8", lay, False)
+    wk, wv, wlen, _ = mixed(values, None, masks, lay, lay.n_tokens)
+    kmix = torch.zeros(3, 1, lay.n_tokens, 64, dtype=torch.bfloat16, device="cuda")
+    vmix, lens = torch.zeros_like(kmix), torch.zeros(3, dtype=torch.int32, device="cuda")
+    vxl.gather_bilevel_kvq(make_layout(lay), vxl.make_desc(1, 1, 64, "bf16"), cache, None, torch.from_numpy(masks).cuda(), kmix, vmix, lens)
+    assert np.array_equal(lens.cpu().numpy(), wlen)
+    assert np.array_equal(kmix.double().cpu().numpy(), wk) and np.array_equal(vmix.double().cpu().numpy(), wv)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("t", [1, 40])
+def test_nan_rows_matter_where_they_are_attended_to(dtype, t):
+    """Block 1 of token 40's value and token 200's key are NaN; token 0, which is read in the place of rows that are not there,
+    is NaN altogether.  Queries with these tokens in a sparse chunk's unkept rows get the results without them."""
+    rng = np.random.default_rng(40)
+    lay = wl.layout_from_lists(0, [30, 70, 90, 101], [np.arange(c, c + 4) + 2 for c in (0, 30, 100, 190)])
+    hq, hkv, d, fmt = 6, 2, 128, "fp4"
+    k, v = random_rows(rng, (hkv, lay.n_tokens, d), dtype), random_rows(rng, (hkv, lay.n_tokens, d), dtype)
+    rows, scales, wk, wv = quantised(k, v, fmt)
+    scales[:, 40, 1, 1] = 255
+    scales[:, 200, 0, 3] = 255
+    scales[:, 0] = 255
+    desc, gl = vxl.make_desc(hq, hkv, d, dtype), make_layout(lay)
+    cache = device_cache(desc, fmt, rows, scales, spare=1)
+    masks = np.array([[0, 0, 1, 0], [0, 1, 1, 0], [0, 0, 0, 1], [1, 0, 0, 0]], np.uint8)
+    wkm, wvm, wlen, _ = oracle.gather_bilevel(wk, wv, masks, 0, lay.chunk_bounds, lay.sparse_offsets, lay.sparse_idx, l_cap=lay.n_tokens)
+    qd = rng.standard_normal((4, t, hq, d)).astype(np.float32) * 0.1
+    dq = vxl.to_device(wl.round_to_bf16(qd), dtype)
+    out, lse = torch.zeros_like(dq), torch.zeros(dq.shape[:3], device="cuda")
+    ws = vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, 4, t, lay.n_tokens))
+    vxl.bilevel_decode_kvq(gl, desc, dq, cache, None, torch.from_numpy(masks).cuda(), lay.n_tokens, out, lse, None, ws)
+    got, got_lse = out.double().cpu().numpy(), lse.cpu().numpy()
+    want, want_lse = oracle.decode_lse(wl.round_to_bf16(qd), wkm, wvm, wlen)
+    assert np.abs(got[0] - want[0]).max() <= 2.0 ** -6 * np.abs(wvm).max() and np.isfinite(got_lse[0]).all()
+    assert np.isnan(got[1][..., 32:64]).all() and np.isfinite(np.delete(got[1], np.s_[32:64], -1)).all()
+    assert np.abs(got_lse[1] - want_lse[1]).max() < 1e-4
+    assert np.isnan(got[2]).all() and np.isnan(got_lse[2]).all()
+    assert np.isnan(got[3]).all() and np.isnan(got_lse[3]).all()
+
+
+def test_queries_that_are_not_finite():
+    """A NaN or an infinity in one query row makes that row NaN and no other."""
+    rng = np.random.default_rng(41)
+    lay = wl.layout_from_lists(300, [], [])
+    for dtype in ("bf16", "f32"):
+        cache, _, _, _ = prompt(rng, dtype, 1, 64, "fp8", lay, False)
+        desc, gl = vxl.make_desc(5, 1, 64, dtype), make_layout(lay)
+        good = torch.randn(1, 7, 5, 64, device="cuda").to(DTYPE[dtype])
+        bad = good.clone()
+        bad[0, 2, 3, 10] = float("nan")
+        bad[0, 6, 0, 63] = float("inf")
+        ws = vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, 1, 7, 300))
+        outs = []
+        for q in (good, bad):
+            outs.append((torch.zeros_like(q), torch.zeros(q.shape[:3], device="cuda")))
+            vxl.bilevel_decode_kvq(gl, desc, q, cache, None, None, 300, *outs[-1], None, ws)
+        hit = torch.zeros(1, 7, 5, dtype=torch.bool, device="cuda")
+        hit[0, 2, 3] = hit[0, 6, 0] = True
+        assert outs[1][0][hit].isnan().all() and outs[1][1][hit].isnan().all()
+        assert outs[1][0][~hit].isfinite().all() and outs[1][1][~hit].isfinite().all()
+        assert (outs[0][0][~hit].float() - outs[1][0][~hit].float()).abs().max() <= 2.0 ** -6 * outs[0][0].float().abs().max()
+
+
+# ---- together, as they are used ------------------------------------------------------------------
+def test_a_prompt_in_a_quantised_cache():
+    """Chunk by chunk into the cache as the pre-filling ends them, pooled rows quantised beside; selection by the mean keys
+    of the plain cache; gather + plain decode and the decode in place agree, the in-place one also for the next tokens."""
+    rng = np.random.default_rng(99)
+    hq, hkv, d, t, top_k = 14, 2, 128, 6, 3
+    lay = wl.random_layout(rng, 40, 9, 60, 200)
+    gl, desc = make_layout(lay), vxl.make_desc(hq, hkv, d, "bf16", token_major=True)
+    n, n_sparse = lay.n_tokens, int(lay.sparse_offsets[-1])
+    q, k, v = (torch.randn(n, h, d, generator=torch.Generator("cuda").manual_seed(5 + h), device="cuda").bfloat16() for h in (hq, hkv, hkv))
+    out = torch.empty_like(q)
+    vxl.chunk_prefill(gl, desc, q, k, v, out, None, vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_PREFILL, gl, desc)))
+    cache, sparse = vxl.KvqCache(desc, "fp8", n), vxl.KvqCache(desc, "fp8", n_sparse)
+    for lo, hi in zip([0, *lay.chunk_bounds[:-1]], lay.chunk_bounds):
+        vxl.kvq_write(desc, k[lo:hi], v[lo:hi], cache, lo)
+    ksp, vsp = (torch.empty(hkv, n_sparse, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    vxl.pool_sparse_kv(gl, desc, k, v, ksp, vsp)
+    vxl.kvq_write(vxl.make_desc(hq, hkv, d, "bf16"), ksp, vsp, sparse)
+    whole = vxl.KvqCache(desc, "fp8", n)
+    vxl.kvq_write(desc, k, v, whole)
+    assert torch.equal(cache.rows, whole.rows) and torch.equal(cache.scales, whole.scales)
+    qd = torch.randn(2, t, hq, d, device="cuda").bfloat16()
+    idx, mask = torch.zeros(2, top_k, dtype=torch.int32, device="cuda"), torch.zeros(2, lay.n_chunks, dtype=torch.uint8, device="cuda")
+    vxl.chunk_score_topk(gl, desc, qd, k, top_k, idx, mask, workspace=vxl.alloc_workspace(
+        vxl.workspace_bytes(vxl.OP_SCORE_TOPK, gl, desc, 2, t)))
+    cap = gl.mixed_kv_capacity(top_k)
+    kmix = torch.zeros(2, hkv, cap, d, dtype=torch.bfloat16, device="cuda")
+    vmix, lens = torch.zeros_like(kmix), torch.zeros(2, dtype=torch.int32, device="cuda")
+    for sp in (None, sparse):
+        vxl.gather_bilevel_kvq(gl, desc, cache, sp, mask, kmix, vmix, lens)
+        a, b = torch.empty_like(qd), torch.empty_like(qd)
+        vxl.bilevel_decode(desc, qd, kmix, vmix, lens, a, None, vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE, None, desc, 2, t, cap)))
+        ws = vxl.alloc_workspace(max(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, 2, x, cap) for x in (1, t)))
+        lens2 = torch.zeros_like(lens)
+        vxl.bilevel_decode_kvq(gl, desc, qd, cache, sp, mask, cap, b, None, lens2, ws)
+        assert torch.equal(lens, lens2)
+        # each of the two rounds its weights and its result to bf16, by half a step (2^-8) of sum p |v| each at most
+        assert (a.float() - b.float()).abs().max() <= 4 * 2.0 ** -8 * vmix.float().abs().max()
+        for i in (0, t - 1):                                       # single tokens on the map that the question left
+            one, got = qd[:, i:i + 1].contiguous(), torch.empty_like(qd[:, :1])
+            vxl.bilevel_decode_kvq(gl, desc, one, cache, sp, mask, cap, got, None, lens2, ws, map_ready=True)
+            assert (got.float() - b[:, i:i + 1].float()).abs().max() <= 4 * 2.0 ** -8 * vmix.float().abs().max()
+        plain = vxl.KvqCache(desc, "fp8", n)                       # read back and written again: the same codes
+        back = [torch.empty_like(k) for _ in range(2)]
+        vxl.kvq_read(desc, cache, *back)
+        vxl.kvq_write(desc, *back, plain)
+        again = [torch.empty_like(k) for _ in range(2)]
+        vxl.kvq_read(desc, plain, *again)
+        assert all(torch.equal(x, y) for x, y in zip(back, again))
+
+
+def test_in_a_replayed_graph():
+    """Write, gather and both forms of the decode in one captured graph, replayed on new inputs with eager work in between."""
+    rng = np.random.default_rng(12)
+    lay = wl.random_layout(rng, 20, 6, 30, 90)
+    hq, hkv, d = 8, 2, 128
+    gl, desc = make_layout(lay), vxl.make_desc(hq, hkv, d, "bf16")
+    n = lay.n_tokens
+    k, v = (torch.randn(hkv, n, d, device="cuda").bfloat16() for _ in range(2))
+    qd = torch.randn(2, 1, hq, d, device="cuda").bfloat16()
+    mask = torch.from_numpy(some_masks(rng, 2, 6)).cuda()
+    cache = vxl.KvqCache(desc, "fp4", n)
+    kmix = torch.zeros(2, hkv, n, d, dtype=torch.bfloat16, device="cuda")
+    bufs = dict(kmix=kmix, vmix=torch.zeros_like(kmix), lens=torch.zeros(2, dtype=torch.int32, device="cuda"), a=torch.zeros_like(qd),
+                b=torch.zeros_like(qd), lse=torch.zeros(2, 1, hq, device="cuda"))
+    ws = vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, 2, 1, n))
+
+    def chain(x, ws):
+        vxl.kvq_write(desc, k, v, cache)
+        vxl.gather_bilevel_kvq(gl, desc, cache, None, mask, x["kmix"], x["vmix"], x["lens"])
+        vxl.bilevel_decode_kvq(gl, desc, qd, cache, None, mask, n, x["a"], x["lse"], x["lens"], ws)
+        vxl.bilevel_decode_kvq(gl, desc, qd, cache, None, mask, n, x["b"], None, x["lens"], ws, map_ready=True)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        chain(bufs, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain(bufs, ws)
+    for i in range(4):
+        for x in (k, v, qd):
+            x.copy_(torch.randn_like(x))
+        mask.copy_(torch.from_numpy(some_masks(rng, 2, 6)))
+        want = {name: torch.zeros_like(x) for name, x in bufs.items()}
+        chain(want, torch.empty_like(ws))
+        torch.cuda.synchronize()
+        for x in bufs.values():
+            x.fill_(3)
+        bufs["kmix"].zero_(), bufs["vmix"].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(same_bits(want[name], x) for name, x in bufs.items()), i
+        assert same_bits(bufs["a"], bufs["b"])
+
+
+def test_on_streams_of_their_own():
+    """Two streams with a workspace each, at once; results as on one."""
+    rng = np.random.default_rng(15)
+    lay = wl.random_layout(rng, 100, 8, 300, 900)
+    cache, sparse, _, _ = prompt(rng, "bf16", 2, 128, "fp4", lay, True)
+    gl, desc, n = make_layout(lay), vxl.make_desc(14, 2, 128, "bf16"), lay.n_tokens
+    qs = [torch.randn(1, t, 14, 128, device="cuda").bfloat16() for t in (1, 30)]
+    masks = [torch.from_numpy(m[None]).cuda() for m in some_masks(rng, 2, 8)]
+    work = [vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, 1, q.shape[1], n)) for q in qs]
+    want = [vxl.bilevel_decode_kvq(gl, desc, q, cache, sparse, m, n, torch.zeros_like(q), workspace=w) for q, m, w in zip(qs, masks, work)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    for _ in range(5):
+        got = [torch.zeros_like(q) for q in qs]
+        torch.cuda.synchronize()
+        for s, q, m, w, o in zip(streams, qs, masks, work, got):
+            vxl.bilevel_decode_kvq(gl, desc, q, cache, sparse, m, n, o, workspace=w, stream=s)
+        torch.cuda.synchronize()
+        assert all(same_bits(a, b) for a, b in zip(want, got))
+
+
+def test_refusals_with_a_layout():
+    rng = np.random.default_rng(16)
+    lay = wl.random_layout(rng, 10, 4, 20, 40)
+    cache, sparse, _, _ = prompt(rng, "bf16", 2, 64, "fp4", lay, True)
+    other, _, _, _ = prompt(rng, "bf16", 2, 64, "fp8", lay, False)
+    gl, desc, n = make_layout(lay), vxl.make_desc(4, 2, 64, "bf16"), lay.n_tokens
+    short = vxl.KvqCache(desc, "fp4", n - 1)
+    few = vxl.KvqCache(desc, "fp4", len(lay.sparse_idx) - 1)
+    mask = torch.zeros(1, 4, dtype=torch.uint8, device="cuda")
+    q = torch.zeros(1, 1, 4, 64, dtype=torch.bfloat16, device="cuda")
+    kmix = torch.zeros(1, 2, n, 64, dtype=torch.bfloat16, device="cuda")
+    vmix, out = torch.zeros_like(kmix), torch.full_like(q, 9.0)
+    lens = torch.full((1,), 9, dtype=torch.int32, device="cuda")
+    need = vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, 1, 1, n)
+    ws = vxl.alloc_workspace(need)
+
+    def refused(status, **kw):
+        a = dict(cache=cache, sparse=sparse, mask=mask, kmix=kmix, vmix=vmix, lens=lens, q=q, out=out, ws=ws[:need], cap=n)
+        a.update(kw)
+        if not {"q", "out", "ws"} & set(kw):
+            with pytest.raises(vxl.VxlError) as e:
+                vxl.gather_bilevel_kvq(gl, desc, a["cache"], a["sparse"], a["mask"], a["kmix"][:, :, :a["cap"]].contiguous(), a["vmix"],
+                                       a["lens"])
+            assert e.value.status == status
+        if not {"kmix", "vmix", "lens"} & set(kw):
+            with pytest.raises(vxl.VxlError) as e:
+                vxl.bilevel_decode_kvq(gl, desc, a["q"], a["cache"], a["sparse"], a["mask"], a["cap"], a["out"], None, a["lens"], a["ws"])
+            assert e.value.status == status
+
+    bad = vxl.VXL_ERR_INVALID_ARG
+    refused(bad, cache=short)
+    refused(bad, sparse=few)
+    refused(bad, sparse=other)                                    # of another format
+    refused(bad, mask=None)
+    refused(bad, cap=gl.mixed_kv_capacity(0) - 1)
+    refused(bad, lens=None)
+    refused(bad, q=out)
+    refused(vxl.VXL_ERR_WORKSPACE, ws=ws[:need - 1])
+    refused(vxl.VXL_ERR_WORKSPACE, ws=None)
+    torch.cuda.synchronize()
+    assert (out == 9.0).all() and (lens == 9).all() and not kmix.any()
