@@ -388,6 +388,7 @@ vxl_status vxl_kv_store_reload(vxl_kv_store* store, const uint8_t* dense_mask, i
  * Both buffers 16-byte aligned.  What the calls below read has been written by vxl_kvq_write, or holds codes and scale bytes
  * of 17 to 252 or 255.  The descriptor gives heads, head_dim and the type and strides of the plain tensors.
  */
+#define VXL_KVQ_MAX_ROWS (1 << 24)   /* capacity of a cache at most (the codes of a KV head are addressed in 32 bits) */
 typedef enum { VXL_KVQ_FP8 = 0, VXL_KVQ_FP4 = 1 } vxl_kvq_format;
 typedef struct {
     void* rows;

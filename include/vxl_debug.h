@@ -84,6 +84,10 @@ double vxl_debug_tile_loop(int mode, const void* kv, float* out, int n_workgroup
  * vxl_status value (0 = launched). */
 int vxl_debug_read_stream(const void* src, size_t bytes, float* out, int n_workgroups, void* stream);
 
+/* The kernel of a vxl_bilevel_decode_kvq call (host only): 1 or 2 = 16-row blocks of a workgroup whose waves walk keys of
+ * their own, 0 = the kernel of many rows; *n_split its key splits. */
+int vxl_debug_kvq_plan(const vxl_attn_desc* desc, int batch, int n_q_tokens, int l_cap, int* n_split);
+
 #ifdef __cplusplus
 }
 #endif

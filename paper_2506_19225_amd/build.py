@@ -15,7 +15,7 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libvxl.so")
 BINDING = os.path.join(PKG, "_vxl_torch" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
-SOURCES = ["vxl_api.hip", "vxl_simple.hip", "vxl_f32.hip", "vxl_bilevel.hip", "vxl_prefill.hip", "vxl_decode.hip", "vxl_mass.hip", "vxl_kvq.hip", "vxl_store.hip", "vxl_debug.hip"]
+SOURCES = ["vxl_api.hip", "vxl_simple.hip", "vxl_f32.hip", "vxl_bilevel.hip", "vxl_prefill.hip", "vxl_decode.hip", "vxl_mass.hip", "vxl_kvq.hip", "vxl_kvq_decode.hip", "vxl_store.hip", "vxl_debug.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=default",

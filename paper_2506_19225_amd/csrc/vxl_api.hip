@@ -649,7 +649,7 @@ vxl_status vxl_bilevel_decode_inplace(const vxl_layout* L, const vxl_attn_desc* 
 static bool cache_ok(const vxl_kvq_cache* c, vxl_status* st) {
     *st = VXL_ERR_INVALID_ARG;
     if (!c || !c->rows || !c->scales || !aligned16(c->rows) || !aligned16(c->scales) || c->capacity <= 0) return false;
-    if (c->format != VXL_KVQ_FP8 && c->format != VXL_KVQ_FP4) { *st = VXL_ERR_UNSUPPORTED; return false; }
+    if ((c->format != VXL_KVQ_FP8 && c->format != VXL_KVQ_FP4) || c->capacity > VXL_KVQ_MAX_ROWS) { *st = VXL_ERR_UNSUPPORTED; return false; }
     return true;
 }
 

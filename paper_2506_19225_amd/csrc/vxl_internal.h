@@ -239,7 +239,9 @@ vxl_status launch_kvq_gather(const vxl_layout* L, const vxl_attn_desc* d, const 
                              const uint8_t* dense_mask, int batch, void* Kmix, void* Vmix, int l_cap, int32_t* mix_len,
                              int32_t* src_idx, hipStream_t s);
 struct KvqPlan {
-    int n_rtile, n_split, tiles_per_wave;      // 16-row tiles; key splits per (query, KV head); 32-key tiles of a wave
+    int blocks;                                // 16-row blocks of a workgroup; 0: the kernel of many rows
+    int waves;                                 // of that one, per workgroup
+    int n_rtile, n_split;                      // workgroups for the rows; key splits per (query, KV head)
     size_t part_ml, total;                     // byte offset of the (reference, sum) of the partial results, bytes of both
 };
 KvqPlan kvq_plan(const vxl_attn_desc* d, int batch, int T, int l_cap);

@@ -126,6 +126,8 @@ def lib() -> C.CDLL:
     L.vxl_debug_decode_plan.restype = C.c_int
     L.vxl_debug_decode_ring_waves.argtypes = [dp, C.c_int, C.c_int, C.c_int, C.c_int]
     L.vxl_debug_decode_ring_waves.restype = C.c_int
+    L.vxl_debug_kvq_plan.argtypes = [dp, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_int)]
+    L.vxl_debug_kvq_plan.restype = C.c_int
     L.vxl_debug_gather_shared.argtypes = [dp, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int]
     L.vxl_debug_gather_shared.restype = C.c_int
     L.vxl_debug_mfma_stream.argtypes = [vp, C.c_int, C.c_int, vp]
@@ -484,6 +486,13 @@ def debug_decode_plan(desc: AttnDesc, batch: int, n_q_tokens: int, l_cap: int, i
 def debug_decode_ring_waves(desc: AttnDesc, batch: int, n_q_tokens: int, l_cap: int, in_place: bool = False) -> int:
     """Waves (8 or 4) of the ring's workgroups for such a call on 256 compute units.  Needs no GPU."""
     return lib().vxl_debug_decode_ring_waves(C.byref(desc), batch, n_q_tokens, l_cap, int(in_place))
+
+
+def debug_kvq_plan(desc: AttnDesc, batch: int, n_q_tokens: int, l_cap: int):
+    """(kernel, key splits) of a bilevel_decode_kvq call; kernel: 16-row blocks of a workgroup, 0 = the one of many rows.  Needs no GPU."""
+    n_split = C.c_int(0)
+    kernel = lib().vxl_debug_kvq_plan(C.byref(desc), batch, n_q_tokens, l_cap, C.byref(n_split))
+    return kernel, n_split.value
 
 
 def debug_gather_shared(desc: AttnDesc, n_tokens: int, n_sparse: int, n_chunks: int, batch: int, l_cap: int) -> bool:

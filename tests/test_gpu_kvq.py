@@ -319,6 +319,38 @@ def test_decode_of_long_sets(fmt, dtype, d, t, tokens, bsz):
         check_decode(rng, dtype, fmt, 4, 1, d, t, lay, some_masks(rng, bsz, 7), True, q_gain=0.5)
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("pooled", [False, True])
+@pytest.mark.parametrize("hq,hkv,d,t,bsz,tokens", [(32, 4, 64, 129, 1, 6000), (32, 4, 128, 129, 1, 6000), (8, 4, 128, 200, 32, 700),
+                                                   (14, 2, 64, 129, 32, 700)])
+def test_decode_of_many_rows(fmt, pooled, hq, hkv, d, t, bsz, tokens):
+    """The kernel whose workgroups convert a tile for all their rows: row tiles and key tiles that are not full, several splits
+    and one, splits without keys, queries without any."""
+    rng = np.random.default_rng(tokens + d + t)
+    cuts = np.sort(rng.choice(np.arange(1, tokens), size=6, replace=False))
+    lens = np.diff(np.concatenate([[0], cuts, [tokens]]))
+    starts = np.concatenate([[0], cuts])
+    kept = [np.sort(rng.choice(n, size=n // 9, replace=False)).astype(np.int32) + s for n, s in zip(lens, starts)]
+    lay = wl.layout_from_lists(0, [int(n) for n in lens], kept)
+    masks = some_masks(rng, bsz, lay.n_chunks)
+    masks[-1] = np.arange(lay.n_chunks) == 3
+    desc = vxl.make_desc(hq, hkv, d, "bf16")
+    kernel, n_split = vxl.debug_kvq_plan(desc, bsz, t, lay.n_tokens)
+    assert kernel == 0 and (n_split > 1) == (bsz == 1)
+    check_decode(rng, "bf16", fmt, hq, hkv, d, t, lay, masks, pooled, q_gain=0.1)
+
+
+def test_plans():
+    """The kernels and numbers of splits that these tests are meant to reach."""
+    plan = lambda hq, hkv, d, dtype, b, t, cap: vxl.debug_kvq_plan(vxl.make_desc(hq, hkv, d, dtype), b, t, cap)  # noqa: E731
+    assert plan(14, 2, 128, "bf16", 2, 1, 900)[0] == 1 and plan(14, 2, 128, "bf16", 2, 1, 900)[1] > 1
+    assert plan(14, 2, 128, "bf16", 1, 1, 128) == (1, 1)
+    assert plan(14, 2, 128, "bf16", 2, 18, 900)[0] == plan(28, 4, 128, "bf16", 1, 64, 900)[0] == 2
+    assert plan(6, 3, 64, "f32", 3, 21, 900)[0] == 1
+    assert plan(4, 2, 128, "bf16", 1, 1, 20000)[1] > 64
+    assert plan(4, 1, 64, "bf16", 2, 3, 30001)[1] > 32
+
+
 def test_decode_with_a_scale_of_its_own_and_steep_logits():
     rng = np.random.default_rng(21)
     lay = wl.random_layout(rng, 30, 5, 50, 200)
