@@ -121,9 +121,23 @@ struct Place {
     }
 };
 
+// x of another lane of the same 16 (CTRL: the DPP control).
+template <int CTRL>
+__device__ __forceinline__ uint32_t from_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true); }
+constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e, kMirror8 = 0x141, kShiftLeft = 0x100;
+
+// 16 bytes that the caches need not keep (NT)
+template <bool NT>
+__device__ __forceinline__ void store16(uint4* p, uint4 v) {
+    typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+    if constexpr (NT) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
+    else *p = v;
+}
+
 // ------------------------------------------------------------------------------------------
 // Rows [first, first + n_rows) of the cache from K and V: a lane takes 16 bytes of a key row and of its value row, the lanes
-// of a block find its largest magnitude by exchange.
+// of a block find its largest magnitude by exchange, and the first lane of 16 stores the scales of all of them.
+// Bound by HBM: 131,328 rows of four heads, 408 MB in and out, 70.5 us (5.8 TB/s), 16,640 rows 8.0.
 // ------------------------------------------------------------------------------------------
 template <int D, int BITS, bool F32>
 __global__ __launch_bounds__(256) void kvq_write_kernel(const uint4* __restrict__ K, const uint4* __restrict__ V,
@@ -131,88 +145,123 @@ __global__ __launch_bounds__(256) void kvq_write_kernel(const uint4* __restrict_
                                                         KvqView c, long long first) {
     using P = Piece<F32, BITS>;
     constexpr int LPR = D / P::N, LPB = kBlock / P::N;        // lanes per row, per block
+    constexpr int TOGETHER = std::min(16 / LPB, D / kBlock);  // scales that one lane stores, of the keys and of the values
     const long long id = (long long)folded_id() * 256 + threadIdx.x;
     if (id >= n_rows * n_heads * LPR) return;                 // (all lanes of a row)
     const Place<LPR> at(id, n_rows);
     const long long src = at.g * head_u4 + at.r * tok_u4 + at.part;
     const uint4 x[2] = {K[src], V[src]};
     const long long row = at.g * c.capacity + first + at.r;
+    uint32_t bytes[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         uint32_t peak = P::peak(x[i]);
-#pragma unroll
-        for (int o = 1; o < LPB; o <<= 1) peak = max(peak, (uint32_t)__shfl_xor((int)peak, o));
+        peak = max(peak, from_lane<kSwap1>(peak));
+        peak = max(peak, from_lane<kSwap2>(peak));
+        if constexpr (LPB == 8) peak = max(peak, from_lane<kMirror8>(peak));
         const uint32_t byte = scale_byte<BITS>(peak);
         uint32_t code[2] = {0, 0};
         if (byte != 255) P::encode(x[i], scale_of(byte), code);
         P::store(c.rows + row * KvqRow<D, BITS>::CODES + i * (D * BITS / 8) + at.part * P::CB, code);
-        if (at.part % LPB == 0) c.scales[row * KvqRow<D, BITS>::SCALES + i * (D / kBlock) + at.part / LPB] = (uint8_t)byte;
+        bytes[i] = byte;
+        if constexpr (TOGETHER > 1) bytes[i] |= from_lane<kShiftLeft + LPB>(byte) << 8;
+        if constexpr (TOGETHER > 2) bytes[i] |= from_lane<kShiftLeft + 2 * LPB>(byte) << 16 | from_lane<kShiftLeft + 3 * LPB>(byte) << 24;
+    }
+    if (at.part % (LPB * TOGETHER) == 0) {
+        uint8_t* p = c.scales + row * KvqRow<D, BITS>::SCALES + at.part / LPB;
+        if constexpr (TOGETHER == 4) *(uint2*)p = make_uint2(bytes[0], bytes[1]);
+        else if constexpr (TOGETHER == D / kBlock) *(uint32_t*)p = bytes[0] | bytes[1] << 16;
+        else {
+            *(uint16_t*)p = (uint16_t)bytes[0];
+            *(uint16_t*)(p + D / kBlock) = (uint16_t)bytes[1];
+        }
     }
 }
 
-// K and V from rows [first, first + n_rows) of the cache.
+// The codes and scales of 16 bytes of a key row and of its value row as a lane reads them.
+template <int D, int BITS, bool F32>
+struct PiecePair {
+    using P = Piece<F32, BITS>;
+    uint32_t code[2][2];
+    uint32_t byte[2];
+    __device__ __forceinline__ void load(const KvqView& c, long long row, int part) {
+        constexpr int LPB = kBlock / P::N;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            P::load(c.rows + row * KvqRow<D, BITS>::CODES + i * (D * BITS / 8) + part * P::CB, code[i]);
+            byte[i] = c.scales[row * KvqRow<D, BITS>::SCALES + i * (D / kBlock) + part / LPB];
+        }
+    }
+    template <bool NT = false>
+    __device__ __forceinline__ void store(uint4* k, uint4* v) const {
+        store16<NT>(k, P::decode(code[0], scale_of(byte[0])));
+        store16<NT>(v, P::decode(code[1], scale_of(byte[1])));
+    }
+};
+
+// K and V from rows [first, first + n_rows) of the cache.  Bound by HBM, at the same rates.
 template <int D, int BITS, bool F32>
 __global__ __launch_bounds__(256) void kvq_read_kernel(uint4* __restrict__ K, uint4* __restrict__ V, long long head_u4,
                                                        long long tok_u4, long long n_rows, int n_heads, KvqView c,
                                                        long long first) {
-    using P = Piece<F32, BITS>;
-    constexpr int LPR = D / P::N, LPB = kBlock / P::N;
+    constexpr int LPR = D / Piece<F32, BITS>::N;
     const long long id = (long long)folded_id() * 256 + threadIdx.x;
     if (id >= n_rows * n_heads * LPR) return;
     const Place<LPR> at(id, n_rows);
-    const long long row = at.g * c.capacity + first + at.r, dst = at.g * head_u4 + at.r * tok_u4 + at.part;
-    uint32_t code[2][2];
-    float scale[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        P::load(c.rows + row * KvqRow<D, BITS>::CODES + i * (D * BITS / 8) + at.part * P::CB, code[i]);
-        scale[i] = scale_of(c.scales[row * KvqRow<D, BITS>::SCALES + i * (D / kBlock) + at.part / LPB]);
-    }
-    K[dst] = P::decode(code[0], scale[0]);
-    V[dst] = P::decode(code[1], scale[1]);
+    const long long dst = at.g * head_u4 + at.r * tok_u4 + at.part;
+    PiecePair<D, BITS, F32> x;
+    x.load(c, at.g * c.capacity + first + at.r, at.part);
+    x.store(K + dst, V + dst);
 }
 
 // ------------------------------------------------------------------------------------------
-// Mixed sets of plain KVs from the quantised rows: the blocks find their rows as those of the plain gather do, a group of
-// LPR lanes per row reads codes and scales and writes 16 bytes of keys and of values each, head by head.
+// Mixed sets of plain KVs from the quantised rows: the blocks find their rows as those of the plain gather do, and a group of
+// LPR lanes per row reads codes and scales of HEADS KV heads and writes 16 bytes of keys and of values of each.  The queries
+// of a batch take turns, so that the cache's rows stay on the chip for all of them, and sets that would push them out of there
+// are stored past the caches (kPastCaches, by their rows).
+// Bound by the writes.  us: eight sets of 25k rows of 8 bits, 497 MB, one head after the other 141, four together 123, past the
+// caches 96 (5.2 TB/s); one set of 45,312 rows of 4 bits 40 -> 31 -> 28; queries one after the other instead of in turn 129.
 // ------------------------------------------------------------------------------------------
-template <int D, int BITS, bool F32>
+constexpr long long kPastCaches = 160ll << 20;
+
+template <int D, int BITS, bool F32, int HEADS>
 __global__ __launch_bounds__(256) void kvq_gather_kernel(KvqView dense, KvqView sparse, bool pooled,
                                                          const uint8_t* __restrict__ dense_mask, const int32_t* __restrict__ bounds,
                                                          const int32_t* __restrict__ soff, const int32_t* __restrict__ sidx,
-                                                         int n_chunks, int n_prefix, int n_kv_heads, int l_cap, int groups,
+                                                         int n_chunks, int n_prefix, int n_kv_heads, int l_cap, int groups, int batch,
                                                          uint4* __restrict__ Kmix, uint4* __restrict__ Vmix,
                                                          int32_t* __restrict__ mix_len, int32_t* __restrict__ src_idx) {
-    using P = Piece<F32, BITS>;
-    constexpr int LPR = D / P::N, LPB = kBlock / P::N, ROWS = 256 / LPR;
+    constexpr int LPR = D / Piece<F32, BITS>::N, ROWS = 256 / LPR;
     extern __shared__ int off[];
     int* from = off + n_chunks;
     const bool table = n_chunks <= kTableChunks;
     __shared__ int wave_tot[4][4];
-    const int tid = threadIdx.x, part = tid % LPR, b = blockIdx.y, block = blockIdx.x;
+    const int tid = threadIdx.x, part = tid % LPR;
+    const unsigned id = folded_id();
+    const int b = (int)(id % batch), block = (int)(id / batch);
     const int len = scan_mixed_rows(dense_mask + (size_t)b * n_chunks, bounds, soff, n_chunks, n_prefix, off, from, table, wave_tot);
     // a mixed set that does not fit l_cap is reported, not truncated: minus the rows it needs
     if (block == 0 && tid == 0) mix_len[b] = len <= l_cap ? len : -len;
     if (len > l_cap) return;
+    const bool past = 2ll * batch * n_kv_heads * len * (LPR * 16) > kPastCaches;
     for (int gi = 0; gi < groups; ++gi) {
-        const int r = (block * groups + gi) * ROWS + tid / LPR;
-        if (r >= len) break;                                  // (rows ascend with gi; the lanes of a row together)
+        const long long r_ = ((long long)block * groups + gi) * ROWS + tid / LPR;
+        if (r_ >= len) break;                                 // (rows ascend with gi; the lanes of a row together)
+        const int r = (int)r_;
         const int src = mixed_row_source<LPR>(r, n_prefix, n_chunks, off, from, table, bounds, soff, sidx, pooled);
         if (src_idx && part == 0) src_idx[(size_t)b * l_cap + r] = src;
         const KvqView& c = src >= 0 ? dense : sparse;
         const long long row0 = src >= 0 ? src : ~src;
-        for (int g = 0; g < n_kv_heads; ++g) {
-            const long long row = g * c.capacity + row0;
-            const size_t dst = (((size_t)b * n_kv_heads + g) * l_cap + r) * LPR + part;
-            uint32_t code[2][2];
-            float scale[2];
+        const size_t head = (size_t)l_cap * LPR, dst = ((size_t)b * n_kv_heads * l_cap + r) * LPR + part;
+        for (int g0 = 0; g0 < n_kv_heads; g0 += HEADS) {
+            PiecePair<D, BITS, F32> x[HEADS];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                P::load(c.rows + row * KvqRow<D, BITS>::CODES + i * (D * BITS / 8) + part * P::CB, code[i]);
-                scale[i] = scale_of(c.scales[row * KvqRow<D, BITS>::SCALES + i * (D / kBlock) + part / LPB]);
-            }
-            Kmix[dst] = P::decode(code[0], scale[0]);
-            Vmix[dst] = P::decode(code[1], scale[1]);
+            for (int g = 0; g < HEADS; ++g) x[g].load(c, (g0 + g) * c.capacity + row0, part);
+            auto store = [&](auto nt) __attribute__((always_inline)) {
+#pragma unroll
+                for (int g = 0; g < HEADS; ++g) x[g].template store<nt>(Kmix + dst + (g0 + g) * head, Vmix + dst + (g0 + g) * head);
+            };
+            if (past) store(std::true_type{}); else store(std::false_type{});
         }
     }
 }
@@ -248,11 +297,18 @@ vxl_status launch_kvq_gather(const vxl_layout* L, const vxl_attn_desc* d, const 
     return by_kind(d, c, [&](auto dim, auto bits, auto f32) {
         constexpr int rows = 256 / (dim / Piece<f32, bits>::N);
         const long long passes = ((long long)l_cap + rows - 1) / rows;
-        const int groups = (int)std::max<long long>(1, std::min<long long>(8, passes * batch / 512));
+        // passes of a block: one, more where the scan of many chunks is to be shared and blocks enough are left (us, one, two,
+        // four passes: 256 chunks 27.9, 30.1, 30.3, 640 chunks 56.5, 56.0, 57.3, 3,500 chunks 157, 116, 96)
+        const int groups = (int)std::max<long long>(1, std::min<long long>(std::min(8, 1 + L->n_chunks / 512), passes * batch / 512));
         const size_t lds = (size_t)L->n_chunks * (L->n_chunks <= kTableChunks ? 2 : 1) * sizeof(int);
-        hipLaunchKernelGGL((kvq_gather_kernel<dim, bits, f32>), dim3((unsigned)((passes + groups - 1) / groups), batch), dim3(256), lds, s,
-                           view(c), view(sp), sp != nullptr, dense_mask, L->d_bounds, L->d_soff, L->d_sidx, L->n_chunks, L->n_prefix,
-                           d->n_kv_heads, l_cap, groups, (uint4*)Kmix, (uint4*)Vmix, mix_len, src_idx);
+        auto run = [&](auto heads) {
+            hipLaunchKernelGGL((kvq_gather_kernel<dim, bits, f32, heads>), folded_grid((passes + groups - 1) / groups * batch), dim3(256), lds,
+                               s, view(c), view(sp), sp != nullptr, dense_mask, L->d_bounds, L->d_soff, L->d_sidx, L->n_chunks, L->n_prefix,
+                               d->n_kv_heads, l_cap, groups, batch, (uint4*)Kmix, (uint4*)Vmix, mix_len, src_idx);
+        };
+        if (d->n_kv_heads % 4 == 0) run(std::integral_constant<int, 4>{});
+        else if (d->n_kv_heads % 2 == 0) run(std::integral_constant<int, 2>{});
+        else run(std::integral_constant<int, 1>{});
         return launched();
     });
 }
