@@ -431,7 +431,8 @@ vxl_status vxl_gather_bilevel_kvq(const vxl_layout* layout, const vxl_attn_desc*
  * the workspace sized by vxl_workspace_bytes(VXL_OP_DECODE_KVQ, layout, desc, batch, n_q_tokens, l_cap), never less.
  * O and LSE are those of the attention over the values that the cache reads back as, within the tolerance of the path; the
  * same call gives the same bits.  A row whose logits include NaN or +inf, or are all -inf, and one that attends to a NaN
- * value, are NaN; what a query does not attend to never matters.
+ * value, are NaN; what a query does not attend to never matters.  256 times the sum of a row's attended |value| has to be finite.
+ * VXL_ERR_UNSUPPORTED if batch times the row tiles of a query, 16, 32 or 256 stacked rows each by size and type, exceeds 65,535.
  */
 vxl_status vxl_bilevel_decode_kvq(const vxl_layout* layout, const vxl_attn_desc* desc, const void* Qd, int32_t batch,
                                   int32_t n_q_tokens, const vxl_kvq_cache* cache, const vxl_kvq_cache* sparse,

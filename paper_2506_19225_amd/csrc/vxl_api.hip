@@ -722,6 +722,7 @@ vxl_status vxl_bilevel_decode_kvq(const vxl_layout* L, const vxl_attn_desc* d, c
     if ((st = kvq_sets_ok(L, cache, sparse, dense_mask, batch, l_cap, &sp)) != VXL_OK) return st;
     if (!Qd || !O || n_q_tokens <= 0 || !aligned16(Qd) || !aligned16(O) || O == Qd) return VXL_ERR_INVALID_ARG;
     const KvqPlan p = kvq_plan(d, batch, n_q_tokens, l_cap);
+    if (!p.fits) return VXL_ERR_UNSUPPORTED;
     const InplaceWorkspace w = inplace_workspace(batch, l_cap, p.total);
     if (!workspace || workspace_bytes < w.total || !aligned16(workspace)) return VXL_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;

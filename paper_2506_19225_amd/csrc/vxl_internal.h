@@ -241,7 +241,9 @@ vxl_status launch_kvq_gather(const vxl_layout* L, const vxl_attn_desc* d, const 
 struct KvqPlan {
     int blocks;                                // 16-row blocks of a workgroup; 0: the kernel of many rows
     int waves;                                 // of that one, per workgroup
-    int n_rtile, n_split;                      // workgroups for the rows; key splits per (query, KV head)
+    long long n_rtile;                         // workgroups for the rows
+    int n_split;                               // key splits per (query, KV head)
+    bool fits;                                 // the grid of the call is one that there can be
     size_t part_ml, total;                     // byte offset of the (reference, sum) of the partial results, bytes of both
 };
 KvqPlan kvq_plan(const vxl_attn_desc* d, int batch, int T, int l_cap);

@@ -1,5 +1,6 @@
 // Decode attention over a quantised KV cache, its rows read in place through a row map (bf16 and fp32 queries, matrix cores).
 #include <algorithm>
+#include <limits>
 #include <numeric>
 
 #include "vxl_kvq.h"
@@ -45,15 +46,25 @@ __device__ __forceinline__ bool kvq_place(int n_kv_heads, int n_split, int n_rti
 
 constexpr int kKvqTile = 32, kKvqWaves = 4;
 
+// A wave's reference, in the units that weights are exponentials of, before it has met a logit above -inf: the first one that
+// it meets raises it, and a logit of -inf has weight 0.
+constexpr float kLowest = -std::numeric_limits<float>::max();
+
 template <bool F32> struct Parts { static constexpr int N = F32 ? 3 : 1; };
 
-// x as bf16 parts, each the rounding of what the ones before it leave.
+// x as one bf16 number, rounded, or as three that add up to it: the upper 8 of the 24 bits, of what is left, and the rest.  They
+// have one sign, and the first is no larger than x: a product that overflows does so in the direction of the whole.
 template <int N>
 __device__ __forceinline__ void split_bf16(float x, __bf16 (&part)[N]) {
+    if constexpr (N == 1) {
+        part[0] = (__bf16)x;
+    } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        part[i] = (__bf16)x;
-        if (i + 1 < N) x -= (float)part[i];
+        for (int i = 0; i < N; ++i) {
+            const uint32_t upper = __float_as_uint(x) & 0xffff0000u;
+            part[i] = __builtin_bit_cast(__bf16, (uint16_t)(upper >> 16));
+            x -= __uint_as_float(upper);
+        }
     }
 }
 
@@ -195,7 +206,7 @@ __global__ __launch_bounds__(64 * kKvqWaves, NB == 1 ? 3 : 2) void kvq_decode_ke
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         m_run[nb] = -INFINITY;
-        mc_run[nb] = -INFINITY;                               // (weights are infinite or NaN: the first tile sets it)
+        mc_run[nb] = kLowest;
         l_run[nb] = 0.f;
 #pragma unroll
         for (int i = 0; i < M; ++i) o[nb][i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -480,7 +491,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kvq_rows_kernel(
         for (int ks = 0; ks < D / 16; ++ks) qreg[0][ks] = __builtin_bit_cast(bf16x8, src[ks * 2 + hi]);
     }
     f32x16 o[DB];
-    float m_run = -INFINITY, mc_run = -INFINITY, l_run = 0.f;
+    float m_run = -INFINITY, mc_run = kLowest, l_run = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db] = zero16();
     const int dhalf = (lane >> 4) & 1, t = lane & 15;
@@ -673,7 +684,7 @@ static KvqPlan kvq_splits(const vxl_attn_desc* d, int batch, long long rows, int
     p.blocks = blocks;
     p.waves = waves;
     const int wg_rows = blocks ? 16 * blocks : 32 * waves, wg_keys = blocks ? kKvqTile * kKvqWaves : kKeyTile;
-    p.n_rtile = (int)((rows + wg_rows - 1) / wg_rows);
+    p.n_rtile = (rows + wg_rows - 1) / wg_rows;
     const long long units = (long long)batch * d->n_kv_heads, per = units * p.n_rtile;
     const long long steps = ((long long)l_cap + wg_keys - 1) / wg_keys;           // of a workgroup that has all keys
     const bool d64 = d->head_dim == 64;
@@ -693,6 +704,7 @@ static KvqPlan kvq_splits(const vxl_attn_desc* d, int batch, long long rows, int
             p.n_split = (int)n;
         }
     }
+    p.fits = p.n_rtile * batch <= 65535 && (long long)d->n_kv_heads * p.n_split <= 65535ll * kXcds;
     if (p.n_split > 1) {
         p.part_ml = align_up((size_t)units * p.n_split * rows * d->head_dim * sizeof(float), 256);
         p.total = p.part_ml + align_up((size_t)units * p.n_split * rows * sizeof(float2), 256);
@@ -706,8 +718,8 @@ KvqPlan kvq_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     if (d->dtype != VXL_BF16 || rows <= 16) return kvq_splits(d, batch, rows, l_cap, 1, 0, &us);
     const KvqPlan p = kvq_splits(d, batch, rows, l_cap, 2, 0, &us);
     if (rows <= 128) return p;
-    // (448 rows x 8 queries, 45,312 keys 413 -> 358 us, 392 rows x 3, 111,488 keys 505 -> 343; but 868 rows, 3,072 keys 22.7
-    // against 27.8, 686 x 8, 11,008 keys 185 and 201)
+    // (448 rows x 8 queries, 45,312 keys 413 -> 358 us, 392 rows x 3, 111,488 keys 505 -> 343; but 686 rows x 8, 11,008 keys
+    // 185 against 201)
     const KvqPlan many = kvq_splits(d, batch, rows, l_cap, 0, kRowsWaves, &us_many);
     return us_many < us ? many : p;
 }
@@ -724,17 +736,15 @@ vxl_status launch_kvq_decode(const KvqPlan& p, const vxl_attn_desc* d, float sca
                              const int32_t* mix_len, void* O, float* LSE, void* ws, hipStream_t s) {
     float* part_o = (float*)ws;
     float2* part_ml = (float2*)((char*)ws + p.part_ml);
-    const int pairs = d->n_kv_heads * p.n_split;
-    const long long members = (long long)p.n_rtile * batch;
-    const dim3 grid(std::min(pairs, kXcds), (unsigned)members, (pairs + kXcds - 1) / kXcds);
-    if (members > 65535 || grid.z > 65535) return VXL_ERR_UNSUPPORTED;
+    const int pairs = d->n_kv_heads * p.n_split, n_rtile = (int)p.n_rtile;
+    const dim3 grid(std::min(pairs, kXcds), n_rtile * batch, (pairs + kXcds - 1) / kXcds);
     const int tiles = (l_cap - 1) / kKvqTile + 1;
     return by_kind(d, c, [&](auto dim, auto bits, auto f32) {
         using T_ = typename Elem<f32>::T;
         auto run = [&](auto pooled, auto nb) {
             hipLaunchKernelGGL((kvq_decode_kernel<dim, bits, f32, pooled, nb>), grid, dim3(64 * kKvqWaves), 0, s,
                                (const T_*)Qd, view(c), view(sp), src_idx, mix_len, part_o, part_ml, T, d->n_q_heads, d->n_kv_heads,
-                               l_cap, p.n_split, tiles / p.n_split, tiles % p.n_split, p.n_rtile, scale * kLog2e, (T_*)O, LSE);
+                               l_cap, p.n_split, tiles / p.n_split, tiles % p.n_split, n_rtile, scale * kLog2e, (T_*)O, LSE);
         };
         auto rows = [&](auto pooled) {
             if constexpr (!f32) {
@@ -753,7 +763,7 @@ vxl_status launch_kvq_decode(const KvqPlan& p, const vxl_attn_desc* d, float sca
                 });
                 if (st != VXL_OK) return;
                 hipLaunchKernelGGL((kvq_rows_kernel<dim, bits, pooled, kRowsWaves>), grid, dim3(64 * kRowsWaves), lds, s, (const uint16_t*)Qd, view(c),
-                                   view(sp), src_idx, mix_len, part_o, part_ml, T, d->n_q_heads, d->n_kv_heads, l_cap, p.n_split, p.n_rtile,
+                                   view(sp), src_idx, mix_len, part_o, part_ml, T, d->n_q_heads, d->n_kv_heads, l_cap, p.n_split, n_rtile,
                                    scale * kLog2e, (uint16_t*)O, LSE);
             };
             if (p.blocks == 0) { if (sp) many(std::true_type{}); else many(std::false_type{}); }

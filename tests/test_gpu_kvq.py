@@ -429,6 +429,60 @@ def test_queries_that_are_not_finite():
         assert (outs[0][0][~hit].float() - outs[1][0][~hit].float()).abs().max() <= 2.0 ** -6 * outs[0][0].float().abs().max()
 
 
+@pytest.mark.parametrize("dtype,hq,hkv,t,bsz,kernel", [("bf16", 1, 1, 1, 1, 1), ("bf16", 4, 2, 30, 1, 2), ("bf16", 8, 4, 200, 32, 0),
+                                                       ("f32", 2, 2, 3, 1, 1)])
+def test_logits_below_the_smallest_number(dtype, hq, hkv, t, bsz, kernel):
+    """Products that overflow to -inf: these keys weigh nothing, also where they are all that a wave sees for a while, and
+    where the rest of an fp32 query that bf16 does not hold overflows by itself (rounded up, it would be of the other sign)."""
+    n, few, d = 700, 60, 128
+    lay = wl.layout_from_lists(n, [], [])
+    desc, gl = vxl.make_desc(hq, hkv, d, dtype), make_layout(lay)
+    assert vxl.debug_kvq_plan(desc, bsz, t, n)[0] == kernel
+    rng = np.random.default_rng(n)
+    k, v = np.zeros((hkv, n, d), np.float32), random_rows(rng, (hkv, n, d), dtype)
+    k[:, :n - few, 0] = -2.0 ** 100
+    rows, scales, _, wv = quantised(k, v, "fp8")
+    cache = device_cache(desc, "fp8", rows, scales)
+    qd = np.zeros((bsz, t, hq, d), np.float32)
+    qd[..., 0] = np.float32(2.0 ** 127 * (1 + 2.0 ** -7 - (2.0 ** -12 if dtype == "f32" else 0)))
+    qd[..., 1:] = 1
+    dq = vxl.to_device(qd, dtype)
+    out, lse = torch.zeros_like(dq), torch.zeros(dq.shape[:3], device="cuda")
+    ws = vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, bsz, t, n))
+    vxl.bilevel_decode_kvq(gl, desc, dq, cache, None, None, n, out, lse, None, ws)
+    part = wv[:, n - few:]
+    # the logits that count are 0 and their weights 1: `few` additions in fp32, a division, the result's rounding
+    want, sums = part.mean(1), np.abs(part).mean(1) * (few + 2) * 2.0 ** -24
+    bound = sums + (np.abs(want) * 1.01 * 2.0 ** -8 if dtype == "bf16" else 0)
+    got = out.double().cpu().numpy().reshape(bsz, t, hkv, hq // hkv, d)
+    assert (np.abs(got - want[:, None]) <= bound[:, None]).all()
+    assert (np.abs(lse.double().cpu().numpy() - np.log(few)) <= 2.0 ** -21 * np.log(few)).all()
+
+
+def test_the_largest_batch():
+    """65,535 queries, each as on its own with its mask; one more is refused before anything is written."""
+    rng = np.random.default_rng(17)
+    lay = wl.random_layout(rng, 3, 4, 10, 20)
+    cache, sparse, _, _ = prompt(rng, "bf16", 2, 64, "fp4", lay, True)
+    gl, desc, cap, bsz = make_layout(lay), vxl.make_desc(2, 2, 64, "bf16"), lay.n_tokens, 65535
+    masks = torch.from_numpy(some_masks(rng, 16, 4)).cuda().repeat(bsz // 16 + 1, 1).contiguous()
+    few = torch.randn(16, 1, 2, 64, device="cuda").bfloat16()
+    qd = few.repeat(bsz // 16 + 1, 1, 1, 1).contiguous()
+    out, lens = torch.full_like(qd, 9.0), torch.full((bsz + 1,), -77, dtype=torch.int32, device="cuda")
+    ws = vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, bsz + 1, 1, cap))
+    with pytest.raises(vxl.VxlError) as e:
+        vxl.bilevel_decode_kvq(gl, desc, qd, cache, sparse, masks, cap, out, None, lens, ws)
+    torch.cuda.synchronize()
+    assert e.value.status == vxl.VXL_ERR_UNSUPPORTED and (out == 9.0).all() and (lens == -77).all()
+    vxl.bilevel_decode_kvq(gl, desc, qd[:bsz], cache, sparse, masks[:bsz], cap, out[:bsz], None, lens[:bsz], ws)
+    want, n = torch.zeros_like(few), torch.zeros(16, dtype=torch.int32, device="cuda")
+    small = vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, 16, 1, cap))
+    vxl.bilevel_decode_kvq(gl, desc, few, cache, sparse, masks[:16], cap, want, None, n, small)
+    assert vxl.debug_kvq_plan(desc, 16, 1, cap) == vxl.debug_kvq_plan(desc, bsz, 1, cap) == (1, 1)
+    assert same_bits(out[:bsz], want.repeat(bsz // 16 + 1, 1, 1, 1)[:bsz]) and torch.equal(lens[:bsz], n.repeat(bsz // 16 + 1)[:bsz])
+    assert (out[bsz:] == 9.0).all() and lens[bsz] == -77
+
+
 # ---- together, as they are used ------------------------------------------------------------------
 def test_a_prompt_in_a_quantised_cache():
     """Chunk by chunk into the cache as the pre-filling ends them, pooled rows quantised beside; selection by the mean keys
