@@ -93,8 +93,10 @@ struct KvqLoad {
     static __device__ __forceinline__ int key_off(int r, int c) { return r * (16 * LANES) + ((c ^ ((r / (16 / LANES)) & (LANES - 1))) << 4); }
 };
 
+// (Two workgroups on a compute unit where a third's registers would not do: fp32 with three, 168 registers a lane and up to
+// 352 bytes of them in memory, 256 rows of 8 bits at 24k keys of pooled sets 195 us, with two 58.)
 template <int D, int BITS, bool F32, bool POOLED, int NB>
-__global__ __launch_bounds__(64 * kKvqWaves, NB == 1 ? 3 : 2) void kvq_decode_kernel(
+__global__ __launch_bounds__(64 * kKvqWaves, NB == 1 && !F32 ? 3 : 2) void kvq_decode_kernel(
     const typename Elem<F32>::T* __restrict__ Qd, KvqView dense, KvqView sparse, const int32_t* __restrict__ src_idx,
     const int32_t* __restrict__ mix_len, float* __restrict__ part_o, float2* __restrict__ part_ml, int T_q, int n_q_heads,
     int n_kv_heads, int l_cap, int n_split, int share, int more, int n_rtile, float c2,
@@ -655,12 +657,12 @@ __global__ __launch_bounds__(THREADS) void kvq_merge_kernel(const float* __restr
     __syncthreads();
     if (threadIdx.x >= D) return;                             // a column each
     M = stat[0].x;
-#pragma unroll
+#pragma unroll 8
     for (int i = 1; i < SG; ++i) M = fmaxf(M, stat[i].x);
     const float ref = M == -INFINITY ? 0.f : M;
     float sum = 0.f;
     L = 0.f;
-#pragma unroll
+#pragma unroll 8
     for (int i = 0; i < SG; ++i) {
         const float f = __builtin_amdgcn_exp2f(stat[i].x - ref);
         L = fmaf(f, stat[i].y, L);
