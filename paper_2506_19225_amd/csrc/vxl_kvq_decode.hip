@@ -136,16 +136,23 @@ __global__ __launch_bounds__(64 * kKvqWaves, NB == 1 && !F32 ? 3 : 2) void kvq_d
     struct Tile {
         uint32_t k[G::LOADS][4], v[8][VW], s;
     };
-    // The workgroup's tiles are its even share of the capacity's; of a wave: tile0, tile0 + kKvqWaves, ...
-    const int tile0 = split * share + min(split, more) + wave;
+    // The workgroup's tiles are its even share of the set's; of a wave: tile0, tile0 + kKvqWaves, ...
+    int tile0 = split * share + min(split, more) + wave;
     // (entries up to the capacity, so that the first ones do not wait for the length; behind the length they may be
     // anything, and row 0 is read there instead, whose values do not count)
     auto entry = [&](int tile) __attribute__((always_inline)) {      // (32-bit byte offsets: a map has fewer than 2^30 entries)
         return *(const int32_t*)((const char*)map + 4u * (uint32_t)min(tile * kKvqTile + own, l_cap - 1));
     };
     int e0 = entry(tile0), e1 = entry(tile0 + kKvqWaves);
-    const int len = min(max(mix_len[b], 0), l_cap);
-    const int end = min((len + kKvqTile - 1) / kKvqTile, tile0 - wave + share + (split < more ? 1 : 0));
+    const int len = min(max(mix_len[b], 0), l_cap), tiles = (len + kKvqTile - 1) / kKvqTile;
+    if (tiles != n_split * share + more) {                    // (shares of the capacity were a guess: chunks differ in length)
+        share = tiles / n_split;
+        more = tiles % n_split;
+        tile0 = split * share + min(split, more) + wave;
+        e0 = entry(tile0);
+        e1 = entry(tile0 + kKvqWaves);
+    }
+    const int end = min(tiles, tile0 - wave + share + (split < more ? 1 : 0));
     const int n = (max(end - tile0, 0) + kKvqWaves - 1) / kKvqWaves;
 
     auto request = [&](int tile, int e, Tile& t) __attribute__((always_inline)) {
@@ -675,12 +682,11 @@ __global__ __launch_bounds__(THREADS) void kvq_merge_kernel(const float* __restr
 
 }  // namespace
 
-// How many splits, and for many rows which kernel, by estimates in us, least squares over random calls (and the times that
-// they leave unexplained: 6 to 10 % rms): a start, the tiles that a wave or workgroup walks, the partial rows, the merge.  More
-// than one workgroup on a compute unit shares its vector and matrix units, so that a tile takes as much longer, but for a few
-// rows, which leave them some time.  (us by workgroups in all, replayed: 7 rows of D = 128, 8,112 keys in 8 bits, two queries
-// 64: 9.3, 128: 8.3, 256: 8.7; 52,992 keys, 16 units 64: 77.9, 256: 32.7, 512: 31.1, 768: 33.0; 16 rows, 16,576 keys, 8 units
-// 128: 12.9, 256: 11.3, 512: 13.2.)
+// How many splits, and for many rows which kernel, by estimates in us, least squares over 3,800 timed calls of 1,376 to 98,176
+// keys (4 to 8 % rms; the splits that they choose cost 0.4 % (more than 16 rows) and 0.8 % more than the best of each call's): a
+// start, the tiles that a wave or workgroup walks, the partial rows, the merge.  More than one workgroup on a compute unit
+// shares its vector and matrix units, so that a tile takes longer, but not as much as there are workgroups; the third one pays
+// for a few rows only (one row of seven heads, D = 64, 98k keys x 8 queries: one 50.8, two and a bit 44.1, three 34.8).
 static KvqPlan kvq_splits(const vxl_attn_desc* d, int batch, long long rows, int l_cap, int blocks, int waves, float* us) {
     KvqPlan p{};
     p.blocks = blocks;
@@ -690,16 +696,17 @@ static KvqPlan kvq_splits(const vxl_attn_desc* d, int batch, long long rows, int
     const long long units = (long long)batch * d->n_kv_heads, per = units * p.n_rtile;
     const long long steps = ((long long)l_cap + wg_keys - 1) / wg_keys;           // of a workgroup that has all keys
     const bool d64 = d->head_dim == 64;
-    const float tile = blocks == 0 ? (d64 ? 1.4f : 2.1f) : blocks == 2 ? (d64 ? 0.45f : 0.72f) : d->dtype == VXL_F32 ? 1.0f : 0.62f;
-    const float start = blocks ? 6.f : 7.f, per_mb = blocks ? 0.8f : 0.45f;
+    const float tile = blocks == 0 ? (d64 ? 1.27f : 1.76f) : blocks == 2 ? (d64 ? 0.57f : 0.76f)
+                       : d->dtype == VXL_F32 ? (d64 ? 0.6f : 0.88f) : d64 ? 0.44f : 0.64f;
+    const float start = blocks == 0 ? 8.f : blocks == 2 ? 5.5f : 4.2f, per_mb = blocks ? 0.9f : 0.5f, merged = blocks == 1 ? 2.8f : 2.5f;
     const int round = kXcds / std::gcd(kXcds, d->n_kv_heads);                     // pairs (KV head, split) go to the XCDs in turn
-    const long long most = std::min<long long>(steps, std::max<long long>(1, (blocks ? 512 : 256) / per));
+    const long long most = std::min<long long>(steps, std::max<long long>(1, 256 * (blocks == 1 ? 3 : blocks == 2 ? 2 : 1) / per));
     *us = INFINITY;
     for (long long n = 1; n <= most; n = n < round ? n + 1 : n + round - n % round) {
         const long long on_unit = (per * n + 255) / 256;
-        const float load = blocks == 1 ? 0.3f + 0.7f * on_unit : blocks == 2 && on_unit > 1 ? 0.8f * on_unit : (float)on_unit;
+        const float load = blocks == 1 ? 0.36f + 0.64f * on_unit : blocks == 2 && on_unit > 1 ? 0.78f * on_unit : (float)on_unit;
         const float mb = 4e-6f * units * n * rows * d->head_dim;
-        const float merge = n == 1 ? 0.f : 2.5f + per_mb * mb + (n > 32 ? 0.5f : 0.f) + (n > 64 ? 0.4f : 0.f);
+        const float merge = n == 1 ? 0.f : merged + per_mb * mb + (n > 32 ? 0.9f : 0.f) + (n > 64 ? 0.4f : 0.f);
         const float t = start + tile * load * ((steps + n - 1) / n) + merge;
         if (t < *us) {
             *us = t;
@@ -720,8 +727,8 @@ KvqPlan kvq_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     if (d->dtype != VXL_BF16 || rows <= 16) return kvq_splits(d, batch, rows, l_cap, 1, 0, &us);
     const KvqPlan p = kvq_splits(d, batch, rows, l_cap, 2, 0, &us);
     if (rows <= 128) return p;
-    // (448 rows x 8 queries, 45,312 keys 413 -> 358 us, 392 rows x 3, 111,488 keys 505 -> 343; but 686 rows x 8, 11,008 keys
-    // 185 against 201)
+    // (us, blocks of 32 rows and all rows: 448 rows, 98,176 keys of D = 64 in 4 queries 172 and 137; 1,792 rows, 4,736 keys, 4
+    // queries 79 and 97, D = 128 116 and 123)
     const KvqPlan many = kvq_splits(d, batch, rows, l_cap, 0, kRowsWaves, &us_many);
     return us_many < us ? many : p;
 }
