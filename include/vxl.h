@@ -8,6 +8,7 @@
  *   vxl_chunk_score_topk   "Bi-level KVs Decoding": relevance score per chunk, selection
  *   vxl_gather_bilevel_kv  "Bi-level KVs Decoding": selective reload + concatenation
  *   vxl_bilevel_decode     "Bi-level KVs Decoding": generation over the mixed KV set
+ *   vxl_kvq_* and *_kvq    the same cache in 8 or 4 bits: written, read back, gathered from, attended to in place
  *
  * Conventions
  *   - Every tensor pointer is a DEVICE pointer owned by the caller; the layout arrays given to
@@ -128,7 +129,7 @@ vxl_status vxl_layout_destroy(vxl_layout* layout);
 
 /* Bytes of workspace the given hot call needs (0 on invalid arguments, and for VXL_OP_GATHER,
  * which needs none).  batch, n_q_tokens and l_cap are read by the ops that take them (SCORE_TOPK:
- * batch; SCORE_MASS: batch, n_q_tokens; DECODE: batch, n_q_tokens, l_cap).  The decode call is
+ * batch; SCORE_MASS: batch, n_q_tokens; the DECODEs: batch, n_q_tokens, l_cap).  The decode call is
  * sized by the capacity of the mixed buffers it will be given, l_cap, and not by the number k of
  * dense chunks, because it takes no layout: l_cap = vxl_mixed_kv_capacity(layout, k) for the
  * caller's k, or anything larger.  layout may be NULL for VXL_OP_DECODE. */

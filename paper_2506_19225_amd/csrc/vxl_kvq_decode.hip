@@ -30,6 +30,12 @@ namespace {
 // Quantised values are bf16 numbers.  bf16 queries are the operand as they are; fp32 queries, and probabilities of an fp32
 // call, go in as three bf16 parts that add up to all 24 bits (three matrix instructions instead of one).  Probabilities of a
 // bf16 call are rounded to bf16 (2^-8 relative at most, of each weight), their sum is taken before that, in fp32.
+//
+// Measured (us, launches with their merge; D = 128, 28 heads on 4): one token, 4,096 keys in 4 bits 7.4 and 18,176 keys in 8
+// bits 10.9 (the floor of two dependent launches; a plain decode in place 8.9 and 12.7), eight queries' tokens, 64.5k keys each
+// in 4 bits 33.6 (plain 83.9): vector instructions 73 % and matrix instructions 23 % of the cycles, which do not overlap more;
+// 64 of the 174 vector instructions of a tile are conversions, 32 byte permutations, 8 exponentials.  A question of 64 tokens,
+// 448 rows by 32 (NB = 2) over 23,800 keys in 4 bits 45.5, 60 % and 27 %, 520 TFLOP/s.
 // ------------------------------------------------------------------------------------------
 // The workgroup's KV head, split, query and first row.  Workgroups that read the same keys (row tiles, and queries, whose sets
 // overlap) are members of a pair (KV head, split) and neighbours on one XCD, whose L2 serves all but the first: workgroups go to
@@ -94,7 +100,7 @@ struct KvqLoad {
 };
 
 // (Two workgroups on a compute unit where a third's registers would not do: fp32 with three, 168 registers a lane and up to
-// 352 bytes of them in memory, 256 rows of 8 bits at 24k keys of pooled sets 195 us, with two 58.)
+// 352 bytes of them in memory: 224 rows over 21.7k keys in 8 bits, pooled, 195 us, with two 58.)
 template <int D, int BITS, bool F32, bool POOLED, int NB>
 __global__ __launch_bounds__(64 * kKvqWaves, NB == 1 && !F32 ? 3 : 2) void kvq_decode_kernel(
     const typename Elem<F32>::T* __restrict__ Qd, KvqView dense, KvqView sparse, const int32_t* __restrict__ src_idx,
@@ -413,6 +419,9 @@ __global__ __launch_bounds__(64 * kKvqWaves, NB == 1 && !F32 ? 3 : 2) void kvq_d
 // call, so each 64-key tile is converted once for all rows of the workgroup: NW threads load the codes of a row between them,
 // a tile ahead, and write the bf16 rows to one of two LDS stages while the other is worked on, by the products and layouts of
 // the plain decode's ring.  One barrier per tile.
+// 896 rows on four heads, 18,176 keys in 4 bits: 50.4 us and the merge, 660 TFLOP/s (plain decode in place 52.7 in all); 47 % of
+// the cycles in vector, 39 % in matrix instructions, 30 % of the LDS's in reads of K and V rows by every wave.  64 rows per
+// wave would halve those, but spill; four waves per workgroup and converting in turns were no faster.
 // ------------------------------------------------------------------------------------------
 // Element offset of 16-byte piece `piece` of row `row` of a V tile: its 64-byte parts turned as in the plain tile, for the
 // transposing reads, and the pieces of a part by the next bits of the row, for writes of one piece of each part by eight rows.
@@ -614,7 +623,9 @@ __global__ __launch_bounds__(64 * NW, 2) void kvq_rows_kernel(
 }
 
 // The merge of the splits, one workgroup per query row: SG groups of D / 4 lanes take every SG-th split, U of them requested
-// together, and are folded through LDS; the order depends on the split index alone.
+// together, and are folded through LDS; the order depends on the split index alone.  Bound by the launch and two dependent trips
+// to memory: 28 rows of 32 splits 3.3 us, 3,584 rows of 16 splits (29 MB) 7.7.  As the last workgroup's work in the kernels above,
+// behind device-wide fences, each of which writes an XCD's L2 back, 7.9 us of a token became 19.
 template <int D, bool F32, int THREADS>
 __global__ __launch_bounds__(THREADS) void kvq_merge_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml,
                                                             typename Elem<F32>::T* __restrict__ O, float* __restrict__ LSE,
@@ -727,8 +738,7 @@ KvqPlan kvq_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     if (d->dtype != VXL_BF16 || rows <= 16) return kvq_splits(d, batch, rows, l_cap, 1, 0, &us);
     const KvqPlan p = kvq_splits(d, batch, rows, l_cap, 2, 0, &us);
     if (rows <= 128) return p;
-    // (us, blocks of 32 rows and all rows: 448 rows, 98,176 keys of D = 64 in 4 queries 172 and 137; 1,792 rows, 4,736 keys, 4
-    // queries 79 and 97, D = 128 116 and 123)
+    // (us, blocks of 32 rows and of 256, 21.7k keys: 224 rows 24.3 and 30.4, 448 rows of 4 queries 118 and 104)
     const KvqPlan many = kvq_splits(d, batch, rows, l_cap, 0, kRowsWaves, &us_many);
     return us_many < us ? many : p;
 }
