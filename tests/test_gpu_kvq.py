@@ -483,6 +483,53 @@ def test_the_largest_batch():
     assert (out[bsz:] == 9.0).all() and lens[bsz] == -77
 
 
+def test_the_longest_cache():
+    """Rows at the end of a cache of the largest capacity, whose offsets pass 32 bits, as from one that holds them alone."""
+    cap, hkv, d, p, last, fmt = 1 << 24, 2, 128, 64, 500, "fp8"
+    desc = vxl.make_desc(4, hkv, d, "bf16")
+    lens = [(cap - p - last) // 40] * 39
+    lens += [cap - p - last - sum(lens), last]
+    tail = cap - last
+    long = wl.layout_from_lists(p, lens, [[]] * 40 + [np.arange(tail + 3, cap, 7)])
+    short = wl.layout_from_lists(p, [last], [np.arange(p + 3, p + last, 7)])
+    whole, part = vxl.KvqCache(desc, fmt, cap), vxl.KvqCache(desc, fmt, p + last)
+    k, v = (torch.randn(hkv, p + last, d, device="cuda").bfloat16() for _ in range(2))
+    vxl.kvq_write(desc, k, v, part)
+    cut = lambda x, a, b: x[:, a:b].contiguous()  # noqa: E731
+    vxl.kvq_write(desc, cut(k, 0, p), cut(v, 0, p), whole)
+    vxl.kvq_write(desc, cut(k, p, p + last), cut(v, p, p + last), whole, tail)
+    with pytest.raises(vxl.VxlError):
+        vxl.kvq_write(desc, cut(k, 0, 1), cut(v, 0, 1), whole, cap)
+    back = [torch.zeros(hkv, last, d, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    vxl.kvq_read(desc, whole, *back[:2], tail)
+    vxl.kvq_read(desc, part, *back[2:], p)
+    assert same_bits(back[0], back[2]) and same_bits(back[1], back[3])
+    sparse = vxl.KvqCache(desc, fmt, len(short.sparse_idx))
+    vxl.kvq_write(desc, *(x[:, short.sparse_idx].contiguous() for x in (v, k)), sparse)
+    l_cap = p + last
+    for kept in (None, sparse):
+        for bsz, t in ((2, 1), (2, 40), (64, 200)):
+            results = []
+            for lay, cache in ((long, whole), (short, part)):
+                gl = make_layout(lay)
+                mask = torch.zeros(bsz, gl.n_chunks, dtype=torch.uint8, device="cuda")
+                mask[::2, -1] = 1
+                kmix = torch.zeros(bsz, hkv, l_cap, d, dtype=torch.bfloat16, device="cuda")
+                vmix, n = torch.zeros_like(kmix), torch.zeros(bsz, dtype=torch.int32, device="cuda")
+                vxl.gather_bilevel_kvq(gl, desc, cache, kept, mask, kmix, vmix, n)
+                q = torch.randn(bsz, t, 4, d, generator=torch.Generator("cuda").manual_seed(t), device="cuda").bfloat16()
+                ws = vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, bsz, t, l_cap))
+                out, lse = torch.zeros_like(q), torch.zeros(q.shape[:3], device="cuda")
+                vxl.bilevel_decode_kvq(gl, desc, q, cache, kept, mask, l_cap, out, lse, None, ws)
+                results.append((kmix, vmix, n, out, lse))
+            assert all(same_bits(a, b) for a, b in zip(*results)) and results[0][2][0] == l_cap
+            assert results[0][3].isfinite().all() and results[0][3].any()
+    assert [vxl.debug_kvq_plan(desc, b, t, l_cap)[0] for b, t in ((2, 1), (2, 40), (64, 200))] == [1, 2, 0]
+    with pytest.raises(vxl.VxlError) as e:
+        vxl.kvq_write(desc, cut(k, 0, 1), cut(v, 0, 1), vxl.KvqCache(desc, "fp4", cap + 1))
+    assert e.value.status == vxl.VXL_ERR_UNSUPPORTED
+
+
 # ---- together, as they are used ------------------------------------------------------------------
 def test_a_prompt_in_a_quantised_cache():
     """Chunk by chunk into the cache as the pre-filling ends them, pooled rows quantised beside; selection by the mean keys
