@@ -193,8 +193,8 @@ const vxl_kvq_cache* cache(long long a) { return (const vxl_kvq_cache*)a; }
 // Whether a tensor of so many elements holds the rows that a call takes off it, by the descriptor's layout.
 bool holds(const vxl_attn_desc* d, long long n_rows, long long numel) {
     if (n_rows <= 0) return true;                             // (for the library to refuse, or nothing to do)
-    const long long head = d->kv_stride_head ? d->kv_stride_head : n_rows * d->head_dim, tok = d->kv_stride_tok ? d->kv_stride_tok : d->head_dim;
-    return (d->n_kv_heads - 1) * head + (n_rows - 1) * tok + d->head_dim <= numel;
+    const __int128 rows = n_rows, head = d->kv_stride_head ? d->kv_stride_head : rows * d->head_dim, tok = d->kv_stride_tok ? d->kv_stride_tok : d->head_dim;
+    return (d->n_kv_heads - 1) * head + (rows - 1) * tok + d->head_dim <= numel;
 }
 
 PyObject* chunk_prefill(PyObject* self, PyObject* const* args, Py_ssize_t n) {
@@ -264,13 +264,13 @@ PyObject* bilevel_decode_inplace(PyObject* self, PyObject* const* args, Py_ssize
 }
 PyObject* kvq_write(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     return call<kDesc, kTensor, kNumel, kTensor, kNumel, kInt, kCache, kInt>(self, args, n, [](const State& lib, const long long* a) {
-        if (!holds(desc(a[0]), a[5], a[2]) || !holds(desc(a[0]), a[5], a[4])) return VXL_ERR_INVALID_ARG;
+        if (!holds(desc(a[0]), a[5], a[2]) || !holds(desc(a[0]), a[5], a[4]) || a[7] != (int32_t)a[7]) return VXL_ERR_INVALID_ARG;
         return lib.kvq_write(desc(a[0]), ptr<void>(a[1]), ptr<void>(a[3]), (int32_t)a[5], cache(a[6]), (int32_t)a[7], (vxl_stream)a[8]);
     });
 }
 PyObject* kvq_read(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     return call<kDesc, kCache, kInt, kInt, kTensor, kNumel, kTensor, kNumel>(self, args, n, [](const State& lib, const long long* a) {
-        if (!holds(desc(a[0]), a[3], a[5]) || !holds(desc(a[0]), a[3], a[7])) return VXL_ERR_INVALID_ARG;
+        if (!holds(desc(a[0]), a[3], a[5]) || !holds(desc(a[0]), a[3], a[7]) || a[2] != (int32_t)a[2]) return VXL_ERR_INVALID_ARG;
         return lib.kvq_read(desc(a[0]), cache(a[1]), (int32_t)a[2], (int32_t)a[3], ptr<void>(a[4]), ptr<void>(a[6]), (vxl_stream)a[8]);
     });
 }

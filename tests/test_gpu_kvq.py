@@ -648,6 +648,25 @@ def test_on_streams_of_their_own():
         assert all(same_bits(a, b) for a, b in zip(want, got))
 
 
+def test_rows_that_a_tensor_or_a_cache_does_not_hold():
+    """Numbers of rows and strides past the tensor, first rows past 32 bits, no rows at all."""
+    desc = vxl.make_desc(4, 2, 64, "bf16")
+    k = torch.ones(2, 10, 64, dtype=torch.bfloat16, device="cuda")
+    cache = vxl.KvqCache(desc, "fp4", 20)
+    cache.rows.fill_(3), cache.scales.fill_(4)
+    wide = vxl.make_desc(4, 2, 64, "bf16")
+    wide.q_stride_head, wide.q_stride_tok, wide.kv_stride_head, wide.kv_stride_tok = 640, 64, 1 << 62, 1 << 62
+    for d, n, first in ((desc, 11, 0), (desc, 10, 11), (desc, 10, 1 << 32), (desc, 10, -(1 << 32)), (desc, (1 << 32) + 10, 0), (desc, -1, 0),
+                        (wide, 10, 0), (wide, 5, 0)):
+        for call in (lambda: vxl.kvq_write(d, k, k, cache, first, n), lambda: vxl.kvq_read(d, cache, k, torch.ones_like(k), first, n)):
+            with pytest.raises(vxl.VxlError) as e:
+                call()
+            assert e.value.status == vxl.VXL_ERR_INVALID_ARG, (n, first)
+    vxl.kvq_write(desc, k, k, cache, 20, 0), vxl.kvq_read(desc, cache, k, k, 0, 0)
+    torch.cuda.synchronize()
+    assert (cache.rows == 3).all() and (cache.scales == 4).all() and (k == 1).all()
+
+
 def test_refusals_with_a_layout():
     rng = np.random.default_rng(16)
     lay = wl.random_layout(rng, 10, 4, 20, 40)
