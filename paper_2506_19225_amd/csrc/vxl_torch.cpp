@@ -188,7 +188,18 @@ PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n, F f) {
 template <typename T> T* ptr(long long a) { return (T*)a; }
 const vxl_layout* lay(long long a) { return (const vxl_layout*)a; }
 const vxl_attn_desc* desc(long long a) { return (const vxl_attn_desc*)a; }
-const vxl_kvq_cache* cache(long long a) { return (const vxl_kvq_cache*)a; }
+// vxl.KvqCacheArg: the library's struct, and what the tensors behind it were made for (0: not told).
+struct CacheArg {
+    vxl_kvq_cache c;
+    int32_t n_kv_heads, head_dim;
+};
+const vxl_kvq_cache* cache(long long a) { return a ? &((const CacheArg*)a)->c : nullptr; }
+
+// Whether a cache (null: there is none) has the descriptor's heads.
+bool of_heads(const vxl_attn_desc* d, long long a) {
+    const CacheArg* c = (const CacheArg*)a;
+    return !c || !c->n_kv_heads || (c->n_kv_heads == d->n_kv_heads && c->head_dim == d->head_dim);
+}
 
 // Whether a tensor of so many elements holds the rows that a call takes off it, by the descriptor's layout.
 bool holds(const vxl_attn_desc* d, long long n_rows, long long numel) {
@@ -264,19 +275,20 @@ PyObject* bilevel_decode_inplace(PyObject* self, PyObject* const* args, Py_ssize
 }
 PyObject* kvq_write(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     return call<kDesc, kTensor, kNumel, kTensor, kNumel, kInt, kCache, kInt>(self, args, n, [](const State& lib, const long long* a) {
-        if (!holds(desc(a[0]), a[5], a[2]) || !holds(desc(a[0]), a[5], a[4]) || a[7] != (int32_t)a[7]) return VXL_ERR_INVALID_ARG;
+        if (!holds(desc(a[0]), a[5], a[2]) || !holds(desc(a[0]), a[5], a[4]) || a[7] != (int32_t)a[7] || !of_heads(desc(a[0]), a[6])) return VXL_ERR_INVALID_ARG;
         return lib.kvq_write(desc(a[0]), ptr<void>(a[1]), ptr<void>(a[3]), (int32_t)a[5], cache(a[6]), (int32_t)a[7], (vxl_stream)a[8]);
     });
 }
 PyObject* kvq_read(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     return call<kDesc, kCache, kInt, kInt, kTensor, kNumel, kTensor, kNumel>(self, args, n, [](const State& lib, const long long* a) {
-        if (!holds(desc(a[0]), a[3], a[5]) || !holds(desc(a[0]), a[3], a[7]) || a[2] != (int32_t)a[2]) return VXL_ERR_INVALID_ARG;
+        if (!holds(desc(a[0]), a[3], a[5]) || !holds(desc(a[0]), a[3], a[7]) || a[2] != (int32_t)a[2] || !of_heads(desc(a[0]), a[1])) return VXL_ERR_INVALID_ARG;
         return lib.kvq_read(desc(a[0]), cache(a[1]), (int32_t)a[2], (int32_t)a[3], ptr<void>(a[4]), ptr<void>(a[6]), (vxl_stream)a[8]);
     });
 }
 PyObject* gather_bilevel_kvq(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     return call<kLayout, kDesc, kCache, kCache, kTensor, size(5, 0), kTensor, kTensor, size(5, 2), kTensor, kTensor>(
         self, args, n, [](const State& lib, const long long* a) {
+        if (!of_heads(desc(a[1]), a[2]) || !of_heads(desc(a[1]), a[3])) return VXL_ERR_INVALID_ARG;
         return lib.gather_bilevel_kvq(lay(a[0]), desc(a[1]), cache(a[2]), cache(a[3]), ptr<uint8_t>(a[4]), (int32_t)a[5], ptr<void>(a[6]),
                                       ptr<void>(a[7]), (int32_t)a[8], ptr<int32_t>(a[9]), ptr<int32_t>(a[10]), (vxl_stream)a[11]);
     });
@@ -285,6 +297,7 @@ PyObject* bilevel_decode_kvq(PyObject* self, PyObject* const* args, Py_ssize_t n
     return call<kLayout, kDesc, kTensor, size(2, 0), size(2, 1), kCache, kCache, kTensor, kInt, kInt, kTensor, kTensor, kTensor,
                 kTensor, kNumel>(
         self, args, n, [](const State& lib, const long long* a) {
+        if (!of_heads(desc(a[1]), a[5]) || !of_heads(desc(a[1]), a[6])) return VXL_ERR_INVALID_ARG;
         return lib.bilevel_decode_kvq(lay(a[0]), desc(a[1]), ptr<void>(a[2]), (int32_t)a[3], (int32_t)a[4], cache(a[5]), cache(a[6]),
                                       ptr<uint8_t>(a[7]), (int32_t)a[8], (int32_t)a[9], ptr<void>(a[10]), ptr<float>(a[11]),
                                       ptr<int32_t>(a[12]), ptr<void>(a[13]), (size_t)a[14], (vxl_stream)a[15]);

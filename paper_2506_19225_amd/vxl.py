@@ -32,8 +32,9 @@ class AttnDesc(C.Structure):
 
 
 class KvqCacheArg(C.Structure):
-    """vxl_kvq_cache"""
-    _fields_ = [("rows", C.c_void_p), ("scales", C.c_void_p), ("format", C.c_int32), ("capacity", C.c_int32)]
+    """vxl_kvq_cache, and the heads and their dimension that it was made for (0: not told), which the binding compares"""
+    _fields_ = [("rows", C.c_void_p), ("scales", C.c_void_p), ("format", C.c_int32), ("capacity", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
 
 
 class VxlError(RuntimeError):
@@ -348,7 +349,7 @@ class KvqCache:
                 raise ValueError(f"a uint8 tensor of shape {(desc.n_kv_heads, rows.shape[1], 2, last)} expected, "
                                  f"not {t.dtype} of {tuple(t.shape)}")
         self.rows, self.scales, self.format, self.capacity = rows, scales, code, int(rows.shape[1])
-        self.arg = KvqCacheArg(_ptr(rows), _ptr(scales), code, self.capacity)
+        self.arg = KvqCacheArg(_ptr(rows), _ptr(scales), code, self.capacity, desc.n_kv_heads, desc.head_dim)
 
 
 def kvq_write(desc: AttnDesc, k, v, cache: KvqCache, first_row: int = 0, n_rows: Optional[int] = None, stream=None):

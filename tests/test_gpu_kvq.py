@@ -667,6 +667,27 @@ def test_rows_that_a_tensor_or_a_cache_does_not_hold():
     assert (cache.rows == 3).all() and (cache.scales == 4).all() and (k == 1).all()
 
 
+def test_caches_of_other_heads_are_refused():
+    rng = np.random.default_rng(18)
+    lay = wl.random_layout(rng, 10, 4, 20, 40)
+    gl, n, desc = make_layout(lay), lay.n_tokens, vxl.make_desc(4, 2, 64, "bf16")
+    cache = vxl.KvqCache(desc, "fp4", n)
+    for hkv, d in ((1, 64), (4, 64), (2, 128)):
+        other = vxl.KvqCache(vxl.make_desc(4, hkv, d, "f32"), "fp4", n)
+        k = torch.zeros(2, n, 64, dtype=torch.bfloat16, device="cuda")
+        mask, lens = torch.zeros(1, 4, dtype=torch.uint8, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        q, mix = torch.zeros(1, 1, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 1, 2, n, 64, dtype=torch.bfloat16, device="cuda")
+        ws = vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, 1, 1, n))
+        for call in (lambda: vxl.kvq_write(desc, k, k, other), lambda: vxl.kvq_read(desc, other, k, torch.zeros_like(k)),
+                     lambda: vxl.gather_bilevel_kvq(gl, desc, other, None, mask, mix[0], mix[1], lens),
+                     lambda: vxl.gather_bilevel_kvq(gl, desc, cache, other, mask, mix[0], mix[1], lens),
+                     lambda: vxl.bilevel_decode_kvq(gl, desc, q, other, None, mask, n, torch.zeros_like(q), workspace=ws),
+                     lambda: vxl.bilevel_decode_kvq(gl, desc, q, cache, other, mask, n, torch.zeros_like(q), workspace=ws)):
+            with pytest.raises(vxl.VxlError) as e:
+                call()
+            assert e.value.status == vxl.VXL_ERR_INVALID_ARG
+
+
 def test_refusals_with_a_layout():
     rng = np.random.default_rng(16)
     lay = wl.random_layout(rng, 10, 4, 20, 40)
