@@ -9,7 +9,7 @@
 #include <new>
 #include <numeric>
 
-#include "vxl_internal.h"
+#include "vxl_kvq.h"
 
 namespace vxl {
 
@@ -206,6 +206,10 @@ InplaceWorkspace inplace_workspace(int batch, int l_cap, size_t partials) {
     off += align_up(std::max<size_t>(256, partials), 256);
     w.total = off;
     return w;
+}
+
+InplaceWorkspace inplace_workspace(const vxl_attn_desc* d, int batch, int T, int l_cap) {
+    return inplace_workspace(batch, l_cap, decode_plan(d, batch, T, l_cap, false).total);
 }
 
 }  // namespace vxl
@@ -457,7 +461,7 @@ size_t vxl_workspace_bytes(vxl_op op, const vxl_layout* L, const vxl_attn_desc* 
             return std::max<size_t>(256, mass_plan(L, d, batch, n_q_tokens).total);
         case VXL_OP_DECODE_INPLACE:
             if (batch <= 0 || n_q_tokens <= 0 || l_cap <= 0) return 0;
-            return inplace_workspace(batch, l_cap, decode_plan(d, batch, n_q_tokens, l_cap, false).total).total;
+            return inplace_workspace(d, batch, n_q_tokens, l_cap).total;
         case VXL_OP_DECODE_KVQ:
             if (batch <= 0 || n_q_tokens <= 0 || l_cap <= 0) return 0;
             return inplace_workspace(batch, l_cap, kvq_plan(d, batch, n_q_tokens, l_cap).total).total;
@@ -620,7 +624,7 @@ vxl_status vxl_bilevel_decode_inplace(const vxl_layout* L, const vxl_attn_desc* 
     if (!aligned16(Qd) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(Ksp) || !aligned16(Vsp))
         return VXL_ERR_INVALID_ARG;
     if (l_cap < vxl_mixed_kv_capacity(L, 0)) return VXL_ERR_INVALID_ARG;
-    const InplaceWorkspace w = inplace_workspace(batch, l_cap, decode_plan(d, batch, n_q_tokens, l_cap, false).total);
+    const InplaceWorkspace w = inplace_workspace(d, batch, n_q_tokens, l_cap);
     // (fp32: the row map is needed, room for partial results is not)
     const DecodePlan p = decode_plan(d, batch, n_q_tokens, l_cap, false, workspace_bytes > w.partials ? workspace_bytes - w.partials : 0);
     const size_t need = w.partials + (d->dtype == VXL_F32 ? 256 : align_up(std::max<size_t>(256, p.total), 256));

@@ -198,13 +198,13 @@ DecodePlan decode_plan(const vxl_attn_desc* d, int batch, int T, int l_cap, bool
 // fp32, either form: total == 0 with one split; a call without this much scratch memory takes one split
 DecodePlan decode_f32_plan(const vxl_attn_desc* d, int batch, int T, int l_cap);
 
-struct InplaceWorkspace {      // byte offsets into the caller's workspace (vxl_bilevel_decode_inplace, vxl_bilevel_decode_kvq)
-    size_t partials;           // the plan's partial results
+struct InplaceWorkspace {      // byte offsets into the caller's workspace (vxl_bilevel_decode_inplace)
+    size_t partials;           // the decode plan's partial results
     size_t src_idx;            // [B][l_cap] int32 row map
     size_t mix_len;            // [B] int32 (used when the caller does not ask for the lengths)
     size_t total;
 };
-InplaceWorkspace inplace_workspace(int batch, int l_cap, size_t partials);
+InplaceWorkspace inplace_workspace(const vxl_attn_desc* d, int batch, int T, int l_cap);
 
 vxl_status launch_decode_bf16(const DecodePlan& p, const vxl_attn_desc* d, float scale, const void* Qd, int batch, int T,
                               const void* Kmix, const void* Vmix, int l_cap, const int32_t* mix_len,
@@ -229,26 +229,5 @@ vxl_status decode_static_scratch(void** ptr);
 vxl_status launch_decode_simple(const vxl_attn_desc* d, float scale, const void* Qd, int batch, int T,
                                 const void* Kmix, const void* Vmix, int l_cap, const int32_t* mix_len,
                                 void* O, float* LSE, hipStream_t s);
-
-// ---- quantised cache ----
-vxl_status launch_kvq_write(const vxl_attn_desc* d, const void* K, const void* V, int n_rows, const vxl_kvq_cache* c, int first,
-                            hipStream_t s);
-vxl_status launch_kvq_read(const vxl_attn_desc* d, const vxl_kvq_cache* c, int first, int n_rows, void* K, void* V, hipStream_t s);
-// sp: quantised sparse rows read instead of the kept rows of c, or null (here and below)
-vxl_status launch_kvq_gather(const vxl_layout* L, const vxl_attn_desc* d, const vxl_kvq_cache* c, const vxl_kvq_cache* sp,
-                             const uint8_t* dense_mask, int batch, void* Kmix, void* Vmix, int l_cap, int32_t* mix_len,
-                             int32_t* src_idx, hipStream_t s);
-struct KvqPlan {
-    int blocks;                                // 16-row blocks of a workgroup; 0: the kernel of many rows
-    int waves;                                 // of that one, per workgroup
-    long long n_rtile;                         // workgroups for the rows
-    int n_split;                               // key splits per (query, KV head)
-    bool fits;                                 // the grid of the call is one that there can be
-    size_t part_ml, total;                     // byte offset of the (reference, sum) of the partial results, bytes of both
-};
-KvqPlan kvq_plan(const vxl_attn_desc* d, int batch, int T, int l_cap);
-vxl_status launch_kvq_decode(const KvqPlan& p, const vxl_attn_desc* d, float scale, const void* Qd, int batch, int T,
-                             const vxl_kvq_cache* c, const vxl_kvq_cache* sp, const int32_t* src_idx, int l_cap,
-                             const int32_t* mix_len, void* O, float* LSE, void* ws, hipStream_t s);
 
 }  // namespace vxl

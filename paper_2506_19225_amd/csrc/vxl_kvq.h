@@ -1,4 +1,4 @@
-// Device and host pieces that the kernels of the quantised cache share.
+// The quantised cache: its launches, and device and host pieces that its kernels share.
 #pragma once
 
 #include <type_traits>
@@ -7,6 +7,29 @@
 #include "vxl_mfma.h"
 
 namespace vxl {
+
+// Of the caller's workspace of an in-place decode over either kind of cache, with so many bytes of partial results.
+InplaceWorkspace inplace_workspace(int batch, int l_cap, size_t partials);
+
+vxl_status launch_kvq_write(const vxl_attn_desc* d, const void* K, const void* V, int n_rows, const vxl_kvq_cache* c, int first,
+                            hipStream_t s);
+vxl_status launch_kvq_read(const vxl_attn_desc* d, const vxl_kvq_cache* c, int first, int n_rows, void* K, void* V, hipStream_t s);
+// sp: quantised sparse rows read instead of the kept rows of c, or null (here and below)
+vxl_status launch_kvq_gather(const vxl_layout* L, const vxl_attn_desc* d, const vxl_kvq_cache* c, const vxl_kvq_cache* sp,
+                             const uint8_t* dense_mask, int batch, void* Kmix, void* Vmix, int l_cap, int32_t* mix_len,
+                             int32_t* src_idx, hipStream_t s);
+struct KvqPlan {
+    int blocks;                                // 16-row blocks of a workgroup; 0: the kernel of many rows
+    int waves;                                 // of that one, per workgroup
+    long long n_rtile;                         // workgroups for the rows
+    int n_split;                               // key splits per (query, KV head)
+    bool fits;                                 // the grid of the call is one that there can be
+    size_t part_ml, total;                     // byte offset of the (reference, sum) of the partial results, bytes of both
+};
+KvqPlan kvq_plan(const vxl_attn_desc* d, int batch, int T, int l_cap);
+vxl_status launch_kvq_decode(const KvqPlan& p, const vxl_attn_desc* d, float scale, const void* Qd, int batch, int T,
+                             const vxl_kvq_cache* c, const vxl_kvq_cache* sp, const int32_t* src_idx, int l_cap,
+                             const int32_t* mix_len, void* O, float* LSE, void* ws, hipStream_t s);
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
