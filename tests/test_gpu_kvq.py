@@ -530,6 +530,30 @@ def test_the_longest_cache():
     assert e.value.status == vxl.VXL_ERR_UNSUPPORTED
 
 
+def test_a_map_of_the_plain_cache():
+    """The row map that the plain decode in place left in the workspace serves the quantised one, and the other way round."""
+    rng = np.random.default_rng(19)
+    lay = wl.random_layout(rng, 30, 5, 40, 90)
+    hq, hkv, d, n, t = 8, 2, 128, lay.n_tokens, 3
+    gl, desc = make_layout(lay), vxl.make_desc(hq, hkv, d, "bf16")
+    k, v = (torch.randn(hkv, n, d, device="cuda").bfloat16() for _ in range(2))
+    cache = vxl.KvqCache(desc, "fp8", n)
+    vxl.kvq_write(desc, k, v, cache)
+    vxl.kvq_read(desc, cache, k, v)                                 # (one set of values for both)
+    qd, mask = torch.randn(2, t, hq, d, device="cuda").bfloat16(), torch.from_numpy(some_masks(rng, 2, 5)).cuda()
+    need = max(vxl.workspace_bytes(op, gl, desc, 2, t, n) for op in (vxl.OP_DECODE_KVQ, vxl.OP_DECODE_INPLACE))
+    plain = lambda o, ws, ready: vxl.bilevel_decode_inplace(gl, desc, qd, k, v, None, None, mask, n, o, workspace=ws, map_ready=ready)  # noqa: E731
+    quant = lambda o, ws, ready: vxl.bilevel_decode_kvq(gl, desc, qd, cache, None, mask, n, o, workspace=ws, map_ready=ready)  # noqa: E731
+    for first, second in ((plain, quant), (quant, plain)):
+        ws, other = vxl.alloc_workspace(need), vxl.alloc_workspace(need)
+        outs = [torch.zeros_like(qd) for _ in range(3)]
+        first(outs[0], ws, False)
+        second(outs[1], ws, True)
+        second(outs[2], other, False)
+        assert same_bits(outs[1], outs[2])
+        assert (outs[0].float() - outs[1].float()).abs().max() <= 4 * 2.0 ** -8 * v.float().abs().max()
+
+
 # ---- together, as they are used ------------------------------------------------------------------
 def test_a_prompt_in_a_quantised_cache():
     """Chunk by chunk into the cache as the pre-filling ends them, pooled rows quantised beside; selection by the mean keys
