@@ -429,7 +429,8 @@ vxl_status vxl_gather_bilevel_kvq(const vxl_layout* layout, const vxl_attn_desc*
 /*
  * vxl_bilevel_decode_inplace over a quantised cache: every query token attends to the quantised rows of its mixed set where
  * they lie.  cache and sparse as above, other arguments as vxl_bilevel_decode_inplace (map_ready too: the row map is the same,
- * and may be one that the other call left), the workspace sized by vxl_workspace_bytes(VXL_OP_DECODE_KVQ, layout, desc, batch, n_q_tokens, l_cap), never less.
+ * and may be one that the other call left), the workspace sized by vxl_workspace_bytes(VXL_OP_DECODE_KVQ, layout, desc, batch,
+ * n_q_tokens, l_cap), never less.
  * O and LSE are those of the attention over the values that the cache reads back as, within the tolerance of the path; the
  * same call gives the same bits.  A row whose logits include NaN or +inf, or are all -inf, and one that attends to a NaN
  * value, are NaN; what a query does not attend to never matters.  256 times the sum of a row's attended |value| has to be finite.
