@@ -1,7 +1,6 @@
 // Decode attention over a quantised KV cache, its rows read in place through a row map (bf16 and fp32 queries, matrix cores).
 #include <algorithm>
 #include <limits>
-#include <numeric>
 
 #include "vxl_kvq.h"
 
@@ -38,11 +37,14 @@ namespace {
 // 448 rows by 32 (NB = 2) over 23,800 keys in 4 bits 45.5, 60 % and 27 %, 520 TFLOP/s.
 // ------------------------------------------------------------------------------------------
 // The workgroup's KV head, split, query and first row.  Workgroups that read the same keys (row tiles, and queries, whose sets
-// overlap) are members of a pair (KV head, split) and neighbours on one XCD, whose L2 serves all but the first: workgroups go to
-// the XCDs in turn, and the grid is eight pairs (fewer, if there are no more) x members x groups of eight pairs.
-__device__ __forceinline__ bool kvq_place(int n_kv_heads, int n_split, int n_rtile, int rows, int* g, int* split, int* b, int* row0) {
-    const int pair = blockIdx.z * gridDim.x + blockIdx.x, member = blockIdx.y;
-    if (pair >= n_kv_heads * n_split) return false;
+// overlap) are members of a pair (KV head, split), one behind the other on one XCD, whose L2 serves all but the first: workgroups
+// go to the XCDs in turn, so the grid is eight (fewer, if there are no more) x as many as each takes, whatever the number of pairs.
+__device__ __forceinline__ bool kvq_place(int n_kv_heads, int n_split, int n_rtile, int members, int rows, int* g, int* split, int* b,
+                                          int* row0) {
+    const unsigned all = (unsigned)(n_kv_heads * n_split * members), each = (all + gridDim.x - 1) / gridDim.x;
+    const unsigned own = blockIdx.z * gridDim.y + blockIdx.y, id = blockIdx.x * each + own;
+    if (own >= each || id >= all) return false;
+    const int pair = (int)(id / members), member = (int)(id % members);
     *g = pair / n_split;
     *split = pair % n_split;
     *b = member / n_rtile;
@@ -105,7 +107,7 @@ template <int D, int BITS, bool F32, bool POOLED, int NB>
 __global__ __launch_bounds__(64 * kKvqWaves, NB == 1 && !F32 ? 3 : 2) void kvq_decode_kernel(
     const typename Elem<F32>::T* __restrict__ Qd, KvqView dense, KvqView sparse, const int32_t* __restrict__ src_idx,
     const int32_t* __restrict__ mix_len, float* __restrict__ part_o, float2* __restrict__ part_ml, int T_q, int n_q_heads,
-    int n_kv_heads, int l_cap, int n_split, int share, int more, int n_rtile, float c2,
+    int n_kv_heads, int l_cap, int n_split, int share, int more, int n_rtile, int members, float c2,
     typename Elem<F32>::T* __restrict__ O, float* __restrict__ LSE) {
     using R = KvqRow<D, BITS>;
     using G = KvqLoad<D, BITS>;
@@ -123,7 +125,7 @@ __global__ __launch_bounds__(64 * kKvqWaves, NB == 1 && !F32 ? 3 : 2) void kvq_d
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int g, split, b, row0;
-    if (!kvq_place(n_kv_heads, n_split, n_rtile, ROWS, &g, &split, &b, &row0)) return;
+    if (!kvq_place(n_kv_heads, n_split, n_rtile, members, ROWS, &g, &split, &b, &row0)) return;
     const int group = n_q_heads / n_kv_heads, all_rows = group * T_q, n_rows = min(ROWS, all_rows - row0);
 
     const int32_t* map = src_idx + (size_t)b * l_cap;
@@ -437,7 +439,7 @@ template <int D, int BITS, bool POOLED, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void kvq_rows_kernel(
     const uint16_t* __restrict__ Qd, KvqView dense, KvqView sparse, const int32_t* __restrict__ src_idx,
     const int32_t* __restrict__ mix_len, float* __restrict__ part_o, float2* __restrict__ part_ml, int T_q, int n_q_heads,
-    int n_kv_heads, int l_cap, int n_split, int n_rtile, float c2, uint16_t* __restrict__ O, float* __restrict__ LSE) {
+    int n_kv_heads, int l_cap, int n_split, int n_rtile, int members, float c2, uint16_t* __restrict__ O, float* __restrict__ LSE) {
     using R = KvqRow<D, BITS>;
     constexpr int ROWS = 32 * NW, TILE = kKeyTile * D, DB = D / 32;
     constexpr int BYTES = D * BITS / 8 / NW, CW = std::min(4, BYTES / 4), NC = BYTES / (4 * CW);       // of a thread: bytes of a key, words of a chunk, chunks
@@ -446,7 +448,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kvq_rows_kernel(
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int g, split, b, row0;
-    if (!kvq_place(n_kv_heads, n_split, n_rtile, ROWS, &g, &split, &b, &row0)) return;
+    if (!kvq_place(n_kv_heads, n_split, n_rtile, members, ROWS, &g, &split, &b, &row0)) return;
     const int group = n_q_heads / n_kv_heads, all_rows = group * T_q;
     const int len = min(max(mix_len[b], 0), l_cap);
     // the split's tiles: an even share of the query's
@@ -710,21 +712,22 @@ static KvqPlan kvq_splits(const vxl_attn_desc* d, int batch, long long rows, int
     const float tile = blocks == 0 ? (d64 ? 1.27f : 1.76f) : blocks == 2 ? (d64 ? 0.57f : 0.76f)
                        : d->dtype == VXL_F32 ? (d64 ? 0.6f : 0.88f) : d64 ? 0.44f : 0.64f;
     const float start = blocks == 0 ? 8.f : blocks == 2 ? 5.5f : 4.2f, per_mb = blocks ? 0.9f : 0.5f, merged = blocks == 1 ? 2.8f : 2.5f;
-    const int round = kXcds / std::gcd(kXcds, d->n_kv_heads);                     // pairs (KV head, split) go to the XCDs in turn
     const long long most = std::min<long long>(steps, std::max<long long>(1, 256 * (blocks == 1 ? 3 : blocks == 2 ? 2 : 1) / per));
     *us = INFINITY;
-    for (long long n = 1; n <= most; n = n < round ? n + 1 : n + round - n % round) {
+    for (long long n = 1; n <= most;) {
+        const long long walk = (steps + n - 1) / n;
         const long long on_unit = (per * n + 255) / 256;
         const float load = blocks == 1 ? 0.36f + 0.64f * on_unit : blocks == 2 && on_unit > 1 ? 0.78f * on_unit : (float)on_unit;
         const float mb = 4e-6f * units * n * rows * d->head_dim;
         const float merge = n == 1 ? 0.f : merged + per_mb * mb + (n > 32 ? 0.9f : 0.f) + (n > 64 ? 0.4f : 0.f);
-        const float t = start + tile * load * ((steps + n - 1) / n) + merge;
+        const float t = start + tile * load * walk + merge;
         if (t < *us) {
             *us = t;
             p.n_split = (int)n;
         }
+        n = walk > 1 ? (steps + walk - 2) / (walk - 1) : most + 1;                // the next that shortens the walk
     }
-    p.fits = p.n_rtile * batch <= 65535 && (long long)d->n_kv_heads * p.n_split <= 65535ll * kXcds;
+    p.fits = p.n_rtile * batch <= 65535 && p.n_rtile * batch * d->n_kv_heads * p.n_split <= INT32_MAX;
     if (p.n_split > 1) {
         p.part_ml = align_up((size_t)units * p.n_split * rows * d->head_dim * sizeof(float), 256);
         p.total = p.part_ml + align_up((size_t)units * p.n_split * rows * sizeof(float2), 256);
@@ -755,15 +758,16 @@ vxl_status launch_kvq_decode(const KvqPlan& p, const vxl_attn_desc* d, float sca
                              const int32_t* mix_len, void* O, float* LSE, void* ws, hipStream_t s) {
     float* part_o = (float*)ws;
     float2* part_ml = (float2*)((char*)ws + p.part_ml);
-    const int pairs = d->n_kv_heads * p.n_split, n_rtile = (int)p.n_rtile;
-    const dim3 grid(std::min(pairs, kXcds), n_rtile * batch, (pairs + kXcds - 1) / kXcds);
+    const int n_rtile = (int)p.n_rtile, members = n_rtile * batch, all = d->n_kv_heads * p.n_split * members;
+    const int xcds = std::min(all, kXcds), each = (all + xcds - 1) / xcds;
+    const dim3 grid(xcds, std::min(each, 65535), (each + 65534) / 65535);
     const int tiles = (l_cap - 1) / kKvqTile + 1;
     return by_kind(d, c, [&](auto dim, auto bits, auto f32) {
         using T_ = typename Elem<f32>::T;
         auto run = [&](auto pooled, auto nb) {
             hipLaunchKernelGGL((kvq_decode_kernel<dim, bits, f32, pooled, nb>), grid, dim3(64 * kKvqWaves), 0, s,
                                (const T_*)Qd, view(c), view(sp), src_idx, mix_len, part_o, part_ml, T, d->n_q_heads, d->n_kv_heads,
-                               l_cap, p.n_split, tiles / p.n_split, tiles % p.n_split, n_rtile, scale * kLog2e, (T_*)O, LSE);
+                               l_cap, p.n_split, tiles / p.n_split, tiles % p.n_split, n_rtile, members, scale * kLog2e, (T_*)O, LSE);
         };
         auto rows = [&](auto pooled) {
             if constexpr (!f32) {
@@ -782,7 +786,7 @@ vxl_status launch_kvq_decode(const KvqPlan& p, const vxl_attn_desc* d, float sca
                 });
                 if (st != VXL_OK) return;
                 hipLaunchKernelGGL((kvq_rows_kernel<dim, bits, pooled, kRowsWaves>), grid, dim3(64 * kRowsWaves), lds, s, (const uint16_t*)Qd, view(c),
-                                   view(sp), src_idx, mix_len, part_o, part_ml, T, d->n_q_heads, d->n_kv_heads, l_cap, p.n_split, n_rtile,
+                                   view(sp), src_idx, mix_len, part_o, part_ml, T, d->n_q_heads, d->n_kv_heads, l_cap, p.n_split, n_rtile, members,
                                    scale * kLog2e, (uint16_t*)O, LSE);
             };
             if (p.blocks == 0) { if (sp) many(std::true_type{}); else many(std::false_type{}); }

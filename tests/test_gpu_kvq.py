@@ -321,11 +321,12 @@ def test_decode_of_long_sets(fmt, dtype, d, t, tokens, bsz):
 
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("pooled", [False, True])
-@pytest.mark.parametrize("hq,hkv,d,t,bsz,tokens", [(32, 4, 64, 129, 1, 6000), (32, 4, 128, 129, 1, 6000), (8, 4, 128, 200, 32, 700),
-                                                   (14, 2, 64, 129, 32, 700)])
-def test_decode_of_many_rows(fmt, pooled, hq, hkv, d, t, bsz, tokens):
-    """The kernel whose workgroups convert a tile for all their rows: row tiles and key tiles that are not full, several splits
-    and one, splits without keys, queries without any."""
+@pytest.mark.parametrize("hq,hkv,d,t,bsz,tokens,many", [
+    (32, 4, 64, 129, 1, 6000, False), (32, 4, 128, 129, 1, 6000, False), (32, 4, 64, 129, 1, 16000, True), (32, 4, 128, 129, 1, 16000, True),
+    (8, 4, 128, 200, 32, 700, True), (14, 2, 64, 129, 32, 700, True)])
+def test_decode_of_many_rows(fmt, pooled, hq, hkv, d, t, bsz, tokens, many):
+    """The kernel whose workgroups convert a tile for all their rows (`many`), and blocks of 32 rows over the same: row tiles and key
+    tiles that are not full, several splits and one, splits without keys, queries without any."""
     rng = np.random.default_rng(tokens + d + t)
     cuts = np.sort(rng.choice(np.arange(1, tokens), size=6, replace=False))
     lens = np.diff(np.concatenate([[0], cuts, [tokens]]))
@@ -336,7 +337,7 @@ def test_decode_of_many_rows(fmt, pooled, hq, hkv, d, t, bsz, tokens):
     masks[-1] = np.arange(lay.n_chunks) == 3
     desc = vxl.make_desc(hq, hkv, d, "bf16")
     kernel, n_split = vxl.debug_kvq_plan(desc, bsz, t, lay.n_tokens)
-    assert kernel == 0 and (n_split > 1) == (bsz == 1)
+    assert kernel == (0 if many else 2) and (n_split > 1) == (bsz == 1)
     check_decode(rng, "bf16", fmt, hq, hkv, d, t, lay, masks, pooled, q_gain=0.1)
 
 
