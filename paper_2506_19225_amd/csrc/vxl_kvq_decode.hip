@@ -34,11 +34,13 @@ namespace {
 // bits 10.9 (the floor of two dependent launches; a plain decode in place 8.9 and 12.7), eight queries' tokens, 64.5k keys each
 // in 4 bits 33.6 (plain 83.9): vector instructions 73 % and matrix instructions 23 % of the cycles, which do not overlap more;
 // 64 of the 174 vector instructions of a tile are conversions, 32 byte permutations, 8 exponentials.  A question of 64 tokens,
-// 448 rows by 32 (NB = 2) over 23,800 keys in 4 bits 45.5, 60 % and 27 %, 520 TFLOP/s.
+// 448 rows by 32 (NB = 2) over 23,800 keys in 4 bits 42.4 (38.7 of them here, 64 % and 28 %, 560 TFLOP/s).
 // ------------------------------------------------------------------------------------------
 // The workgroup's KV head, split, query and first row.  Workgroups that read the same keys (row tiles, and queries, whose sets
 // overlap) are members of a pair (KV head, split), one behind the other on one XCD, whose L2 serves all but the first: workgroups
-// go to the XCDs in turn, so the grid is eight (fewer, if there are no more) x as many as each takes, whatever the number of pairs.
+// go to the XCDs in turn, so the grid is eight (fewer, if there are no more) x as many as each takes, whatever the number of pairs
+// (whole pairs on an XCD: 448 rows, 23,800 keys, four heads 45.5 us instead of 42.4; a split's heads together, not a head's splits:
+// 1,792 rows, 21.7k keys 95.7 instead of 93.8).
 __device__ __forceinline__ bool kvq_place(int n_kv_heads, int n_split, int n_rtile, int members, int rows, int* g, int* split, int* b,
                                           int* row0) {
     const unsigned all = (unsigned)(n_kv_heads * n_split * members), each = (all + gridDim.x - 1) / gridDim.x;
@@ -421,8 +423,8 @@ __global__ __launch_bounds__(64 * kKvqWaves, NB == 1 && !F32 ? 3 : 2) void kvq_d
 // call, so each 64-key tile is converted once for all rows of the workgroup: NW threads load the codes of a row between them,
 // a tile ahead, and write the bf16 rows to one of two LDS stages while the other is worked on, by the products and layouts of
 // the plain decode's ring.  One barrier per tile.
-// 896 rows on four heads, 18,176 keys in 4 bits: 50.4 us and the merge, 660 TFLOP/s (plain decode in place 52.7 in all); 47 % of
-// the cycles in vector, 39 % in matrix instructions, 30 % of the LDS's in reads of K and V rows by every wave.  64 rows per
+// 896 rows on four heads, 18,176 keys in 4 bits: 48.8 us, 52 with the merge (plain decode in place 52.7), 680 TFLOP/s; 49 % of
+// the cycles in vector, 40 % in matrix instructions, 31 % of the LDS's in reads of K and V rows by every wave.  64 rows per
 // wave would halve those, but spill; four waves per workgroup and converting in turns were no faster.
 // ------------------------------------------------------------------------------------------
 // Element offset of 16-byte piece `piece` of row `row` of a V tile: its 64-byte parts turned as in the plain tile, for the
@@ -741,7 +743,7 @@ KvqPlan kvq_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     if (d->dtype != VXL_BF16 || rows <= 16) return kvq_splits(d, batch, rows, l_cap, 1, 0, &us);
     const KvqPlan p = kvq_splits(d, batch, rows, l_cap, 2, 0, &us);
     if (rows <= 128) return p;
-    // (us, blocks of 32 rows and of 256, 21.7k keys: 224 rows 24.3 and 30.4, 448 rows of 4 queries 118 and 104)
+    // (us, blocks of 32 rows and of 256, 21.7k keys: 224 rows 24.3 and 30.4, 448 rows of 4 queries 118 and 102)
     const KvqPlan many = kvq_splits(d, batch, rows, l_cap, 0, kRowsWaves, &us_many);
     return us_many < us ? many : p;
 }
