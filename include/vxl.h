@@ -432,8 +432,9 @@ vxl_status vxl_gather_bilevel_kvq(const vxl_layout* layout, const vxl_attn_desc*
  * and may be one that the other call left), the workspace sized by vxl_workspace_bytes(VXL_OP_DECODE_KVQ, layout, desc, batch,
  * n_q_tokens, l_cap), never less.
  * O and LSE are those of the attention over the values that the cache reads back as, within the tolerance of the path; the
- * same call gives the same bits.  A row whose logits include NaN or +inf, or are all -inf, and one that attends to a NaN
- * value, are NaN; what a query does not attend to never matters.  256 times the sum of a row's attended |value| has to be finite.
+ * same call gives the same bits.  A row whose logits include NaN or +inf, or are all -inf (its LSE is -inf then), and one that
+ * attends to a NaN value, are NaN, other logits of -inf weigh nothing (a scaled product past the type's range is an infinity);
+ * what a query does not attend to never matters.  256 times the sum of a row's attended |value| has to be finite.
  * Queries that share a selection (answers sampled in parallel) are better tokens of one query: they attend to the same set then,
  * and its rows are read and converted once for several of them.
  * VXL_ERR_UNSUPPORTED if batch times the row tiles of a query, 16, 32 or 256 stacked rows each by size and type, exceeds 65,535.

@@ -56,9 +56,11 @@ __device__ __forceinline__ bool kvq_place(int n_kv_heads, int n_split, int n_rti
 
 constexpr int kKvqTile = 32, kKvqWaves = 4;
 
-// A wave's reference, in the units that weights are exponentials of, before it has met a logit above -inf: the first one that
-// it meets raises it, and a logit of -inf has weight 0.
+// A row's reference in the units that weights are exponentials of: never -inf, also where the row has met no logit above it (as
+// scaled) yet, but its neighbours in the wave have and raise theirs.  The first one that it meets raises it then, and a logit
+// of -inf has weight 0.
 constexpr float kLowest = -std::numeric_limits<float>::max();
+__device__ __forceinline__ float weight_reference(float m, float c2) { return fmaxf(m * c2, kLowest); }
 
 template <bool F32> struct Parts { static constexpr int N = F32 ? 3 : 1; };
 
@@ -310,7 +312,7 @@ __global__ __launch_bounds__(64 * kKvqWaves, NB == 1 && !F32 ? 3 : 2) void kvq_d
                 const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run[nb] - m_new) * c2);
                 l_run[nb] *= alpha;
                 m_run[nb] = m_new;
-                mc_run[nb] = m_new == -INFINITY ? 0.f : m_new * c2;
+                mc_run[nb] = weight_reference(m_new, c2);
 #pragma unroll
                 for (int i = 0; i < M; ++i) o[nb][i] *= alpha;
                 against();
@@ -551,7 +553,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kvq_rows_kernel(
             const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run - m_new) * c2);
             l_run *= alpha;
             m_run = m_new;
-            mc_run = m_new == -INFINITY ? 0.f : m_new * c2;
+            mc_run = weight_reference(m_new, c2);
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll

@@ -460,6 +460,59 @@ def test_logits_below_the_smallest_number(dtype, hq, hkv, t, bsz, kernel):
     assert (np.abs(lse.double().cpu().numpy() - np.log(few)) <= 2.0 ** -21 * np.log(few)).all()
 
 
+@pytest.mark.parametrize("scale", [0.0, 4.0])
+@pytest.mark.parametrize("dtype,hq,hkv,d,t,bsz,n,kernel,one", [
+    ("bf16", 6, 2, 128, 1, 400, 2100, 1, True), ("bf16", 6, 2, 128, 1, 64, 2100, 1, False), ("f32", 6, 2, 128, 3, 400, 2100, 1, True),
+    ("f32", 6, 2, 64, 3, 64, 2100, 1, False), ("bf16", 6, 2, 64, 20, 400, 2100, 2, True), ("bf16", 6, 2, 128, 20, 16, 2100, 2, False),
+    ("bf16", 8, 4, 64, 200, 32, 2100, 0, True), ("bf16", 32, 4, 128, 129, 1, 16000, 0, False)])
+def test_rows_below_the_smallest_number_beside_others(dtype, hq, hkv, d, t, bsz, n, kernel, one, scale):
+    """Of three query rows that a wave has side by side one meets runs of keys whose products overflow to -inf (scale 4: whose
+    products do when they are scaled) before, between and behind others, one has logits of a few units with all of them, and
+    one has -inf with all: its result is NaN and its LSE -inf.  One KV head has a key of the first run that all rows can be
+    compared with."""
+    lay = wl.layout_from_lists(n, [], [])
+    desc, gl = vxl.make_desc(hq, hkv, d, dtype, scale), make_layout(lay)
+    far, gain = (2.0 ** 27, 3 / (scale * d ** 0.5)) if scale else (2.0 ** 127, 3)
+    scale = scale or d ** -0.5
+    plan = vxl.debug_kvq_plan(desc, bsz, t, n)
+    assert plan[0] == kernel and (plan[1] == 1) == one
+    rng = np.random.default_rng(n + d + t)
+    k, v = rng.standard_normal((hkv, n, d)).astype(np.float32) * np.float32(0.3), random_rows(rng, (hkv, n, d), dtype)
+    runs = np.arange(n) // 256 % 2 == 0                             # (eight 32-key tiles: two steps of a workgroup's four waves)
+    k[..., 0] = np.where(runs, -2.0 ** 100, 0)
+    k[1, 5, 0] = 0
+    k[..., -1] = -2.0 ** 100
+    rows, scales, wk, wv = quantised(wl.round_to_bf16(k), v, "fp8")
+    cache = device_cache(desc, "fp8", rows, scales)
+    some = min(bsz, 2)
+    qd = rng.standard_normal((some, t, hq, d)).astype(np.float32) * np.float32(gain)
+    kind = (np.arange(t)[:, None] * hq + np.arange(hq)) % 3
+    qd[..., 0] = np.where(kind == 0, far, 0)
+    qd[..., -1] = np.where(kind == 2, far, 0)
+    qd = wl.round_to_bf16(qd) if dtype == "bf16" else qd
+    dq = vxl.to_device(qd, dtype).repeat(bsz // some, 1, 1, 1)
+    out, lse = torch.zeros_like(dq), torch.zeros(dq.shape[:3], device="cuda")
+    ws = vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, bsz, t, n))
+    vxl.bilevel_decode_kvq(gl, desc, dq, cache, None, None, n, out, lse, None, ws)
+    for b in range(some, bsz, some):
+        assert same_bits(out[b:b + some], out[:some]) and same_bits(lse[b:b + some], lse[:some])
+    got, got_lse = out[:some].double().cpu().numpy(), lse[:some].double().cpu().numpy()
+    assert np.isnan(got[:, kind == 2]).all() and (got_lse[:, kind == 2] == -np.inf).all()
+    inner = qd.copy()
+    inner[..., [0, -1]] = 0                                         # (the elements behind a logit that is no infinity)
+    for b in range(some):
+        o, wlse, av, _ = attention(np.where(kind[..., None] == 2, 0, qd[b]), wk, wv, n, scale)
+        aq = attention(inner[b], wk, wv, n, scale)[3]
+        # the bounds of check_decode
+        logit, sums = (44 + 4) * 2.0 ** -24 * aq * 1.5 + 2.0 ** -22, (n / 16 + 100) * 2.0 ** -24
+        bound = av * (2 * logit + 2 * sums)[..., None] + n * 2.0 ** -126 * np.abs(wv).max()
+        if dtype == "bf16":
+            bound = bound + 1.01 * 2.0 ** -8 * (av + np.abs(o))
+        finite = kind < 2
+        assert (np.abs(got[b] - o)[finite] <= bound[finite]).all(), float((np.abs(got[b] - o)[finite] / bound[finite]).max())
+        assert (np.abs(got_lse[b] - wlse)[finite] <= (logit + sums + np.abs(wlse) * 2.0 ** -22)[finite]).all()
+
+
 def test_the_largest_batch():
     """65,535 queries, each as on its own with its mask; one more is refused before anything is written."""
     rng = np.random.default_rng(17)
