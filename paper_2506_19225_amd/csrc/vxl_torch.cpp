@@ -201,6 +201,8 @@ bool of_heads(const vxl_attn_desc* d, long long a) {
     return !c || !c->n_kv_heads || (c->n_kv_heads == d->n_kv_heads && c->head_dim == d->head_dim);
 }
 
+bool in_32_bits(long long n) { return n == (int32_t)n; }
+
 // Whether a tensor of so many elements holds the rows that a call takes off it, by the descriptor's layout.
 bool holds(const vxl_attn_desc* d, long long n_rows, long long numel) {
     if (n_rows <= 0) return true;                             // (for the library to refuse, or nothing to do)
@@ -275,13 +277,13 @@ PyObject* bilevel_decode_inplace(PyObject* self, PyObject* const* args, Py_ssize
 }
 PyObject* kvq_write(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     return call<kDesc, kTensor, kNumel, kTensor, kNumel, kInt, kCache, kInt>(self, args, n, [](const State& lib, const long long* a) {
-        if (!holds(desc(a[0]), a[5], a[2]) || !holds(desc(a[0]), a[5], a[4]) || a[7] != (int32_t)a[7] || !of_heads(desc(a[0]), a[6])) return VXL_ERR_INVALID_ARG;
+        if (!in_32_bits(a[5]) || !in_32_bits(a[7]) || !holds(desc(a[0]), a[5], a[2]) || !holds(desc(a[0]), a[5], a[4]) || !of_heads(desc(a[0]), a[6])) return VXL_ERR_INVALID_ARG;
         return lib.kvq_write(desc(a[0]), ptr<void>(a[1]), ptr<void>(a[3]), (int32_t)a[5], cache(a[6]), (int32_t)a[7], (vxl_stream)a[8]);
     });
 }
 PyObject* kvq_read(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     return call<kDesc, kCache, kInt, kInt, kTensor, kNumel, kTensor, kNumel>(self, args, n, [](const State& lib, const long long* a) {
-        if (!holds(desc(a[0]), a[3], a[5]) || !holds(desc(a[0]), a[3], a[7]) || a[2] != (int32_t)a[2] || !of_heads(desc(a[0]), a[1])) return VXL_ERR_INVALID_ARG;
+        if (!in_32_bits(a[2]) || !in_32_bits(a[3]) || !holds(desc(a[0]), a[3], a[5]) || !holds(desc(a[0]), a[3], a[7]) || !of_heads(desc(a[0]), a[1])) return VXL_ERR_INVALID_ARG;
         return lib.kvq_read(desc(a[0]), cache(a[1]), (int32_t)a[2], (int32_t)a[3], ptr<void>(a[4]), ptr<void>(a[6]), (vxl_stream)a[8]);
     });
 }

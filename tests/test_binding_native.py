@@ -188,6 +188,28 @@ def test_calls_end_in_the_library_that_was_loaded(streams):
             n.setup(vxl.AttnDesc, C.c_void_p, vxl._stream, *bad)
 
 
+class LikeBytes(Like):
+    dtype = torch.uint8
+
+
+def cache_of(fmt="fp4", heads=4, capacity=20, head_dim=128, ptr=0x1000):
+    code = head_dim // 2 if fmt == "fp4" else head_dim
+    return vxl.KvqCache(vxl.make_desc(heads, heads, head_dim, "bf16"), fmt, rows=LikeBytes((heads, capacity, 2, code), ptr),
+                        scales=LikeBytes((heads, capacity, 2, head_dim // 32), ptr + 0x100000))
+
+
+def test_numbers_of_rows_past_32_bits(streams):
+    """What 32 bits leave of a number of rows, or of a first row, is not what a call takes off tensors of ten rows."""
+    cache, x, y = cache_of(), Like((4, 10, 128), 0x10000), Like((4, 10, 128), 0x20000)
+    for n, first in ((-(1 << 32), 0), (10 - (1 << 32), 0), (1 << 32, 0), ((1 << 32) + 10, 0), (-1, 0), (11, 0), (0, 1 << 32), (10, 1 << 32),
+                     (10, -(1 << 32)), (1 << 62, 0), (-(1 << 62), 0)):
+        for call in (lambda: vxl.kvq_write(DESC, x, y, cache, first, n), lambda: vxl.kvq_read(DESC, cache, x, y, first, n)):
+            with pytest.raises(vxl.VxlError) as e:
+                call()
+            assert e.value.status == vxl.VXL_ERR_INVALID_ARG, (n, first)
+    vxl.kvq_write(DESC, x, y, cache, 20, 0), vxl.kvq_read(DESC, cache, x, y, 0, 0)
+
+
 def test_the_library_is_built_where_the_binding_cannot_be(monkeypatch, tmp_path):
     """By the compiler that builds the library; where that fails (no Python headers), the C library is there all the same, and
     the build says what is missing."""
