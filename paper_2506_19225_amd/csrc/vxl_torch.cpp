@@ -8,8 +8,10 @@
 // kinds at each function below): an object of another kind is refused, never taken for an address.  The result is the
 // vxl_status.
 #include <Python.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <exception>
 
 #include "vxl.h"
@@ -26,12 +28,13 @@ namespace {
 // Of one module object: a vxl.py that is loaded twice has two.
 struct State {
     PyObject *desc_type, *handle_type, *stream_of, *cache_type;
+    PyObject *rows, *scales, *format;                         // names of a cache's attributes
 #define VXL_DECLARE(name) decltype(&vxl_##name) name;
     VXL_PATH(VXL_DECLARE)
 };
 
 // Kinds of an argument: a layout's c_void_p (or a number or None, the library's to refuse); the descriptor; a quantised cache
-// or None, a null pointer; a tensor (its
+// (its tensors as they are at the call, and its format) or None, a null pointer; a tensor (its
 // data pointer; a contiguous CUDA tensor or AssertionError) or None, a null pointer; a number.  Python does not pass
 // kNumel, the number of elements of the tensor before it (0 for None), and size(i, d), dimension d of its argument i.
 enum Kind { kLayout, kDesc, kCache, kTensor, kInt, kNumel, kSize };
@@ -135,12 +138,58 @@ bool layout_of(const State& st, PyObject* o, long long* out) {
     return true;
 }
 
-bool cache_of(const State& st, PyObject* o, long long* out) {
-    void* p = nullptr;
+// A quantised cache for the library, and the heads that its tensors are of.
+struct CacheArg {
+    vxl_kvq_cache c;
+    long long n_kv_heads, head_dim;
+};
+
+// What a call keeps until it returns: the place of the next argument, the caches given, references to their tensors.
+struct Frame {
+    int next = 0, n_caches = 0, n_held = 0;
+    CacheArg caches[2];
+    PyObject* held[4];
+    ~Frame() { while (n_held > 0) Py_DECREF(held[--n_held]); }
+};
+
+// Pointer and dimensions of a cache's tensor: four, of uint8.
+bool bytes_of(Frame& f, PyObject* cache, PyObject* name, long long* p, long long (&dims)[4]) {
+    PyObject* t = PyObject_GetAttr(cache, name);
+    if (!t) return false;
+    f.held[f.n_held++] = t;
+    if (!tensor_of(t, p)) return false;
+    bool ok = t != Py_None;
+    if (ok && THPVariable_Check(t)) {
+        const at::Tensor& x = THPVariable_Unpack(t);
+        ok = x.scalar_type() == at::kByte && x.dim() == 4;
+        for (int d = 0; ok && d < 4; ++d) dims[d] = x.size(d);
+    } else if (ok) {
+        PyObject *type = PyObject_GetAttrString(t, "dtype"), *shape = type ? PyObject_GetAttrString(t, "shape") : nullptr;
+        ok = shape && THPDtype_Check(type) && ((THPDtype*)type)->scalar_type == at::kByte && PySequence_Size(shape) == 4;
+        Py_XDECREF(type);
+        Py_XDECREF(shape);
+        for (int d = 0; ok && d < 4; ++d) ok = size_of(t, d, &dims[d]);
+    }
+    if (!ok && !PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "the %U of a quantised cache are a uint8 tensor of four dimensions", name);
+    return ok;
+}
+
+bool cache_of(const State& st, Frame& f, PyObject* o, long long* out) {
     if (o == Py_None) { *out = 0; return true; }
     if (!st.cache_type || !PyObject_TypeCheck(o, (PyTypeObject*)st.cache_type)) return refuse(o, "a quantised cache");
-    if (!memory_of(o, &p)) return false;
-    *out = (long long)p;
+    long long rows, scales, r[4], s[4], format;
+    PyObject* code = PyObject_GetAttr(o, st.format);
+    const bool known = code && int_of(code, &format);
+    Py_XDECREF(code);
+    if (!known || !bytes_of(f, o, st.rows, &rows, r) || !bytes_of(f, o, st.scales, &scales, s)) return false;
+    if (r[0] != s[0] || r[1] != s[1] || r[2] != 2 || s[2] != 2 || r[3] != s[3] * (format == VXL_KVQ_FP4 ? 16 : 32)) {
+        PyErr_SetString(PyExc_ValueError, "the rows and the scales of a quantised cache do not fit each other");
+        return false;
+    }
+    CacheArg& c = f.caches[f.n_caches++];
+    c = {{(void*)rows, (void*)scales, (int32_t)std::clamp<long long>(format, -1, INT32_MAX), (int32_t)std::min<long long>(r[1], INT32_MAX)},
+         r[0], s[3] * 32};
+    *out = (long long)&c;
     return true;
 }
 
@@ -148,12 +197,13 @@ constexpr bool passed(int kind) { return kind < kNumel; }
 
 // The argument of this kind: the next of Python's, or a number read off one.
 template <int KIND>
-bool convert(const State& st, PyObject* const* args, int* next, long long* out) {
+bool convert(const State& st, PyObject* const* args, Frame& f, long long* out) {
+    int* const next = &f.next;
     if constexpr ((KIND & 255) == kSize) return size_of(args[KIND >> 8 & 255], KIND >> 16, out);
     else if constexpr (KIND == kNumel) return numel_of(args[*next - 1], out);
     else if constexpr (KIND == kLayout) return layout_of(st, args[(*next)++], out);
     else if constexpr (KIND == kDesc) return desc_of(st, args[(*next)++], out);
-    else if constexpr (KIND == kCache) return cache_of(st, args[(*next)++], out);
+    else if constexpr (KIND == kCache) return cache_of(st, f, args[(*next)++], out);
     else if constexpr (KIND == kTensor) return tensor_of(args[(*next)++], out);
     else return int_of(args[(*next)++], out);
 }
@@ -166,9 +216,9 @@ PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n, F f) {
     if (n != given) { PyErr_Format(PyExc_TypeError, "%d arguments expected, %zd given", given, n); return nullptr; }
     if (!st.desc_type) { PyErr_SetString(PyExc_RuntimeError, "setup() has not been called"); return nullptr; }
     long long a[sizeof...(KINDS) + 1], *out = a;
-    int next = 0;
+    Frame frame;
     try {
-        if (!(convert<KINDS>(st, args, &next, out++) && ...)) return nullptr;
+        if (!(convert<KINDS>(st, args, frame, out++) && ...)) return nullptr;
     } catch (const std::exception& e) {                       // (a tensor without memory)
         PyErr_SetString(PyExc_RuntimeError, e.what());
         return nullptr;
@@ -188,17 +238,12 @@ PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n, F f) {
 template <typename T> T* ptr(long long a) { return (T*)a; }
 const vxl_layout* lay(long long a) { return (const vxl_layout*)a; }
 const vxl_attn_desc* desc(long long a) { return (const vxl_attn_desc*)a; }
-// vxl.KvqCacheArg: the library's struct, and what the tensors behind it were made for (0: not told).
-struct CacheArg {
-    vxl_kvq_cache c;
-    int32_t n_kv_heads, head_dim;
-};
 const vxl_kvq_cache* cache(long long a) { return a ? &((const CacheArg*)a)->c : nullptr; }
 
 // Whether a cache (null: there is none) has the descriptor's heads.
 bool of_heads(const vxl_attn_desc* d, long long a) {
     const CacheArg* c = (const CacheArg*)a;
-    return !c || !c->n_kv_heads || (c->n_kv_heads == d->n_kv_heads && c->head_dim == d->head_dim);
+    return !c || (c->n_kv_heads == d->n_kv_heads && c->head_dim == d->head_dim);
 }
 
 bool in_32_bits(long long n) { return n == (int32_t)n; }
@@ -332,6 +377,10 @@ PyObject* setup(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 PyObject* setup_cache(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     if (n != 1 || !PyType_Check(args[0])) { PyErr_SetString(PyExc_TypeError, "a type expected"); return nullptr; }
     State& st = *(State*)PyModule_GetState(self);
+    PyObject** const names[] = {&st.rows, &st.scales, &st.format};
+    const char* const text[] = {"rows", "scales", "format"};
+    for (int i = 0; i < 3; ++i)
+        if (!*names[i] && !(*names[i] = PyUnicode_InternFromString(text[i]))) return nullptr;
     Py_INCREF(args[0]);
     Py_XSETREF(st.cache_type, args[0]);
     Py_RETURN_NONE;
@@ -352,6 +401,9 @@ int clear(PyObject* self) {
     Py_CLEAR(st->desc_type);
     Py_CLEAR(st->handle_type);
     Py_CLEAR(st->cache_type);
+    Py_CLEAR(st->rows);
+    Py_CLEAR(st->scales);
+    Py_CLEAR(st->format);
     Py_CLEAR(st->stream_of);
     return 0;
 }

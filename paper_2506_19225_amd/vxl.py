@@ -32,9 +32,8 @@ class AttnDesc(C.Structure):
 
 
 class KvqCacheArg(C.Structure):
-    """vxl_kvq_cache, and the heads and their dimension that it was made for (0: not told), which the binding compares"""
-    _fields_ = [("rows", C.c_void_p), ("scales", C.c_void_p), ("format", C.c_int32), ("capacity", C.c_int32),
-                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+    """vxl_kvq_cache"""
+    _fields_ = [("rows", C.c_void_p), ("scales", C.c_void_p), ("format", C.c_int32), ("capacity", C.c_int32)]
 
 
 class VxlError(RuntimeError):
@@ -163,7 +162,7 @@ def native():
             raise RuntimeError(f"{BINDING_PATH} was built for torch {module.torch_version}, this is {torch.__version__}: "
                                f"{build} again")
         module.setup(AttnDesc, C.c_void_p, _stream, *(C.cast(getattr(L, "vxl_" + n), C.c_void_p).value for n in _PATH))
-        module.setup_cache(KvqCacheArg)
+        module.setup_cache(KvqCache)
         _native = module
     return _native
 
@@ -330,8 +329,9 @@ def bilevel_decode_inplace(layout: Layout, desc: AttnDesc, qd, k, v, ksp, vsp, d
 
 
 class KvqCache:
-    """A quantised KV cache of one layer (vxl_kvq_cache) and the tensors that hold it: rows uint8 [Hkv, capacity, 2,
-    D * bits / 8] and scales uint8 [Hkv, capacity, 2, D / 32], allocated (uninitialised) unless given."""
+    """A quantised KV cache of one layer (vxl_kvq_cache): the tensors that hold it, rows uint8 [Hkv, capacity, 2, D * bits / 8]
+    and scales uint8 [Hkv, capacity, 2, D / 32], allocated (uninitialised) unless given, and their format.  A call takes the
+    tensors that the cache has when it is made, and checks them."""
 
     def __init__(self, desc: AttnDesc, format, capacity: Optional[int] = None, rows=None, scales=None, device="cuda"):
         code = {"fp8": KVQ_FP8, "fp4": KVQ_FP4}.get(format, format)
@@ -348,8 +348,12 @@ class KvqCache:
             if t.dtype != torch.uint8 or tuple(t.shape) != (desc.n_kv_heads, rows.shape[1], 2, last):
                 raise ValueError(f"a uint8 tensor of shape {(desc.n_kv_heads, rows.shape[1], 2, last)} expected, "
                                  f"not {t.dtype} of {tuple(t.shape)}")
-        self.rows, self.scales, self.format, self.capacity = rows, scales, code, int(rows.shape[1])
-        self.arg = KvqCacheArg(_ptr(rows), _ptr(scales), code, self.capacity, desc.n_kv_heads, desc.head_dim)
+        _ptr(rows), _ptr(scales)
+        self.rows, self.scales, self.format = rows, scales, code
+
+    @property
+    def capacity(self) -> int:
+        return int(self.rows.shape[1])
 
 
 def kvq_write(desc: AttnDesc, k, v, cache: KvqCache, first_row: int = 0, n_rows: Optional[int] = None, stream=None):
@@ -357,7 +361,7 @@ def kvq_write(desc: AttnDesc, k, v, cache: KvqCache, first_row: int = 0, n_rows:
     of these rows (n_rows None: all they hold in dense storage)."""
     if n_rows is None:
         n_rows = k.numel() // (desc.n_kv_heads * desc.head_dim)
-    st = (_native or native()).kvq_write(desc, k, v, int(n_rows), cache.arg, int(first_row), stream)
+    st = (_native or native()).kvq_write(desc, k, v, int(n_rows), cache, int(first_row), stream)
     _check(st, "vxl_kvq_write")
 
 
@@ -365,7 +369,7 @@ def kvq_read(desc: AttnDesc, cache: KvqCache, k, v, first_row: int = 0, n_rows: 
     """vxl_kvq_read: k / v from rows [first_row, first_row + n_rows) of the cache; tensors as kvq_write's."""
     if n_rows is None:
         n_rows = k.numel() // (desc.n_kv_heads * desc.head_dim)
-    st = (_native or native()).kvq_read(desc, cache.arg, int(first_row), int(n_rows), k, v, stream)
+    st = (_native or native()).kvq_read(desc, cache, int(first_row), int(n_rows), k, v, stream)
     _check(st, "vxl_kvq_read")
 
 
@@ -373,16 +377,15 @@ def gather_bilevel_kvq(layout: Layout, desc: AttnDesc, cache: KvqCache, sparse: 
                        mix_len, src_idx=None, stream=None):
     """vxl_gather_bilevel_kvq: as gather_bilevel_kv, rows read back from the quantised cache (sparse: quantised sparse rows
     [Hkv, S_total], or None: the kept rows of the cache)."""
-    st = (_native or native()).gather_bilevel_kvq(layout.handle, desc, cache.arg, sparse.arg if sparse is not None else None,
-                                                  dense_mask, kmix, vmix, mix_len, src_idx, stream)
+    st = (_native or native()).gather_bilevel_kvq(layout.handle, desc, cache, sparse, dense_mask, kmix, vmix, mix_len, src_idx, stream)
     _check(st, "vxl_gather_bilevel_kvq")
 
 
 def bilevel_decode_kvq(layout: Layout, desc: AttnDesc, qd, cache: KvqCache, sparse: Optional[KvqCache], dense_mask, l_cap: int, out,
                        lse=None, mix_len=None, workspace=None, map_ready: bool = False, stream=None):
     """vxl_bilevel_decode_kvq: as bilevel_decode_inplace, over the rows of the quantised cache."""
-    st = (_native or native()).bilevel_decode_kvq(layout.handle, desc, qd, cache.arg, sparse.arg if sparse is not None else None,
-                                                  dense_mask, int(l_cap), int(bool(map_ready)), out, lse, mix_len, workspace, stream)
+    st = (_native or native()).bilevel_decode_kvq(layout.handle, desc, qd, cache, sparse, dense_mask, int(l_cap), int(bool(map_ready)),
+                                                  out, lse, mix_len, workspace, stream)
     _check(st, "vxl_bilevel_decode_kvq")
     return out
 

@@ -210,6 +210,46 @@ def test_numbers_of_rows_past_32_bits(streams):
     vxl.kvq_write(DESC, x, y, cache, 20, 0), vxl.kvq_read(DESC, cache, x, y, 0, 0)
 
 
+def test_a_cache_is_its_tensors_at_the_call(streams):
+    """Tensors put in the place of a cache's are what the next call reads and writes, and are checked there."""
+    n, got = vxl.native(), []
+    read_cache = lambda p: (lambda c: (c.rows, c.scales, c.format, c.capacity))(C.cast(p, C.POINTER(vxl.KvqCacheArg)).contents)  # noqa: E731
+    form = C.CFUNCTYPE(C.c_int, *[C.c_void_p] * 3, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p)
+    other = form(lambda *a: got.append(read_cache(a[4])) or vxl.VXL_OK)
+    own = [C.cast(getattr(vxl.lib(), "vxl_" + x), C.c_void_p).value for x in vxl._PATH]
+    given = list(own)
+    given[vxl._PATH.index("kvq_write")] = C.cast(other, C.c_void_p).value
+    cache, x = cache_of(), Like((4, 10, 128), 0x10000)
+    write = lambda: vxl.kvq_write(DESC, x, x, cache)  # noqa: E731
+    try:
+        n.setup(vxl.AttnDesc, C.c_void_p, vxl._stream, *given)
+        write()
+        cache.rows = LikeBytes((4, 20, 2, 64), 0x700000)
+        write()
+        cache.rows, cache.scales = LikeBytes((4, 50, 2, 64), 0x800000), LikeBytes((4, 50, 2, 4), 0x900000)
+        write()
+        assert cache.capacity == 50
+        assert got == [(0x1000, 0x101000, vxl.KVQ_FP4, 20), (0x700000, 0x101000, vxl.KVQ_FP4, 20), (0x800000, 0x900000, vxl.KVQ_FP4, 50)]
+        good = cache.rows, cache.scales
+        for name, bad, error in (("rows", Like((4, 50, 2, 64)), AttributeError), ("rows", LikeBytes((4, 49, 2, 64)), ValueError),
+                                 ("rows", LikeBytes((4, 50, 2, 128)), ValueError), ("rows", LikeBytes((4, 50, 128)), ValueError),
+                                 ("rows", None, ValueError), ("scales", None, ValueError), ("rows", 0x1000, AttributeError),
+                                 ("scales", LikeBytes((3, 50, 2, 4)), ValueError), ("scales", LikeBytes((4, 50, 1, 4)), ValueError),
+                                 ("rows", LikeBytes((4, 50, 2, 64), contiguous=False), AssertionError),
+                                 ("scales", torch.zeros(4, 50, 2, 4, dtype=torch.uint8), AssertionError), ("format", "fp4", TypeError),
+                                 ("format", vxl.KVQ_FP8, ValueError)):
+            cache.rows, cache.scales, cache.format = *good, vxl.KVQ_FP4
+            setattr(cache, name, bad)
+            with pytest.raises(error):
+                write()
+        cache.rows, cache.scales, cache.format = LikeBytes((2, 50, 2, 64)), LikeBytes((2, 50, 2, 4)), vxl.KVQ_FP4
+        with pytest.raises(vxl.VxlError) as e:                  # (of other heads than the descriptor's)
+            write()
+        assert e.value.status == vxl.VXL_ERR_INVALID_ARG and len(got) == 3
+    finally:
+        n.setup(vxl.AttnDesc, C.c_void_p, vxl._stream, *own)
+
+
 def test_the_library_is_built_where_the_binding_cannot_be(monkeypatch, tmp_path):
     """By the compiler that builds the library; where that fails (no Python headers), the C library is there all the same, and
     the build says what is missing."""

@@ -745,6 +745,36 @@ def test_rows_that_a_tensor_or_a_cache_does_not_hold():
     assert (cache.rows == 3).all() and (cache.scales == 4).all() and (k == 1).all()
 
 
+def test_a_cache_whose_tensors_are_replaced():
+    """Written, read and attended to are the tensors that a cache has at the call; those it had before are left as they are."""
+    rng = np.random.default_rng(23)
+    lay = wl.random_layout(rng, 10, 4, 20, 40)
+    gl, n, desc = make_layout(lay), lay.n_tokens, vxl.make_desc(4, 2, 64, "bf16")
+    k, v = (torch.randn(2, n, 64, device="cuda").bfloat16() for _ in range(2))
+    cache, want = vxl.KvqCache(desc, "fp4", n), vxl.KvqCache(desc, "fp4", n + 5)
+    old = cache.rows.fill_(3), cache.scales.fill_(4)
+    cache.rows, cache.scales = torch.zeros(2, n + 5, 2, 32, dtype=torch.uint8, device="cuda"), torch.zeros(2, n + 5, 2, 2, dtype=torch.uint8, device="cuda")
+    for c in (cache, want):
+        c.rows.zero_(), c.scales.zero_()
+        vxl.kvq_write(desc, k, v, c, 5)
+    assert cache.capacity == n + 5 and torch.equal(cache.rows, want.rows) and torch.equal(cache.scales, want.scales) and cache.rows.any()
+    assert (old[0] == 3).all() and (old[1] == 4).all()
+    del old
+    back = [torch.zeros_like(k) for _ in range(4)]
+    vxl.kvq_read(desc, cache, *back[:2], 5), vxl.kvq_read(desc, want, *back[2:], 5)
+    assert same_bits(back[0], back[2]) and same_bits(back[1], back[3]) and back[0].any()
+    q, mask = torch.randn(1, 2, 4, 64, device="cuda").bfloat16(), torch.ones(1, 4, dtype=torch.uint8, device="cuda")
+    ws = vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, 1, 2, n))
+    out = [vxl.bilevel_decode_kvq(gl, desc, q, c, None, mask, n, torch.zeros_like(q), workspace=ws) for c in (cache, want)]
+    assert same_bits(*out) and out[0].any()
+    cache.rows.resize_(2, n - 1, 2, 32)
+    with pytest.raises(ValueError, match="do not fit"):
+        vxl.kvq_write(desc, k, v, cache)
+    cache.scales.resize_(2, n - 1, 2, 2)
+    with pytest.raises(vxl.VxlError):                               # (fewer rows than the layout's tokens)
+        vxl.bilevel_decode_kvq(gl, desc, q, cache, None, mask, n, torch.zeros_like(q), workspace=ws)
+
+
 def test_caches_of_other_heads_are_refused():
     rng = np.random.default_rng(18)
     lay = wl.random_layout(rng, 10, 4, 20, 40)
