@@ -710,14 +710,19 @@ static KvqPlan kvq_splits(const vxl_attn_desc* d, int batch, long long rows, int
     p.waves = waves;
     const int wg_rows = blocks ? 16 * blocks : 32 * waves, wg_keys = blocks ? kKvqTile * kKvqWaves : kKeyTile;
     p.n_rtile = (rows + wg_rows - 1) / wg_rows;
-    const long long units = (long long)batch * d->n_kv_heads, per = units * p.n_rtile;
+    const long long units = (long long)batch * d->n_kv_heads;
+    *us = INFINITY;
+    p.n_split = 1;
+    // (in 128 bits: beyond these bounds, which no memory's tensors reach, 64 do not hold the products)
+    p.fits = (__int128)p.n_rtile * batch <= 65535 && (__int128)p.n_rtile * units <= INT32_MAX;
+    if (!p.fits) return p;
+    const long long per = units * p.n_rtile;
     const long long steps = ((long long)l_cap + wg_keys - 1) / wg_keys;           // of a workgroup that has all keys
     const bool d64 = d->head_dim == 64;
     const float tile = blocks == 0 ? (d64 ? 1.27f : 1.76f) : blocks == 2 ? (d64 ? 0.57f : 0.76f)
                        : d->dtype == VXL_F32 ? (d64 ? 0.6f : 0.88f) : d64 ? 0.44f : 0.64f;
     const float start = blocks == 0 ? 8.f : blocks == 2 ? 5.5f : 4.2f, per_mb = blocks ? 0.9f : 0.5f, merged = blocks == 1 ? 2.8f : 2.5f;
     const long long most = std::min<long long>(steps, std::max<long long>(1, 256 * (blocks == 1 ? 3 : blocks == 2 ? 2 : 1) / per));
-    *us = INFINITY;
     for (long long n = 1; n <= most;) {
         const long long walk = (steps + n - 1) / n;
         const long long on_unit = (per * n + 255) / 256;
@@ -731,7 +736,6 @@ static KvqPlan kvq_splits(const vxl_attn_desc* d, int batch, long long rows, int
         }
         n = walk > 1 ? (steps + walk - 2) / (walk - 1) : most + 1;                // the next that shortens the walk
     }
-    p.fits = p.n_rtile * batch <= 65535 && p.n_rtile * batch * d->n_kv_heads * p.n_split <= INT32_MAX;
     if (p.n_split > 1) {
         p.part_ml = align_up((size_t)units * p.n_split * rows * d->head_dim * sizeof(float), 256);
         p.total = p.part_ml + align_up((size_t)units * p.n_split * rows * sizeof(float2), 256);

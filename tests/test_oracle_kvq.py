@@ -117,6 +117,17 @@ def test_sizes():
     assert vxl.workspace_bytes(vxl.OP_DECODE_KVQ, None, DESC, 2, 3, 1000) >= 8000
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sizes_past_64_bits(dtype):
+    """Numbers of queries, tokens and heads whose products pass 64 bits (and are 0 there) end in a number, or in the refusal."""
+    big = 1 << 30
+    for hq, hkv, b, t in ((256, 256, big, big), (512, 256, big, big), (2**31 - 1, 2**31 - 1, 2**31 - 1, 2**31 - 1), (2**31 - 1, 1, 1, 2**31 - 1),
+                          (1 << 30, 1, 1 << 15, 1 << 30), (256, 256, 1 << 16, 1 << 20), (4, 2, 65536, 1)):
+        desc = vxl.make_desc(hq, hkv, 128, dtype)
+        assert vxl.workspace_bytes(vxl.OP_DECODE_KVQ, None, desc, b, t, 100) >= b * 404
+        assert vxl.debug_kvq_plan(desc, b, t, 100)[1] == 1
+
+
 def test_cache_objects():
     with pytest.raises(ValueError, match="format"):
         vxl.KvqCache(DESC, "int4", 10)
