@@ -437,7 +437,8 @@ vxl_status vxl_gather_bilevel_kvq(const vxl_layout* layout, const vxl_attn_desc*
  * what a query does not attend to never matters.  256 times the sum of a row's attended |value| has to be finite.
  * Queries that share a selection (answers sampled in parallel) are better tokens of one query: they attend to the same set then,
  * and its rows are read and converted once for several of them.
- * VXL_ERR_UNSUPPORTED if batch times the row tiles of a query, 16, 32 or 256 stacked rows each by size and type, exceeds 65,535.
+ * VXL_ERR_UNSUPPORTED if batch exceeds 65,535, the stacked rows of a query and KV head 2^30, or the workgroups, one per query, KV
+ * head and 16, 32 or 256 stacked rows (by size and type), 2^31 - 1.
  */
 vxl_status vxl_bilevel_decode_kvq(const vxl_layout* layout, const vxl_attn_desc* desc, const void* Qd, int32_t batch,
                                   int32_t n_q_tokens, const vxl_kvq_cache* cache, const vxl_kvq_cache* sparse,

@@ -713,8 +713,9 @@ static KvqPlan kvq_splits(const vxl_attn_desc* d, int batch, long long rows, int
     const long long units = (long long)batch * d->n_kv_heads;
     *us = INFINITY;
     p.n_split = 1;
-    // (in 128 bits: beyond these bounds, which no memory's tensors reach, 64 do not hold the products)
-    p.fits = (__int128)p.n_rtile * batch <= 65535 && (__int128)p.n_rtile * units <= INT32_MAX;
+    // The pass that writes the row map has the queries in its grid's second dimension; rows and workgroups are counted in 32
+    // bits by the kernels.  (In 128 bits: 64 do not hold what these bounds refuse.)
+    p.fits = batch <= 65535 && rows <= 1 << 30 && (__int128)p.n_rtile * units <= INT32_MAX;
     if (!p.fits) return p;
     const long long per = units * p.n_rtile;
     const long long steps = ((long long)l_cap + wg_keys - 1) / wg_keys;           // of a workgroup that has all keys

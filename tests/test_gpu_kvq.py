@@ -537,6 +537,36 @@ def test_the_largest_batch():
     assert (out[bsz:] == 9.0).all() and lens[bsz] == -77
 
 
+@pytest.mark.parametrize("dtype,hq,hkv,t,bsz,kernel", [("f32", 16, 1, 14, 5000, 1), ("f32", 8, 8, 17, 33000, 1), ("bf16", 16, 1, 8, 20000, 2),
+                                                       ("bf16", 16, 1, 32, 33000, 0)])
+def test_more_row_tiles_than_a_grid_dimension(dtype, hq, hkv, t, bsz, kernel):
+    """Queries that are fewer than 65,536, but whose row tiles together are more: each as on its own with its mask."""
+    rng = np.random.default_rng(bsz)
+    lay = wl.random_layout(rng, 3, 4, 5, 12)
+    cache, sparse, values, sparse_values = prompt(rng, dtype, hkv, 64, "fp8", lay, True)
+    gl, desc, cap, rows = make_layout(lay), vxl.make_desc(hq, hkv, 64, dtype), lay.n_tokens, hq // hkv * t
+    assert vxl.debug_kvq_plan(desc, bsz, t, cap) == (kernel, 1) and bsz * -(-rows // (16 * kernel or 256)) > 65535
+    masks = some_masks(rng, 16, 4)
+    qd = wl.round_to_bf16(rng.standard_normal((16, t, hq, 64)).astype(np.float32))
+    whole, more = bsz // 16, bsz % 16
+    dm, dq = torch.from_numpy(masks).cuda().repeat(whole + 1, 1)[:bsz], vxl.to_device(qd, dtype).repeat(whole + 1, 1, 1, 1)[:bsz]
+    out = torch.full((bsz + 1, t, hq, 64), 9.0, dtype=DTYPE[dtype], device="cuda")
+    lens = torch.full((bsz + 1,), -77, dtype=torch.int32, device="cuda")
+    ws = vxl.alloc_workspace(vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, bsz, t, cap))
+    vxl.bilevel_decode_kvq(gl, desc, dq, cache, sparse, dm, cap, out[:bsz], None, lens[:bsz], ws)
+    wk, wv, wlen, _ = mixed(values, sparse_values, masks, lay, cap)
+    assert np.array_equal(lens[:bsz].cpu().numpy(), np.tile(wlen, whole + 1)[:bsz]) and lens[bsz] == -77 and (out[bsz] == 9.0).all()
+    assert same_bits(out[16:16 * whole], out[:16].repeat(whole - 1, 1, 1, 1)) and same_bits(out[16 * whole:bsz], out[:more])
+    got = out[:16].double().cpu().numpy()
+    for b in range(16):
+        n = int(wlen[b])
+        o, _, av, aq = attention(qd[b], wk[b], wv[b], n, 64 ** -0.5)
+        # the bounds of check_decode
+        bound = av * (2 * ((44 + 4) * 2.0 ** -24 * aq * 1.5 + 2.0 ** -22) + 2 * (n / 16 + 100) * 2.0 ** -24)[..., None] + n * 2.0 ** -126 * np.abs(wv).max()
+        bound = bound + (1.01 * 2.0 ** -8 * (av + np.abs(o)) if dtype == "bf16" else 0)
+        assert (np.abs(got[b] - o) <= bound).all()
+
+
 def test_the_longest_cache():
     """Rows at the end of a cache of the largest capacity, whose offsets pass 32 bits, as from one that holds them alone."""
     cap, hkv, d, p, last, fmt = 1 << 24, 2, 128, 64, 500, "fp8"
