@@ -405,12 +405,13 @@ size_t vxl_kvq_row_bytes(const vxl_attn_desc* desc, int32_t format, size_t* scal
  * Writes rows [first_row, first_row + n_rows) of the cache from K and V; other rows are left as they are.
  *   K, V   device, n_rows rows of every KV head in the descriptor's layout (strides 0: dense [n_kv_heads, n_rows, head_dim];
  *          a part of a longer tensor is its first row and the strides of the whole)
- * n_rows == 0 does nothing.  No workspace.  Errors: VXL_ERR_INVALID_ARG (null, misaligned or aliasing buffers, rows outside the
- * capacity), VXL_ERR_UNSUPPORTED, VXL_ERR_HIP.
+ * n_rows == 0 does nothing.  No workspace.  Errors: VXL_ERR_INVALID_ARG (null or misaligned buffers, rows of K or V that overlap the
+ * cache, codes that overlap scales, rows outside the capacity), VXL_ERR_UNSUPPORTED, VXL_ERR_HIP.
  */
 vxl_status vxl_kvq_write(const vxl_attn_desc* desc, const void* K, const void* V, int32_t n_rows, const vxl_kvq_cache* cache,
                          int32_t first_row, vxl_stream stream);
-/* The inverse: K and V (written, in the layout above) from rows [first_row, first_row + n_rows) of the cache. */
+/* The inverse: K and V (written, in the layout above; rows of one that overlap the other's are refused) from rows [first_row,
+ * first_row + n_rows) of the cache. */
 vxl_status vxl_kvq_read(const vxl_attn_desc* desc, const vxl_kvq_cache* cache, int32_t first_row, int32_t n_rows, void* K, void* V,
                         vxl_stream stream);
 
@@ -420,7 +421,7 @@ vxl_status vxl_kvq_read(const vxl_attn_desc* desc, const vxl_kvq_cache* cache, i
  *   sparse   quantised sparse rows in chunk order (capacity >= S_total, the format of `cache`): the pooled rows of
  *            vxl_pool_sparse_kv, or the kept rows compacted; NULL: the kept rows are read where they lie in `cache`
  * Other arguments, capacity, report of an overflow and src_idx as vxl_gather_bilevel_kv (sparse == NULL) or
- * vxl_gather_bilevel_kv_pooled.  No workspace.
+ * vxl_gather_bilevel_kv_pooled.  No workspace.  Outputs that overlap each other or a cache are refused (VXL_ERR_INVALID_ARG).
  */
 vxl_status vxl_gather_bilevel_kvq(const vxl_layout* layout, const vxl_attn_desc* desc, const vxl_kvq_cache* cache,
                                   const vxl_kvq_cache* sparse, const uint8_t* dense_mask, int32_t batch, void* Kmix, void* Vmix,
@@ -438,7 +439,8 @@ vxl_status vxl_gather_bilevel_kvq(const vxl_layout* layout, const vxl_attn_desc*
  * Queries that share a selection (answers sampled in parallel) are better tokens of one query: they attend to the same set then,
  * and its rows are read and converted once for several of them.
  * VXL_ERR_UNSUPPORTED if batch exceeds 65,535, the stacked rows of a query and KV head 2^30, or the workgroups, one per query, KV
- * head and 16, 32 or 256 stacked rows (by size and type), 2^31 - 1.
+ * head and 16, 32 or 256 stacked rows (by size and type), 2^31 - 1.  VXL_ERR_INVALID_ARG also if O, LSE, mix_len or the workspace
+ * overlaps another of them, the queries or a cache.
  */
 vxl_status vxl_bilevel_decode_kvq(const vxl_layout* layout, const vxl_attn_desc* desc, const void* Qd, int32_t batch,
                                   int32_t n_q_tokens, const vxl_kvq_cache* cache, const vxl_kvq_cache* sparse,

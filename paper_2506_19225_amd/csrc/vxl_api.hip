@@ -657,6 +657,67 @@ static bool cache_ok(const vxl_kvq_cache* c, vxl_status* st) {
     return true;
 }
 
+// Bytes [at, at + bytes) of memory (none: no buffer there).
+struct Range {
+    uintptr_t at;
+    size_t bytes;
+};
+static Range range(const void* p, size_t bytes) { return {(uintptr_t)p, p ? bytes : 0}; }
+static bool meet(Range a, Range b) { return a.bytes > 0 && b.bytes > 0 && a.at < b.at + b.bytes && b.at < a.at + a.bytes; }
+
+static Range codes_of(const vxl_attn_desc* d, const vxl_kvq_cache* c) {
+    return c ? range(c->rows, (size_t)d->n_kv_heads * c->capacity * vxl_kvq_row_bytes(d, c->format, nullptr)) : Range{};
+}
+static Range scales_of(const vxl_attn_desc* d, const vxl_kvq_cache* c) {
+    return c ? range(c->scales, (size_t)d->n_kv_heads * c->capacity * (2 * d->head_dim / 32)) : Range{};
+}
+
+// Whether an output meets another one or an input.
+static bool outputs_meet(std::initializer_list<Range> out, std::initializer_list<Range> in) {
+    for (const Range* a = out.begin(); a != out.end(); ++a) {
+        for (const Range* b = out.begin(); b != a; ++b)
+            if (meet(*a, *b)) return true;
+        for (const Range& b : in)
+            if (meet(*a, b)) return true;
+    }
+    return false;
+}
+
+// Whether first + i * step lies between lo and hi, neither included, for an i in [0, n).
+static bool steps_into(__int128 first, __int128 step, long long n, __int128 lo, __int128 hi) {
+    const __int128 i = first > lo ? 0 : (lo - first) / step + 1;
+    return i < n && first + i * step < hi;
+}
+
+// Plain rows in the descriptor's layout, in bytes.
+struct PlainRows {
+    __int128 at, head, tok;
+    long long heads, n, bytes;
+    PlainRows(const vxl_attn_desc* d, const void* p, int n_rows) : at((uintptr_t)p), heads(d->n_kv_heads), n(n_rows) {
+        const TokStrides ts = tok_strides(d, n_rows);
+        const size_t e = elem_bytes(d);
+        head = (__int128)ts.kh * e;
+        tok = (__int128)ts.kt * e;
+        bytes = d->head_dim * e;
+    }
+    __int128 span() const { return (heads - 1) * head + (n - 1) * tok + bytes; }
+    // Whether one of the rows meets r.
+    bool meet(Range r) const {
+        const __int128 lo = r.at, hi = lo + r.bytes;
+        if (r.bytes == 0 || hi <= at || at + span() <= lo) return false;
+        for (long long g = 0; g < heads; ++g)
+            if (steps_into(at + g * head, tok, n, lo - bytes, hi)) return true;
+        return false;
+    }
+    // Whether one of the rows meets one of the same many, as far apart, from another address on.
+    bool meet(const PlainRows& o) const {
+        if (o.at + span() <= at || at + span() <= o.at) return false;
+        for (long long g = 1 - heads; g < heads; ++g)
+            if (steps_into(o.at - at + g * head - (n - 1) * tok, tok, 2 * n - 1, -bytes, bytes)) return true;
+        return false;
+    }
+};
+
 // Arguments that a gather and a decode of quantised rows share; *sp: the sparse rows where there are any.
 static vxl_status kvq_sets_ok(const vxl_layout* L, const vxl_kvq_cache* cache, const vxl_kvq_cache* sparse,
                               const uint8_t* dense_mask, int32_t batch, int32_t l_cap, const vxl_kvq_cache** sp) {
@@ -685,6 +746,11 @@ static vxl_status kvq_rows_ok(const vxl_attn_desc* d, const void* K, const void*
     if (n_rows > 0 && (!K || !V || !aligned16(K) || !aligned16(V))) return VXL_ERR_INVALID_ARG;
     for (const void* p : {K, V})
         if (p && (p == cache->rows || p == cache->scales)) return VXL_ERR_INVALID_ARG;
+    if (n_rows > 0)
+        for (const void* p : {K, V}) {
+            const PlainRows rows(d, p, n_rows);
+            if (rows.meet(codes_of(d, cache)) || rows.meet(scales_of(d, cache))) return VXL_ERR_INVALID_ARG;
+        }
     return VXL_OK;
 }
 
@@ -692,6 +758,7 @@ vxl_status vxl_kvq_write(const vxl_attn_desc* d, const void* K, const void* V, i
                          int32_t first_row, vxl_stream stream) {
     const vxl_status st = kvq_rows_ok(d, K, V, n_rows, cache, first_row);
     if (st != VXL_OK || n_rows == 0) return st;
+    if (meet(codes_of(d, cache), scales_of(d, cache))) return VXL_ERR_INVALID_ARG;
     return launch_kvq_write(d, K, V, n_rows, cache, first_row, (hipStream_t)stream);
 }
 
@@ -699,7 +766,7 @@ vxl_status vxl_kvq_read(const vxl_attn_desc* d, const vxl_kvq_cache* cache, int3
                         vxl_stream stream) {
     const vxl_status st = kvq_rows_ok(d, K, V, n_rows, cache, first_row);
     if (st != VXL_OK || n_rows == 0) return st;
-    if (K == V) return VXL_ERR_INVALID_ARG;
+    if (PlainRows(d, K, n_rows).meet(PlainRows(d, V, n_rows))) return VXL_ERR_INVALID_ARG;
     return launch_kvq_read(d, cache, first_row, n_rows, K, V, (hipStream_t)stream);
 }
 
@@ -711,7 +778,11 @@ vxl_status vxl_gather_bilevel_kvq(const vxl_layout* L, const vxl_attn_desc* d, c
     if (!L) return VXL_ERR_INVALID_ARG;
     if (!desc_ok(d, &st)) return st;
     if ((st = kvq_sets_ok(L, cache, sparse, dense_mask, batch, l_cap, &sp)) != VXL_OK) return st;
-    if (!Kmix || !Vmix || !mix_len || !aligned16(Kmix) || !aligned16(Vmix) || Kmix == Vmix) return VXL_ERR_INVALID_ARG;
+    if (!Kmix || !Vmix || !mix_len || !aligned16(Kmix) || !aligned16(Vmix)) return VXL_ERR_INVALID_ARG;
+    const size_t rows = (size_t)batch * l_cap, bytes = rows * d->n_kv_heads * d->head_dim * elem_bytes(d);
+    if (outputs_meet({range(Kmix, bytes), range(Vmix, bytes), range(mix_len, batch * sizeof(int32_t)), range(src_idx, rows * sizeof(int32_t))},
+                     {codes_of(d, cache), scales_of(d, cache), codes_of(d, sp), scales_of(d, sp)}))
+        return VXL_ERR_INVALID_ARG;
     return launch_kvq_gather(L, d, cache, sp, dense_mask, batch, Kmix, Vmix, l_cap, mix_len, src_idx, (hipStream_t)stream);
 }
 
@@ -729,6 +800,10 @@ vxl_status vxl_bilevel_decode_kvq(const vxl_layout* L, const vxl_attn_desc* d, c
     if (!p.fits) return VXL_ERR_UNSUPPORTED;
     const InplaceWorkspace w = inplace_workspace(batch, l_cap, p.total);
     if (!workspace || workspace_bytes < w.total || !aligned16(workspace)) return VXL_ERR_WORKSPACE;
+    const size_t rows = (size_t)batch * n_q_tokens * d->n_q_heads, bytes = rows * d->head_dim * elem_bytes(d);
+    if (outputs_meet({range(O, bytes), range(LSE, rows * sizeof(float)), range(mix_len, batch * sizeof(int32_t)), range(workspace, w.total)},
+                     {range(Qd, bytes), codes_of(d, cache), scales_of(d, cache), codes_of(d, sp), scales_of(d, sp)}))
+        return VXL_ERR_INVALID_ARG;
     hipStream_t s = (hipStream_t)stream;
     int32_t* src_idx = (int32_t*)((char*)workspace + w.src_idx);
     int32_t* len = mix_len ? mix_len : (int32_t*)((char*)workspace + w.mix_len);

@@ -775,6 +775,78 @@ def test_rows_that_a_tensor_or_a_cache_does_not_hold():
     assert (cache.rows == 3).all() and (cache.scales == 4).all() and (k == 1).all()
 
 
+def test_buffers_side_by_side():
+    """Keys and values of one tensor, token by token, and everything in one allocation without a gap: the same rows."""
+    hkv, n, d = 4, 33, 64
+    desc = vxl.make_desc(hkv, hkv, d, "bf16")
+    k, v = (torch.randn(hkv, n, d, device="cuda").bfloat16() for _ in range(2))
+    want = vxl.KvqCache(desc, "fp4", n)
+    vxl.kvq_write(desc, k, v, want)
+    pair = vxl.make_desc(hkv, hkv, d, "bf16")
+    pair.q_stride_head = pair.kv_stride_head = d
+    pair.q_stride_tok = pair.kv_stride_tok = 2 * hkv * d
+    both = torch.stack((k, v)).permute(2, 0, 1, 3).contiguous()         # [n, 2, hkv, d]
+    cache = vxl.KvqCache(desc, "fp4", n)
+    flat = both.view(-1)
+    vxl.kvq_write(pair, flat, flat[hkv * d:], cache, 0, n)
+    assert torch.equal(cache.rows, want.rows) and torch.equal(cache.scales, want.scales)
+    back = torch.zeros_like(flat)
+    vxl.kvq_read(pair, cache, back, back[hkv * d:], 0, n)
+    values = [torch.zeros_like(k) for _ in range(2)]
+    vxl.kvq_read(desc, want, *values)
+    assert same_bits(back.view(n, 2, hkv, d), torch.stack(values).permute(2, 0, 1, 3).contiguous())
+    plain, codes, scales = k.numel() * 2, want.rows.numel(), want.scales.numel()
+    room = torch.zeros(2 * plain + codes + scales, dtype=torch.uint8, device="cuda")
+    kk, vv, rows, sc = room.split([plain, plain, codes, scales])
+    near = vxl.KvqCache(desc, "fp4", rows=rows.view_as(want.rows), scales=sc.view_as(want.scales))
+    kk.view(torch.bfloat16).copy_(k.view(-1)), vv.view(torch.bfloat16).copy_(v.view(-1))
+    vxl.kvq_write(desc, kk.view(torch.bfloat16), vv.view(torch.bfloat16), near)
+    assert torch.equal(near.rows, want.rows) and torch.equal(near.scales, want.scales)
+    vxl.kvq_read(desc, near, kk.view(torch.bfloat16), vv.view(torch.bfloat16))
+    assert same_bits(kk.view(torch.bfloat16).view_as(k), values[0]) and same_bits(vv.view(torch.bfloat16).view_as(v), values[1])
+
+
+def test_outputs_that_overlap():
+    """A mixed set, a result, an LSE, lengths or a workspace in a cache or in another of them: refused, and nothing is written."""
+    rng = np.random.default_rng(29)
+    lay = wl.random_layout(rng, 10, 4, 20, 40)
+    cache, sparse, _, _ = prompt(rng, "bf16", 2, 64, "fp4", lay, True)
+    gl, desc, n = make_layout(lay), vxl.make_desc(4, 2, 64, "bf16"), lay.n_tokens
+    before = [t.clone() for c in (cache, sparse) for t in (c.rows, c.scales)]
+    mask = torch.ones(1, 4, dtype=torch.uint8, device="cuda")
+    size, need = 2 * n * 64 * 2, vxl.workspace_bytes(vxl.OP_DECODE_KVQ, gl, desc, 1, 3, n)
+
+    class At:                                                           # (a tensor of this size at this address, in bounds or not)
+        is_cuda = True
+
+        def __init__(self, ptr, shape):
+            self.ptr, self.shape = ptr, shape
+        is_contiguous, data_ptr, numel = (lambda self: True), (lambda self: self.ptr), (lambda self: int(np.prod(self.shape)))
+
+    part = (size + need) // 256 * 256 + 256
+    room = torch.zeros(7 * part, dtype=torch.uint8, device="cuda")
+    free = room.data_ptr()
+    mix = lambda p: At(p, (1, 2, n, 64))  # noqa: E731
+    q = lambda p: At(p, (1, 3, 4, 64))  # noqa: E731
+    kmix, vmix, lens, ws, qd, out, lse = (free + i * part for i in range(7))
+    gather = lambda k=kmix, v=vmix, m=lens, s=0: vxl.gather_bilevel_kvq(gl, desc, cache, sparse, mask, mix(k), mix(v), At(m, (1,)), At(s, (1, n)) if s else None)  # noqa: E731
+    decode = lambda o=out, l=lse, m=lens, w=ws: vxl.bilevel_decode_kvq(gl, desc, q(qd), cache, sparse, mask, n, q(o), At(l, (1, 3, 4)), At(m, (1,)), At(w, (need,)))  # noqa: E731
+    inside = [t.data_ptr() + t.numel() // 2 // 16 * 16 for c in (cache, sparse) for t in (c.rows, c.scales)]
+    calls = [(gather, dict(v=kmix + 16)), (gather, dict(m=kmix + 64)), (gather, dict(s=vmix)), (gather, dict(s=lens - 4))]
+    calls += [(gather, {x: p}) for x in "kvms" for p in inside] + [(decode, {x: p}) for x in "olmw" for p in inside]
+    calls += [(decode, dict(o=qd + 16)), (decode, dict(l=out + 4)), (decode, dict(m=lse)), (decode, dict(w=out - 256)), (decode, dict(w=qd - need + 16)),
+              (decode, dict(m=ws + need - 4))]
+    for call, kw in calls:
+        with pytest.raises(vxl.VxlError) as e:
+            call(**kw)
+        assert e.value.status == vxl.VXL_ERR_INVALID_ARG, kw
+    torch.cuda.synchronize()
+    assert not room.any() and all(torch.equal(a, b) for a, b in zip(before, [t for c in (cache, sparse) for t in (c.rows, c.scales)]))
+    gather(), decode()
+    torch.cuda.synchronize()
+    assert room.any()
+
+
 def test_a_cache_whose_tensors_are_replaced():
     """Written, read and attended to are the tensors that a cache has at the call; those it had before are left as they are."""
     rng = np.random.default_rng(23)

@@ -97,6 +97,32 @@ def test_refusals_of_write_and_read(call):
     assert lib.vxl_kvq_read(C.byref(DESC), C.byref(arg()), 0, 1, 0x10000, 0x10000, None) == bad
 
 
+@pytest.mark.parametrize("call", [write, read])
+def test_buffers_that_overlap(call):
+    """Ten rows of four heads, 10,240 bytes or parts of a longer tensor, and a cache with 51,200 bytes of codes and 3,200 of scales."""
+    bad, at = vxl.VXL_ERR_INVALID_ARG, 0x1000000
+    cache = arg(rows=at, scales=at + 0x100000)
+    ends = [lo + off for lo, size in ((at, 51200), (at + 0x100000, 3200)) for off in (16 - 10240, -16, 16, size - 16)]
+    for p in ends:
+        assert call(k=p, v=0x20000, cache=cache) == call(k=0x20000, v=p, cache=cache) == bad, hex(p)
+        assert call(k=p, v=0x20000, cache=cache, desc=vxl.make_desc(28, 4, 128, "bf16", token_major=True)) == bad
+    long = vxl.make_desc(28, 4, 128, "bf16")                            # (rows of a tensor of 100,000 bytes per head)
+    long.q_stride_head = long.kv_stride_head = 50000
+    long.q_stride_tok = long.kv_stride_tok = 128
+    for g in range(4):
+        assert call(k=at - g * 100000 - 9 * 256, v=0x20000, cache=cache, desc=long) == bad
+    if call is write:
+        for off in (0, 16, 51200 - 16, 16 - 3200):
+            assert call(cache=arg(rows=at, scales=at + off)) == bad
+    else:
+        pair = vxl.make_desc(28, 4, 128, "bf16")                        # (a key and its value side by side, 2,048 bytes a token)
+        pair.q_stride_head = pair.kv_stride_head = 128
+        pair.q_stride_tok = pair.kv_stride_tok = 1024
+        for desc, off in ((DESC, 10240 - 16), (DESC, 16 - 10240), (pair, 1024 - 16), (pair, 16), (pair, 2048 * 9 + 1008), (long, 100000 * 3),
+                          (long, 2560 - 16)):
+            assert call(k=0x800000, v=0x800000 + off, cache=cache, desc=desc) == bad, off
+
+
 def test_refusals_without_a_layout():
     lib, c = vxl.lib(), C.byref(arg())
     assert lib.vxl_gather_bilevel_kvq(None, C.byref(DESC), c, None, 0x10, 1, 0x10000, 0x20000, 10, 0x30, None,
