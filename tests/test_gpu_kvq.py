@@ -193,6 +193,76 @@ def test_gather(fmt, pooled, dtype, hkv, d, bsz, chunks, prefix):
             assert np.array_equal(src[b, :n].cpu().numpy(), wsrc[b, :n]) and (src[b, n:] == -5).all()
 
 
+@pytest.mark.parametrize("fmt,pooled,dtype,hkv,d,bsz,chunks,length,groups", [
+    ("fp4", False, "bf16", 4, 128, 1, 640, 28, 2), ("fp8", True, "bf16", 4, 128, 1, 640, 28, 2), ("fp8", False, "bf16", 2, 64, 3, 1500, 33, 3),
+    ("fp4", True, "f32", 1, 64, 1, 1600, 20, 3), ("fp8", False, "f32", 3, 128, 1, 3000, 12, 6), ("fp4", True, "bf16", 1, 64, 2, 3500, 40, 7)])
+def test_gather_of_several_passes_per_block(fmt, pooled, dtype, hkv, d, bsz, chunks, length, groups):
+    """Sets of so many chunks that a block takes several passes over its rows (`groups`, as the launch counts them)."""
+    rng = np.random.default_rng(chunks + d)
+    lay = wl.random_layout(rng, 37, chunks, 1, 2 * length)
+    l_cap = lay.n_tokens + 5
+    rows = 256 // (d // (8 if dtype == "bf16" else 4))
+    assert max(1, min(8, 1 + chunks // 512, -(-l_cap // rows) * bsz // 512)) == groups
+    cache, sparse, values, sparse_values = prompt(rng, dtype, hkv, d, fmt, lay, pooled)
+    masks = some_masks(rng, bsz, chunks)
+    masks[0] = rng.integers(0, 3, size=chunks) > 0
+    wk, wv, wlen, wsrc = mixed(values, sparse_values, masks, lay, l_cap)
+    desc = vxl.make_desc(hkv, hkv, d, dtype)
+    kmix = torch.full((bsz, hkv, l_cap, d), 7.0, dtype=DTYPE[dtype], device="cuda")
+    vmix = torch.full_like(kmix, 7.0)
+    lens, src = torch.full((bsz,), -1, dtype=torch.int32, device="cuda"), torch.full((bsz, l_cap), -5, dtype=torch.int32, device="cuda")
+    vxl.gather_bilevel_kvq(make_layout(lay), desc, cache, sparse, torch.from_numpy(masks).cuda(), kmix, vmix, lens, src)
+    assert np.array_equal(lens.cpu().numpy(), wlen)
+    for b in range(bsz):
+        n = int(wlen[b])
+        for got, want in ((kmix, wk), (vmix, wv)):
+            got = got[b].double().cpu().numpy()
+            assert np.array_equal(got[:, :n], want[b, :, :n]) and (got[:, n:] == 7.0).all()
+        assert np.array_equal(src[b, :n].cpu().numpy(), wsrc[b, :n]) and (src[b, n:] == -5).all()
+
+
+@pytest.mark.parametrize("fmt,pooled,dtype,hkv,d,bsz", [
+    ("fp4", False, "bf16", 4, 128, 8), ("fp8", True, "bf16", 4, 128, 8), ("fp4", True, "bf16", 2, 64, 20), ("fp8", False, "bf16", 3, 64, 20),
+    ("fp4", False, "f32", 1, 128, 16), ("fp8", True, "f32", 4, 64, 9)])
+def test_gather_past_the_caches(fmt, pooled, dtype, hkv, d, bsz):
+    """Sets of 160 MB and more, whose rows are stored past the caches, beside smaller ones, which are not: every row is the one that
+    the cache reads back as."""
+    rng = np.random.default_rng(d + hkv)
+    elem = 2 if dtype == "bf16" else 4
+    row = 2 * bsz * hkv * d * elem                                  # bytes of one row of all sets
+    tokens = (160 << 20) // row + 3000
+    lens = [int(x) for x in np.diff(np.concatenate([[0], np.sort(rng.choice(np.arange(1, tokens), size=40, replace=False)), [tokens]]))]
+    starts = 21 + np.cumsum([0] + lens[:-1])
+    lay = wl.layout_from_lists(21, lens, [np.sort(rng.choice(n, size=n // 5, replace=False)).astype(np.int32) + s for n, s in zip(lens, starts)])
+    desc, n, n_sparse = vxl.make_desc(hkv, hkv, d, dtype), lay.n_tokens, len(lay.sparse_idx)
+    gen = torch.Generator("cuda").manual_seed(hkv)
+    values = []
+    caches = [vxl.KvqCache(desc, fmt, size) for size in ([n, n_sparse] if pooled else [n])]
+    for c in caches:
+        k, v = (torch.randn(hkv, c.capacity, d, generator=gen, device="cuda").to(DTYPE[dtype]) for _ in range(2))
+        vxl.kvq_write(desc, k, v, c)
+        vxl.kvq_read(desc, c, k, v)
+        values.append((k, v))
+    masks = some_masks(rng, bsz, lay.n_chunks)
+    masks[2:] |= rng.integers(0, 50, size=masks[2:].shape) > 0
+    kmix = torch.full((bsz, hkv, n + 9, d), 7.0, dtype=DTYPE[dtype], device="cuda")
+    vmix, lens_got = torch.full_like(kmix, 7.0), torch.zeros(bsz, dtype=torch.int32, device="cuda")
+    vxl.gather_bilevel_kvq(make_layout(lay), desc, caches[0], caches[1] if pooled else None, torch.from_numpy(masks).cuda(), kmix, vmix, lens_got)
+    past = []
+    for b in range(bsz):
+        src = [np.arange(21)]
+        for c in range(lay.n_chunks):
+            dense, kept = np.arange(lay.chunk_bounds[c], lay.chunk_bounds[c + 1]), np.arange(lay.sparse_offsets[c], lay.sparse_offsets[c + 1])
+            src.append(dense if masks[b, c] else n + kept if pooled else lay.sparse_idx[kept])
+        src = torch.from_numpy(np.concatenate(src).astype(np.int64)).cuda()
+        past.append(row * len(src) > 160 << 20)
+        assert int(lens_got[b]) == len(src)
+        for got, i in ((kmix, 0), (vmix, 1)):
+            want = torch.cat([x[i] for x in values], 1)[:, src]
+            assert same_bits(got[b, :, :len(src)], want) and (got[b, :, len(src):] == 7.0).all()
+    assert any(past) and not all(past)
+
+
 def test_gather_reports_an_overflow():
     rng = np.random.default_rng(3)
     lay = wl.random_layout(rng, 9, 6, 20, 50)
