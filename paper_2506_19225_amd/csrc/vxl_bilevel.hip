@@ -22,13 +22,6 @@ __device__ __forceinline__ uint4 load16(const uint4* p) {
     if constexpr (NT) return __builtin_bit_cast(uint4, __builtin_nontemporal_load((const u32x4*)p));
     else return *p;
 }
-// 16 bytes that the caches need not keep (NT)
-template <bool NT>
-__device__ __forceinline__ void store16(uint4* p, uint4 v) {
-    typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
-    if constexpr (NT) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
-    else *p = v;
-}
 
 // ------------------------------------------------------------------------------------------
 // kbar[g, c, :] = mean of the dense key rows of chunk c.  One block per (chunk, kv head).
@@ -485,7 +478,6 @@ __global__ __launch_bounds__(256, 8) void pool_sparse_kernel(const T* __restrict
 // With Kmix == nullptr nothing is copied at all: the call only writes mix_len and src_idx (the row
 // map the in-place decode reads the dense and sparse rows through).
 // ------------------------------------------------------------------------------------------
-constexpr long long kPastCaches = 160ll << 20;
 template <int ROW_BYTES, bool FOUR, bool ONCE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(FOUR ? 4 : 8, FOUR ? 4 : 8))) void gather_kernel(
     const uint4* __restrict__ K, const uint4* __restrict__ V, const uint8_t* __restrict__ dense_mask,

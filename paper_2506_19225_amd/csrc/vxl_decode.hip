@@ -11,6 +11,7 @@
 
 #include "vxl_internal.h"
 #include "vxl_mfma.h"
+#include "vxl_round.h"
 
 namespace vxl {
 
@@ -28,13 +29,6 @@ struct RowMap {
     long long kv_tok;           // elements
     int s_total;
 };
-
-__device__ __forceinline__ uint16_t f32_to_bf16(float v) {
-    uint32_t b = __float_as_uint(v);
-    if ((b & 0x7fffffffu) > 0x7f800000u) return 0x7fc0;
-    b += 0x7fffu + ((b >> 16) & 1u);
-    return (uint16_t)(b >> 16);
-}
 
 // Four results of a row that has one split, whose merge is the value itself (`some`: the row's LSE is a number;
 // like the merge, a row without keys or with an LSE that is none gives 0).

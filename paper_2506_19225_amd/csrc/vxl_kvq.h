@@ -20,7 +20,6 @@ vxl_status launch_kvq_gather(const vxl_layout* L, const vxl_attn_desc* d, const 
                              int32_t* src_idx, hipStream_t s);
 struct KvqPlan {
     int blocks;                                // 16-row blocks of a workgroup; 0: the kernel of many rows
-    int waves;                                 // of that one, per workgroup
     long long n_rtile;                         // workgroups for the rows
     int n_split;                               // key splits per (query, KV head)
     bool fits;                                 // the grid of the call is one that there can be

@@ -126,14 +126,6 @@ template <int CTRL>
 __device__ __forceinline__ uint32_t from_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true); }
 constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e, kMirror8 = 0x141, kShiftLeft = 0x100;
 
-// 16 bytes that the caches need not keep (NT)
-template <bool NT>
-__device__ __forceinline__ void store16(uint4* p, uint4 v) {
-    typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
-    if constexpr (NT) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
-    else *p = v;
-}
-
 // ------------------------------------------------------------------------------------------
 // Rows [first, first + n_rows) of the cache from K and V: a lane takes 16 bytes of a key row and of its value row, the lanes
 // of a block find its largest magnitude by exchange, and the first lane of 16 stores the scales of all of them.
@@ -222,8 +214,6 @@ __global__ __launch_bounds__(256) void kvq_read_kernel(uint4* __restrict__ K, ui
 // Bound by the writes.  us: eight sets of 25k rows of 8 bits, 497 MB, one head after the other 141, four together 123, past the
 // caches 96 (5.2 TB/s); one set of 45,312 rows of 4 bits 40 -> 31 -> 28; queries one after the other instead of in turn 129.
 // ------------------------------------------------------------------------------------------
-constexpr long long kPastCaches = 160ll << 20;
-
 template <int D, int BITS, bool F32, int HEADS>
 __global__ __launch_bounds__(256) void kvq_gather_kernel(KvqView dense, KvqView sparse, bool pooled,
                                                          const uint8_t* __restrict__ dense_mask, const int32_t* __restrict__ bounds,

@@ -3,6 +3,7 @@
 #include <limits>
 
 #include "vxl_kvq.h"
+#include "vxl_round.h"
 
 namespace vxl {
 
@@ -80,15 +81,11 @@ __device__ __forceinline__ void split_bf16(float x, __bf16 (&part)[N]) {
     }
 }
 
-__device__ __forceinline__ uint16_t to_bf16_bits(float v) {
-    const uint32_t b = __float_as_uint(v);
-    return (b & 0x7fffffffu) > 0x7f800000u ? 0x7fc0 : (uint16_t)((b + 0x7fffu + ((b >> 16) & 1u)) >> 16);
-}
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store1(uint16_t* p, float v) { *p = to_bf16_bits(v); }
+__device__ __forceinline__ void store1(uint16_t* p, float v) { *p = f32_to_bf16(v); }
 __device__ __forceinline__ void store4(float* p, const float (&v)[4]) { *(float4*)p = make_float4(v[0], v[1], v[2], v[3]); }
 __device__ __forceinline__ void store4(uint16_t* p, const float (&v)[4]) {
-    __attribute__((aligned(8))) const uint16_t o[4] = {to_bf16_bits(v[0]), to_bf16_bits(v[1]), to_bf16_bits(v[2]), to_bf16_bits(v[3])};
+    __attribute__((aligned(8))) const uint16_t o[4] = {f32_to_bf16(v[0]), f32_to_bf16(v[1]), f32_to_bf16(v[2]), f32_to_bf16(v[3])};
     *(uint2*)p = *(const uint2*)o;
 }
 
@@ -421,8 +418,8 @@ __global__ __launch_bounds__(64 * kKvqWaves, NB == 1 && !F32 ? 3 : 2) void kvq_d
 }
 
 // ------------------------------------------------------------------------------------------
-// Decode of many stacked rows: 32 rows per wave, NW waves per workgroup.  Here the matrix cores and what feeds them bound the
-// call, so each 64-key tile is converted once for all rows of the workgroup: NW threads load the codes of a row between them,
+// Decode of many stacked rows: 32 rows per wave, eight waves per workgroup.  Here the matrix cores and what feeds them bound the
+// call, so each 64-key tile is converted once for all rows of the workgroup: eight threads load the codes of a row between them,
 // a tile ahead, and write the bf16 rows to one of two LDS stages while the other is worked on, by the products and layouts of
 // the plain decode's ring.  One barrier per tile.
 // 896 rows on four heads, 18,176 keys in 4 bits: 48.8 us, 52 with the merge (plain decode in place 52.7), 680 TFLOP/s; 49 % of
@@ -437,22 +434,22 @@ __device__ __forceinline__ int rows_v_off(int row, int piece) {
     return row * D + ((((piece >> 2) ^ ((row / RPL) & (CPR - 1))) << 2 | ((piece & 3) ^ ((row >> 2) & 3))) << 3);
 }
 
-constexpr int kRowsWaves = 8;
+constexpr int kRowsWaves = 8, kRowsTile = 32 * kRowsWaves;
 
-template <int D, int BITS, bool POOLED, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void kvq_rows_kernel(
+template <int D, int BITS, bool POOLED>
+__global__ __launch_bounds__(64 * kRowsWaves, 2) void kvq_rows_kernel(
     const uint16_t* __restrict__ Qd, KvqView dense, KvqView sparse, const int32_t* __restrict__ src_idx,
     const int32_t* __restrict__ mix_len, float* __restrict__ part_o, float2* __restrict__ part_ml, int T_q, int n_q_heads,
     int n_kv_heads, int l_cap, int n_split, int n_rtile, int members, float c2, uint16_t* __restrict__ O, float* __restrict__ LSE) {
     using R = KvqRow<D, BITS>;
-    constexpr int ROWS = 32 * NW, TILE = kKeyTile * D, DB = D / 32;
+    constexpr int NW = kRowsWaves, TILE = kKeyTile * D, DB = D / 32;
     constexpr int BYTES = D * BITS / 8 / NW, CW = std::min(4, BYTES / 4), NC = BYTES / (4 * CW);       // of a thread: bytes of a key, words of a chunk, chunks
     constexpr int E = CW * 32 / BITS, SW = R::SCALES / 4;
     extern __shared__ __attribute__((aligned(16))) uint16_t stages[];             // [2][K tile, V tile]
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int g, split, b, row0;
-    if (!kvq_place(n_kv_heads, n_split, n_rtile, members, ROWS, &g, &split, &b, &row0)) return;
+    if (!kvq_place(n_kv_heads, n_split, n_rtile, members, kRowsTile, &g, &split, &b, &row0)) return;
     const int group = n_q_heads / n_kv_heads, all_rows = group * T_q;
     const int len = min(max(mix_len[b], 0), l_cap);
     // the split's tiles: an even share of the query's
@@ -704,11 +701,10 @@ __global__ __launch_bounds__(THREADS) void kvq_merge_kernel(const float* __restr
 // start, the tiles that a wave or workgroup walks, the partial rows, the merge.  More than one workgroup on a compute unit
 // shares its vector and matrix units, so that a tile takes longer, but not as much as there are workgroups; the third one pays
 // for a few rows only (one row of seven heads, D = 64, 98k keys x 8 queries: one 50.8, two and a bit 44.1, three 34.8).
-static KvqPlan kvq_splits(const vxl_attn_desc* d, int batch, long long rows, int l_cap, int blocks, int waves, float* us) {
+static KvqPlan kvq_splits(const vxl_attn_desc* d, int batch, long long rows, int l_cap, int blocks, float* us) {
     KvqPlan p{};
     p.blocks = blocks;
-    p.waves = waves;
-    const int wg_rows = blocks ? 16 * blocks : 32 * waves, wg_keys = blocks ? kKvqTile * kKvqWaves : kKeyTile;
+    const int wg_rows = blocks ? 16 * blocks : kRowsTile, wg_keys = blocks ? kKvqTile * kKvqWaves : kKeyTile;
     p.n_rtile = (rows + wg_rows - 1) / wg_rows;
     const long long units = (long long)batch * d->n_kv_heads;
     *us = INFINITY;
@@ -747,11 +743,11 @@ static KvqPlan kvq_splits(const vxl_attn_desc* d, int batch, long long rows, int
 KvqPlan kvq_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     const long long rows = (long long)(d->n_q_heads / d->n_kv_heads) * T;
     float us, us_many;
-    if (d->dtype != VXL_BF16 || rows <= 16) return kvq_splits(d, batch, rows, l_cap, 1, 0, &us);
-    const KvqPlan p = kvq_splits(d, batch, rows, l_cap, 2, 0, &us);
+    if (d->dtype != VXL_BF16 || rows <= 16) return kvq_splits(d, batch, rows, l_cap, 1, &us);
+    const KvqPlan p = kvq_splits(d, batch, rows, l_cap, 2, &us);
     if (rows <= 128) return p;
     // (us, blocks of 32 rows and of 256, 21.7k keys: 224 rows 24.3 and 30.4, 448 rows of 4 queries 118 and 102)
-    const KvqPlan many = kvq_splits(d, batch, rows, l_cap, 0, kRowsWaves, &us_many);
+    const KvqPlan many = kvq_splits(d, batch, rows, l_cap, 0, &us_many);
     return us_many < us ? many : p;
 }
 
@@ -790,11 +786,11 @@ vxl_status launch_kvq_decode(const KvqPlan& p, const vxl_attn_desc* d, float sca
                 constexpr int lds = 2 * 2 * kKeyTile * dim * 2;
                 static PerDeviceOnce attr;
                 st = attr.run([&] {
-                    VXL_HIP_TRY(hipFuncSetAttribute((const void*)kvq_rows_kernel<dim, bits, pooled, kRowsWaves>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+                    VXL_HIP_TRY(hipFuncSetAttribute((const void*)kvq_rows_kernel<dim, bits, pooled>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
                     return VXL_OK;
                 });
                 if (st != VXL_OK) return;
-                hipLaunchKernelGGL((kvq_rows_kernel<dim, bits, pooled, kRowsWaves>), grid, dim3(64 * kRowsWaves), lds, s, (const uint16_t*)Qd, view(c),
+                hipLaunchKernelGGL((kvq_rows_kernel<dim, bits, pooled>), grid, dim3(64 * kRowsWaves), lds, s, (const uint16_t*)Qd, view(c),
                                    view(sp), src_idx, mix_len, part_o, part_ml, T, d->n_q_heads, d->n_kv_heads, l_cap, p.n_split, n_rtile, members,
                                    scale * kLog2e, (uint16_t*)O, LSE);
             };

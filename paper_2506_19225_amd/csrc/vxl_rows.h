@@ -16,6 +16,17 @@ constexpr int kTableChunks = 2500;
 // In LDS: off[c] = first mixed row of chunk c, top bit: dense; (table) from[c] = its first token, or -1 - its first kept row.
 constexpr int kDenseChunk = INT32_MIN;
 
+// Bytes of mixed sets beyond which a gather stores them past the caches.
+constexpr long long kPastCaches = 160ll << 20;
+
+// 16 bytes that the caches need not keep (NT)
+template <bool NT>
+__device__ __forceinline__ void store16(uint4* p, uint4 v) {
+    typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+    if constexpr (NT) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
+    else *p = v;
+}
+
 // Fills off and from; the number of rows of the set.
 __device__ __forceinline__ int scan_mixed_rows(const uint8_t* mask, const int32_t* bounds, const int32_t* soff, int n_chunks,
                                                int n_prefix, int* off, int* from, bool table, int (&wave_tot)[4][4]) {
