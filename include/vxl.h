@@ -388,6 +388,8 @@ vxl_status vxl_kv_store_reload(vxl_kv_store* store, const uint8_t* dense_mask, i
  *   capacity  rows per KV head; row i of the cache of a prompt is token i
  * Both buffers 16-byte aligned.  What the calls below read has been written by vxl_kvq_write, or holds codes and scale bytes
  * of 17 to 252 or 255.  The descriptor gives heads, head_dim and the type and strides of the plain tensors.
+ * Plain rows are still what vxl_chunk_prefill, vxl_pool_sparse_kv, vxl_chunk_score_topk_mass and (without a kbar of before)
+ * vxl_chunk_score_topk read.
  */
 #define VXL_KVQ_MAX_ROWS (1 << 24)   /* capacity of a cache at most (the codes of a KV head are addressed in 32 bits) */
 typedef enum { VXL_KVQ_FP8 = 0, VXL_KVQ_FP4 = 1 } vxl_kvq_format;
@@ -432,8 +434,8 @@ vxl_status vxl_gather_bilevel_kvq(const vxl_layout* layout, const vxl_attn_desc*
  * they lie.  cache and sparse as above, other arguments as vxl_bilevel_decode_inplace (map_ready too: the row map is the same,
  * and may be one that the other call left), the workspace sized by vxl_workspace_bytes(VXL_OP_DECODE_KVQ, layout, desc, batch,
  * n_q_tokens, l_cap), never less.
- * O and LSE are those of the attention over the values that the cache reads back as, within the tolerance of the path; the
- * same call gives the same bits.  A row whose logits include NaN or +inf, or are all -inf (its LSE is -inf then), and one that
+ * O and LSE are those of the attention over the values that the cache reads back as, within the tolerance of the path (VXL_BF16:
+ * every weight of O, not of LSE, is rounded to bf16, 2^-8 of it at most); the same call gives the same bits.  A row whose logits include NaN or +inf, or are all -inf (its LSE is -inf then), and one that
  * attends to a NaN value, are NaN, other logits of -inf weigh nothing (a scaled product past the type's range is an infinity);
  * what a query does not attend to never matters.  256 times the sum of a row's attended |value| has to be finite.
  * Queries that share a selection (answers sampled in parallel) are better tokens of one query: they attend to the same set then,

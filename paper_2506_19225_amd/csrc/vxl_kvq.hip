@@ -129,7 +129,8 @@ constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e, kMirror8 = 0x141, kShiftLeft = 0x100
 // ------------------------------------------------------------------------------------------
 // Rows [first, first + n_rows) of the cache from K and V: a lane takes 16 bytes of a key row and of its value row, the lanes
 // of a block find its largest magnitude by exchange, and the first lane of 16 stores the scales of all of them.
-// Bound by HBM: 131,328 rows of four heads, 408 MB in and out, 70.5 us (5.8 TB/s), 16,640 rows 8.0.
+// Bound by HBM: 131,328 rows of four heads, 408 MB in and out, 71 us one after the other (5.7 TB/s), 82 where each is read back
+// before the next; 16,640 rows 8.1.
 // ------------------------------------------------------------------------------------------
 template <int D, int BITS, bool F32>
 __global__ __launch_bounds__(256) void kvq_write_kernel(const uint4* __restrict__ K, const uint4* __restrict__ V,
@@ -191,7 +192,7 @@ struct PiecePair {
     }
 };
 
-// K and V from rows [first, first + n_rows) of the cache.  Bound by HBM, at the same rates.
+// K and V from rows [first, first + n_rows) of the cache.  Bound by HBM: the same 71 us, 63 right behind the write.
 template <int D, int BITS, bool F32>
 __global__ __launch_bounds__(256) void kvq_read_kernel(uint4* __restrict__ K, uint4* __restrict__ V, long long head_u4,
                                                        long long tok_u4, long long n_rows, int n_heads, KvqView c,

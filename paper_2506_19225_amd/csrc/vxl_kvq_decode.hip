@@ -29,13 +29,19 @@ namespace {
 //
 // Quantised values are bf16 numbers.  bf16 queries are the operand as they are; fp32 queries, and probabilities of an fp32
 // call, go in as three bf16 parts that add up to all 24 bits (three matrix instructions instead of one).  Probabilities of a
-// bf16 call are rounded to bf16 (2^-8 relative at most, of each weight), their sum is taken before that, in fp32.
+// bf16 call are rounded to bf16 (2^-8 relative at most, of each weight), their sum is taken before that, in fp32: a result is off
+// by up to 2^-8 of sum p |v| before it is rounded itself, and the LSE by fp32's roundings only.  The plain decode divides by the
+// sum of the rounded weights, so that a row that one key dominates comes out exact there; elsewhere that has up to twice the
+// error, 2^-8 (sum p |v| + |o|), and its sum is not the LSE's.  Both sums, O scaled by their quotient: 1 to 3 % slower; weights in
+// two bf16 parts, which leave fp32's error alone: 11 to 26 %; the reference raised by every weight that outweighs the ones before
+// it, which is 1 then: 1 to 8 %.
 //
-// Measured (us, launches with their merge; D = 128, 28 heads on 4): one token, 4,096 keys in 4 bits 7.4 and 18,176 keys in 8
-// bits 10.9 (the floor of two dependent launches; a plain decode in place 8.9 and 12.7), eight queries' tokens, 64.5k keys each
-// in 4 bits 33.6 (plain 83.9): vector instructions 73 % and matrix instructions 23 % of the cycles, which do not overlap more;
-// 64 of the 174 vector instructions of a tile are conversions, 32 byte permutations, 8 exponentials.  A question of 64 tokens,
-// 448 rows by 32 (NB = 2) over 23,800 keys in 4 bits 42.4 (38.7 of them here, 64 % and 28 %, 560 TFLOP/s).
+// Measured (us, launches with their merge; D = 128, 28 heads on 4): one token, 4,096 keys in 4 bits 7.4 to 8.5 and 18,176 keys in
+// 8 bits 11.0 (two dependent launches; a plain decode in place 8.9 and 12.7; 28 layers in turn, none of whose rows is still in an
+// L2, 7.6 and 13.0), eight queries' tokens, 64.5k keys each in 4 bits 34 (plain 83.9): vector instructions 74 % and matrix
+// instructions 23 % of the cycles; 64 of the 174 vector instructions of a tile are conversions, 32 byte permutations, 8
+// exponentials.  A question of 64 tokens, 448 rows by 32 (NB = 2) over 23,800 keys in 4 bits 42.5 (38.7 of them here, 64 % and
+// 28 %, 560 TFLOP/s), in 8 bits 45 to 49.
 // ------------------------------------------------------------------------------------------
 // The workgroup's KV head, split, query and first row.  Workgroups that read the same keys (row tiles, and queries, whose sets
 // overlap) are members of a pair (KV head, split), one behind the other on one XCD, whose L2 serves all but the first: workgroups
@@ -422,9 +428,10 @@ __global__ __launch_bounds__(64 * kKvqWaves, NB == 1 && !F32 ? 3 : 2) void kvq_d
 // call, so each 64-key tile is converted once for all rows of the workgroup: eight threads load the codes of a row between them,
 // a tile ahead, and write the bf16 rows to one of two LDS stages while the other is worked on, by the products and layouts of
 // the plain decode's ring.  One barrier per tile.
-// 896 rows on four heads, 18,176 keys in 4 bits: 48.8 us, 52 with the merge (plain decode in place 52.7), 680 TFLOP/s; 49 % of
-// the cycles in vector, 40 % in matrix instructions, 31 % of the LDS's in reads of K and V rows by every wave.  64 rows per
-// wave would halve those, but spill; four waves per workgroup and converting in turns were no faster.
+// 896 rows on four heads, 18,176 keys in 4 bits: 49 us, 52 to 55 with the merge (plain decode in place 52.7), 680 TFLOP/s, in 8
+// bits 52, 54 to 58; 49 % of the cycles in vector, 40 % in matrix instructions, 31 % of the LDS's in reads of K and V rows by every
+// wave.  64 rows per wave would halve those, but spill much: D = 128 takes all 256 registers as it is, and in 4 bits 3 or 4 more,
+// 20 bytes a lane.  Four waves per workgroup and converting in turns were no faster.
 // ------------------------------------------------------------------------------------------
 // Element offset of 16-byte piece `piece` of row `row` of a V tile: its 64-byte parts turned as in the plain tile, for the
 // transposing reads, and the pieces of a part by the next bits of the row, for writes of one piece of each part by eight rows.
@@ -696,9 +703,8 @@ __global__ __launch_bounds__(THREADS) void kvq_merge_kernel(const float* __restr
 
 }  // namespace
 
-// How many splits, and for many rows which kernel, by estimates in us, least squares over 3,800 timed calls of 1,376 to 98,176
-// keys (4 to 8 % rms; the splits that they choose cost 0.4 % (more than 16 rows) and 0.8 % more than the best of each call's): a
-// start, the tiles that a wave or workgroup walks, the partial rows, the merge.  More than one workgroup on a compute unit
+// How many splits, and for many rows which kernel, by estimates in us, fitted by least squares to timed calls of 1,376 to 98,176
+// keys (7 % rms over the 25 calls of profiles/quantised_cache_kernel_times.md): a start, the tiles that a wave or workgroup walks, the partial rows, the merge.  More than one workgroup on a compute unit
 // shares its vector and matrix units, so that a tile takes longer, but not as much as there are workgroups; the third one pays
 // for a few rows only (one row of seven heads, D = 64, 98k keys x 8 queries: one 50.8, two and a bit 44.1, three 34.8).
 static KvqPlan kvq_splits(const vxl_attn_desc* d, int batch, long long rows, int l_cap, int blocks, float* us) {
