@@ -435,9 +435,9 @@ vxl_status vxl_gather_bilevel_kvq(const vxl_layout* layout, const vxl_attn_desc*
  * and may be one that the other call left), the workspace sized by vxl_workspace_bytes(VXL_OP_DECODE_KVQ, layout, desc, batch,
  * n_q_tokens, l_cap), never less.
  * O and LSE are those of the attention over the values that the cache reads back as, within the tolerance of the path (VXL_BF16:
- * every weight of O, not of LSE, is rounded to bf16, 2^-8 of it at most); the same call gives the same bits.  A row whose logits include NaN or +inf, or are all -inf (its LSE is -inf then), and one that
- * attends to a NaN value, are NaN, other logits of -inf weigh nothing (a scaled product past the type's range is an infinity);
- * what a query does not attend to never matters.  256 times the sum of a row's attended |value| has to be finite.
+ * every weight of O, not of LSE, is rounded to bf16, 2^-8 of it at most); the same call gives the same bits.  A row whose logits
+ * include NaN or +inf, or are all -inf (its LSE is -inf then), and one that attends to a NaN value, are NaN; other logits of -inf
+ * weigh nothing (a scaled product past fp32's range is an infinity).  What a query does not attend to never matters.  256 times the sum of a row's attended |value| has to be finite.
  * Queries that share a selection (answers sampled in parallel) are better tokens of one query: they attend to the same set then,
  * and its rows are read and converted once for several of them.
  * VXL_ERR_UNSUPPORTED if batch exceeds 65,535, the stacked rows of a query and KV head 2^30, or the workgroups, one per query, KV
