@@ -706,7 +706,8 @@ __global__ __launch_bounds__(THREADS) void kvq_merge_kernel(const float* __restr
 // How many splits, and for many rows which kernel, by estimates in us, fitted by least squares to timed calls of 1,376 to 98,176
 // keys (7 % rms over the 25 calls of profiles/quantised_cache_kernel_times.md): a start, the tiles that a wave or workgroup
 // walks, the partial rows, the merge.  More than one workgroup on a compute unit shares its vector and matrix units, so that a
-// tile takes longer, but not as much as there are workgroups; the third one pays for a few rows only (one row of seven heads, D = 64, 98k keys x 8 queries: one 50.8, two and a bit 44.1, three 34.8).
+// tile takes longer, but not as much as there are workgroups; the third one pays for a few rows only (one row of seven heads,
+// D = 64, 98k keys x 8 queries: one 50.8, two and a bit 44.1, three 34.8).
 static KvqPlan kvq_splits(const vxl_attn_desc* d, int batch, long long rows, int l_cap, int blocks, float* us) {
     KvqPlan p{};
     p.blocks = blocks;
