@@ -9,6 +9,8 @@
  *   vxl_gather_bilevel_kv  "Bi-level KVs Decoding": selective reload + concatenation
  *   vxl_bilevel_decode     "Bi-level KVs Decoding": generation over the mixed KV set
  *   vxl_kvq_* and *_kvq    the same cache in 8 or 4 bits: written, read back, gathered from, attended to in place
+ *   vxl_rotate, vxl_mixed_* rotary positions; mixed KV sets that generated tokens are put behind, attended to by position,
+ *                          and cut back to the rows that received the most attention
  *
  * Conventions
  *   - Every tensor pointer is a DEVICE pointer owned by the caller; the layout arrays given to
@@ -64,7 +66,9 @@ typedef enum {
     VXL_OP_DECODE = 3,
     VXL_OP_SCORE_MASS = 4,
     VXL_OP_DECODE_INPLACE = 5,
-    VXL_OP_DECODE_KVQ = 6
+    VXL_OP_DECODE_KVQ = 6,
+    VXL_OP_MIXED_ATTEND = 7,
+    VXL_OP_MIXED_EVICT = 8
 } vxl_op;
 
 /*
@@ -129,10 +133,9 @@ vxl_status vxl_layout_destroy(vxl_layout* layout);
 
 /* Bytes of workspace the given hot call needs (0 on invalid arguments, and for VXL_OP_GATHER,
  * which needs none).  batch, n_q_tokens and l_cap are read by the ops that take them (SCORE_TOPK:
- * batch; SCORE_MASS: batch, n_q_tokens; the DECODEs: batch, n_q_tokens, l_cap).  The decode call is
- * sized by the capacity of the mixed buffers it will be given, l_cap, and not by the number k of
- * dense chunks, because it takes no layout: l_cap = vxl_mixed_kv_capacity(layout, k) for the
- * caller's k, or anything larger.  layout may be NULL for VXL_OP_DECODE. */
+ * batch; SCORE_MASS: batch, n_q_tokens; the DECODEs and MIXED_ATTEND: batch, n_q_tokens, l_cap; MIXED_EVICT: batch, l_cap).  The
+ * decode call is sized by the capacity of the mixed buffers it will be given, l_cap, and not by the number k of dense chunks, because it takes no layout: l_cap = vxl_mixed_kv_capacity(layout, k) for the
+ * caller's k, or anything larger.  layout may be NULL for VXL_OP_DECODE and is not read for the VXL_OP_MIXED ones. */
 size_t vxl_workspace_bytes(vxl_op op, const vxl_layout* layout, const vxl_attn_desc* desc,
                            int32_t batch, int32_t n_q_tokens, int32_t l_cap);
 
@@ -448,6 +451,119 @@ vxl_status vxl_bilevel_decode_kvq(const vxl_layout* layout, const vxl_attn_desc*
                                   int32_t n_q_tokens, const vxl_kvq_cache* cache, const vxl_kvq_cache* sparse,
                                   const uint8_t* dense_mask, int32_t l_cap, int32_t map_ready, void* O, float* LSE,
                                   int32_t* mix_len, void* workspace, size_t workspace_bytes, vxl_stream stream);
+
+/*
+ * Rotary positions.  Of the first rotary_dim elements of a row, pairs (a, b) are turned by an angle that grows with the
+ * token's position p: of pair i, (a cos t - b sin t, a sin t + b cos t) * magnitude with t = p * freqs[i]; the elements
+ * behind rotary_dim are copied.
+ *   freqs       device double [rotary_dim / 2], radians per position: any base, stretched for long prompts as the model wants
+ *               it.  t is computed and reduced in 64 bits, its sine and cosine in 32
+ *   rotary_dim  even, 2 to head_dim
+ *   interleaved 0: pair i is elements i and i + rotary_dim / 2; != 0: elements 2 i and 2 i + 1
+ *   magnitude   finite
+ *   transpose   != 0: turned by -t.  With the same magnitude this is the transpose of the map, which takes the gradient of its
+ *               result to the gradient of its argument; with 1 / magnitude it is the inverse
+ */
+typedef struct {
+    const double* freqs;
+    int32_t rotary_dim;
+    int32_t interleaved;
+    float magnitude;
+    int32_t transpose;
+} vxl_rotary;
+
+/*
+ * Rotates the queries and keys of a prompt.
+ *   Q, K, Q_out, K_out  device, layouts of the descriptor (Q_out as Q, K_out as K); a tensor may be rotated in place (Q_out ==
+ *                       Q, K_out == K); K and K_out may both be NULL
+ *   positions           device int32 [n_tokens], any values
+ * n_tokens == 0 does nothing.  No workspace.  Errors: VXL_ERR_INVALID_ARG (null or misaligned buffers, a malformed rotary,
+ * outputs that meet each other or an input in any other way), VXL_ERR_UNSUPPORTED, VXL_ERR_HIP.
+ */
+vxl_status vxl_rotate(const vxl_attn_desc* desc, const vxl_rotary* rotary, const int32_t* positions, int32_t n_tokens,
+                      const void* Q, const void* K, void* Q_out, void* K_out, vxl_stream stream);
+
+/*
+ * Puts n_new tokens of every query of a batch behind the rows of its mixed set: their queries and keys are rotated, the keys and
+ * values become rows mix_len[b] - n_new .. mix_len[b] - 1.
+ *   Q, K, V     device, batch * n_new tokens (those of query 0 first) in the layouts of the descriptor, as a projection writes them
+ *   positions   device int32 [batch, n_new]
+ *   Qd          device [batch, n_new, n_q_heads, head_dim] (written; may be Q itself where Q is dense and token-major)
+ *   Kmix, Vmix  device [batch, n_kv_heads, l_cap, head_dim]; other rows are left as they are
+ *   mix_len     device int32 [batch], rows with the new ones; a token whose row would lie outside [0, l_cap) is not stored
+ *   row_pos     device int32 [batch, n_kv_heads, l_cap] or NULL: positions of the rows (written for the new ones)
+ *   row_weight  device float [batch, n_kv_heads, l_cap] or NULL: attention weights of the rows (0 for the new ones)
+ *   rotary      NULL: queries and keys are copied as they are
+ * No workspace.  Errors: VXL_ERR_INVALID_ARG (null or misaligned buffers, a malformed rotary, outputs that overlap each other or
+ * an input), VXL_ERR_UNSUPPORTED, VXL_ERR_HIP.
+ */
+vxl_status vxl_mixed_append(const vxl_attn_desc* desc, const vxl_rotary* rotary, const int32_t* positions, int32_t batch,
+                            int32_t n_new, const void* Q, const void* K, const void* V, void* Qd, void* Kmix, void* Vmix,
+                            int32_t l_cap, const int32_t* mix_len, int32_t* row_pos, float* row_weight, vxl_stream stream);
+
+/*
+ * Which rows of a mixed set a query token sees and what its logits are.  With s = softmax_scale * q.k, a row of position pk and a
+ * token of position pq:
+ *   logit    x = softcap > 0 ? softcap * tanh(s / softcap) : s;  with slopes: minus slopes[h] * |pq - pk|
+ *   visible  pq >= 0 and pk >= 0 and (pk < n_always or ((not causal or pk <= pq) and (window == 0 or pq - pk < window)))
+ * A negative position marks a padding token or an empty row.
+ *   softcap  >= 0, finite;  window, n_always >= 0;  slopes device float [n_q_heads], or NULL
+ * A NULL rule: s as it is, no causal or window rule.
+ */
+typedef struct {
+    float softcap;
+    int32_t causal;
+    int32_t window;
+    int32_t n_always;
+    const float* slopes;
+} vxl_score_rule;
+
+/*
+ * vxl_bilevel_decode with a rule, by position, and with the attention weight that every row receives:
+ *   O, LSE          over the visible rows r < mix_len[b] of the token's set; a token that sees no row, or whose logits are all -inf,
+ *                   has O = 0 and LSE = -inf and weighs nothing
+ *   weight_out      device float [batch, n_kv_heads, l_cap] or NULL: weight + sum over the query tokens and over the query heads of the KV
+ *                   head of the probabilities of the row (fp32, in an order that depends on the sizes alone); rows >= mix_len[b] are
+ *                   left as they are
+ *   weight          device float, the same shape: what the rows have received before (may be weight_out itself), or NULL: 0
+ *   q_pos, row_pos  device int32 [batch, n_q_tokens] and [batch, n_kv_heads, l_cap], positions of the tokens and of the rows.  Both may
+ *                   be NULL where the rule needs none: every row of the set is visible then
+ *   mix_len         as vxl_bilevel_decode
+ *   workspace       sized by vxl_workspace_bytes(VXL_OP_MIXED_ATTEND, NULL, desc, batch, n_q_tokens, l_cap), never less
+ * Other arguments as vxl_bilevel_decode.  Results are those of the formulas within the tolerance of the path (VXL_BF16: every weight of O
+ * is rounded to bf16, 2^-8 of it at most, LSE and weight_out have fp32's errors); the same call gives the same bits.  A token
+ * with a visible logit of NaN or +inf has no softmax: its O and LSE are NaN, and so is the weight of the rows that it sees.  What a token
+ * does not see never matters to it, whatever its rows hold.
+ * Errors: VXL_ERR_INVALID_ARG (also one of q_pos and row_pos without the other, a rule that needs positions without them, outputs
+ * or a workspace that overlap each other or an input), VXL_ERR_UNSUPPORTED (also batch * n_kv_heads > 65,535, 2^30 stacked
+ * rows of a query and KV head), VXL_ERR_WORKSPACE, VXL_ERR_HIP.
+ */
+vxl_status vxl_mixed_attend(const vxl_attn_desc* desc, const vxl_score_rule* rule, const void* Qd, const int32_t* q_pos, int32_t batch,
+                            int32_t n_q_tokens, const void* Kmix, const void* Vmix, int32_t l_cap, const int32_t* mix_len,
+                            const int32_t* row_pos, void* O, float* LSE, const float* weight, float* weight_out, void* workspace,
+                            size_t workspace_bytes, vxl_stream stream);
+
+/*
+ * Cuts every mixed set of a batch back to its n = min(mix_len[b], keep) rows of the largest weight.  Every KV head keeps rows of
+ * its own, in this order of preference:
+ *   rows of a position below n_first (a prompt's first tokens) or with newest[b] - position < n_recent (the latest), all alike;
+ *   then by weight, the largest first (+inf before all numbers, -0 as 0, NaN behind -inf);  then empty rows (a negative position)
+ * and of equal rows the lower one.  Kept rows below n stay in their place; those above take the places of the dropped ones below, in
+ * order.  (The order of rows has no meaning: their positions go with them.)
+ *   Kmix, Vmix, weight, row_pos   device, the sets: [batch, n_kv_heads, l_cap, head_dim], float and int32 [batch, n_kv_heads, l_cap]
+ *   newest                        device int32 [batch], or NULL where n_recent == 0
+ *   Kout, Vout, weight_out, pos_out  device, the same with out_cap rows, out_cap >= min(keep, l_cap); rows >= n are left as they are.
+ *                                 All four may be the inputs themselves (out_cap == l_cap): then only the rows that change place move
+ *   kept                          device int32 [batch] (written: n, 0 for lengths <= 0), may be mix_len
+ *   workspace                     sized by vxl_workspace_bytes(VXL_OP_MIXED_EVICT, NULL, desc, batch, 0, l_cap)
+ * keep >= 0, n_first >= 0, n_recent >= 0.
+ * Errors: VXL_ERR_INVALID_ARG (null or misaligned buffers, outputs that overlap each other or an input in any other way),
+ * VXL_ERR_UNSUPPORTED (batch * n_kv_heads > 65,535), VXL_ERR_WORKSPACE, VXL_ERR_HIP.
+ */
+vxl_status vxl_mixed_evict(const vxl_attn_desc* desc, const void* Kmix, const void* Vmix, int32_t l_cap, const int32_t* mix_len,
+                           const float* weight, const int32_t* row_pos, const int32_t* newest, int32_t batch, int32_t keep,
+                           int32_t n_first, int32_t n_recent, void* Kout, void* Vout, int32_t out_cap, float* weight_out,
+                           int32_t* pos_out, int32_t* kept, void* workspace, size_t workspace_bytes, vxl_stream stream);
 
 const char* vxl_status_string(vxl_status s);
 const char* vxl_last_error(void);   /* text of the last failing HIP call on this thread */

@@ -26,10 +26,12 @@ from .prefill import prefill_def, prefill_blk
 from .bilevel import (chunk_scores, chunk_scores_mass, select_topk, gather_bilevel, decode_mixed, decode_lse,
                       pool_groups, pool_sparse_kv, gather_bilevel_pooled)
 from .kvq import kvq_numbers, kvq_quantise, kvq_values
+from .mixed import rotate, visible, attend_mixed, evict_rows
 
 __all__ = [
     "allowed_mask", "allowed_keys", "allowed_pair_count", "mixed_source_index",
     "prefill_def", "prefill_blk",
     "chunk_scores", "chunk_scores_mass", "select_topk", "gather_bilevel", "decode_mixed", "decode_lse",
     "pool_groups", "pool_sparse_kv", "gather_bilevel_pooled", "kvq_numbers", "kvq_quantise", "kvq_values",
+    "rotate", "visible", "attend_mixed", "evict_rows",
 ]

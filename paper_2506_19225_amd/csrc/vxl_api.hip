@@ -10,6 +10,7 @@
 #include <numeric>
 
 #include "vxl_kvq.h"
+#include "vxl_mixed.h"
 
 namespace vxl {
 
@@ -465,6 +466,12 @@ size_t vxl_workspace_bytes(vxl_op op, const vxl_layout* L, const vxl_attn_desc* 
         case VXL_OP_DECODE_KVQ:
             if (batch <= 0 || n_q_tokens <= 0 || l_cap <= 0) return 0;
             return inplace_workspace(batch, l_cap, kvq_plan(d, batch, n_q_tokens, l_cap).total).total;
+        case VXL_OP_MIXED_ATTEND:
+            if (batch <= 0 || n_q_tokens <= 0 || l_cap <= 0) return 0;
+            return mixed_plan(d, batch, n_q_tokens, l_cap).total;
+        case VXL_OP_MIXED_EVICT:
+            if (batch <= 0 || l_cap <= 0) return 0;
+            return evict_plan(d, batch, l_cap).total;
     }
     return 0;
 }
@@ -693,11 +700,12 @@ static bool steps_into(__int128 first, __int128 step, long long n, __int128 lo, 
 struct PlainRows {
     __int128 at, head, tok;
     long long heads, n, bytes;
-    PlainRows(const vxl_attn_desc* d, const void* p, int n_rows) : at((uintptr_t)p), heads(d->n_kv_heads), n(n_rows) {
+    PlainRows(const vxl_attn_desc* d, const void* p, int n_rows, bool queries = false)
+        : at((uintptr_t)p), heads(queries ? d->n_q_heads : d->n_kv_heads), n(n_rows) {
         const TokStrides ts = tok_strides(d, n_rows);
         const size_t e = elem_bytes(d);
-        head = (__int128)ts.kh * e;
-        tok = (__int128)ts.kt * e;
+        head = (__int128)(queries ? ts.qh : ts.kh) * e;
+        tok = (__int128)(queries ? ts.qt : ts.kt) * e;
         bytes = d->head_dim * e;
     }
     __int128 span() const { return (heads - 1) * head + (n - 1) * tok + bytes; }
@@ -709,11 +717,19 @@ struct PlainRows {
             if (steps_into(at + g * head, tok, n, lo - bytes, hi)) return true;
         return false;
     }
-    // Whether one of the rows meets one of the same many, as far apart, from another address on.
+    // Whether one of the rows meets one of the same number of tokens (where these are not as far apart, or the heads very many:
+    // whether the memory from first to last does).
     bool meet(const PlainRows& o) const {
-        if (o.at + span() <= at || at + span() <= o.at) return false;
-        for (long long g = 1 - heads; g < heads; ++g)
-            if (steps_into(o.at - at + g * head - (n - 1) * tok, tok, 2 * n - 1, -bytes, bytes)) return true;
+        if (o.at + o.span() <= at || at + span() <= o.at) return false;
+        if (o.tok != tok || (__int128)heads * o.heads > 1 << 20) return true;
+        if (heads == o.heads && head == o.head) {
+            for (long long g = 1 - heads; g < heads; ++g)
+                if (steps_into(o.at - at + g * head - (n - 1) * tok, tok, 2 * n - 1, -bytes, bytes)) return true;
+            return false;
+        }
+        for (long long g = 0; g < heads; ++g)
+            for (long long h = 0; h < o.heads; ++h)
+                if (steps_into(o.at + h * o.head - at - g * head - (n - 1) * tok, tok, 2 * n - 1, -bytes, bytes)) return true;
         return false;
     }
 };
@@ -814,6 +830,137 @@ vxl_status vxl_bilevel_decode_kvq(const vxl_layout* L, const vxl_attn_desc* d, c
     }
     return launch_kvq_decode(p, d, resolve_scale(d), Qd, batch, n_q_tokens, cache, sp, src_idx, l_cap, len, O, LSE,
                              (char*)workspace + w.partials, s);
+}
+
+static bool rotary_ok(const vxl_attn_desc* d, const vxl_rotary* r) {
+    return r && r->freqs && (reinterpret_cast<uintptr_t>(r->freqs) & 7u) == 0 && r->rotary_dim >= 2 && r->rotary_dim <= d->head_dim &&
+           r->rotary_dim % 2 == 0 && std::isfinite(r->magnitude);
+}
+
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+vxl_status vxl_rotate(const vxl_attn_desc* d, const vxl_rotary* r, const int32_t* positions, int32_t n_tokens, const void* Q, const void* K,
+                      void* Q_out, void* K_out, vxl_stream stream) {
+    vxl_status st;
+    if (!desc_ok(d, &st)) return st;
+    if (!rotary_ok(d, r) || n_tokens < 0) return VXL_ERR_INVALID_ARG;
+    if (n_tokens == 0) return VXL_OK;
+    if (!positions || !aligned4(positions) || !Q || !Q_out || !K != !K_out) return VXL_ERR_INVALID_ARG;
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(Q_out) || !aligned16(K_out)) return VXL_ERR_INVALID_ARG;
+    const PlainRows q(d, Q, n_tokens, true), qo(d, Q_out, n_tokens, true);
+    const Range small[] = {range(positions, n_tokens * sizeof(int32_t)), range(r->freqs, r->rotary_dim / 2 * sizeof(double))};
+    for (const Range& in : small)
+        if (qo.meet(in)) return VXL_ERR_INVALID_ARG;
+    if (Q_out != Q && qo.meet(q)) return VXL_ERR_INVALID_ARG;
+    if (K) {
+        const PlainRows k(d, K, n_tokens), ko(d, K_out, n_tokens);
+        for (const Range& in : small)
+            if (ko.meet(in)) return VXL_ERR_INVALID_ARG;
+        if ((K_out != K && ko.meet(k)) || qo.meet(k) || ko.meet(q) || qo.meet(ko)) return VXL_ERR_INVALID_ARG;
+    }
+    return launch_rotate(d, r, positions, n_tokens, Q, K, Q_out, K_out, (hipStream_t)stream);
+}
+
+// Bytes of the tensors of a mixed set of a batch, and of its rows' numbers.
+static size_t mixed_bytes(const vxl_attn_desc* d, int32_t batch, int32_t rows) {
+    return (size_t)batch * d->n_kv_heads * rows * d->head_dim * elem_bytes(d);
+}
+static size_t row_bytes(const vxl_attn_desc* d, int32_t batch, int32_t rows) { return (size_t)batch * d->n_kv_heads * rows * sizeof(float); }
+
+// Whether the sizes of a call on mixed sets are ones that its kernels count: a batch and its KV heads in a grid's second dimension, its
+// tokens and query rows in 32 bits, its elements far below 64.
+static bool mixed_sizes_ok(const vxl_attn_desc* d, int32_t batch, int32_t tokens) {
+    return (long long)batch * d->n_kv_heads <= 65535 && (long long)batch * tokens <= INT32_MAX &&
+           (long long)(d->n_q_heads / d->n_kv_heads) * tokens <= 1 << 30;
+}
+
+vxl_status vxl_mixed_append(const vxl_attn_desc* d, const vxl_rotary* r, const int32_t* positions, int32_t batch, int32_t n_new, const void* Q,
+                            const void* K, const void* V, void* Qd, void* Kmix, void* Vmix, int32_t l_cap, const int32_t* mix_len,
+                            int32_t* row_pos, float* row_weight, vxl_stream stream) {
+    vxl_status st;
+    if (!desc_ok(d, &st)) return st;
+    if ((r && !rotary_ok(d, r)) || !positions || batch <= 0 || n_new <= 0 || l_cap <= 0 || !mix_len) return VXL_ERR_INVALID_ARG;
+    for (const void* p : {Q, K, V, (const void*)Qd, (const void*)Kmix, (const void*)Vmix})
+        if (!p || !aligned16(p)) return VXL_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)positions, (const void*)mix_len, (const void*)row_pos, (const void*)row_weight})
+        if (!aligned4(p)) return VXL_ERR_INVALID_ARG;
+    if (!mixed_sizes_ok(d, batch, n_new)) return VXL_ERR_UNSUPPORTED;
+    const int n = batch * n_new;
+    const size_t set = mixed_bytes(d, batch, l_cap), rows = row_bytes(d, batch, l_cap);
+    const Range out[] = {range(Qd, (size_t)n * d->n_q_heads * d->head_dim * elem_bytes(d)), range(Kmix, set), range(Vmix, set),
+                         range(row_pos, rows), range(row_weight, rows)};
+    if (outputs_meet({out[0], out[1], out[2], out[3], out[4]},
+                     {range(positions, n * sizeof(int32_t)), range(mix_len, batch * sizeof(int32_t)),
+                      r ? range(r->freqs, r->rotary_dim / 2 * sizeof(double)) : Range{}}))
+        return VXL_ERR_INVALID_ARG;
+    const PlainRows in[] = {{d, Q, n, true}, {d, K, n}, {d, V, n}};
+    const bool own_place = Qd == Q && in[0].head == in[0].bytes && in[0].tok == in[0].bytes * d->n_q_heads;
+    for (const Range& o : out)
+        for (const PlainRows& x : in)
+            if (!(own_place && &o == out && &x == in) && x.meet(o)) return VXL_ERR_INVALID_ARG;
+    return launch_mixed_append(d, r, positions, batch, n_new, Q, K, V, Qd, Kmix, Vmix, l_cap, mix_len, row_pos, row_weight, (hipStream_t)stream);
+}
+
+vxl_status vxl_mixed_attend(const vxl_attn_desc* d, const vxl_score_rule* rule, const void* Qd, const int32_t* q_pos, int32_t batch,
+                            int32_t n_q_tokens, const void* Kmix, const void* Vmix, int32_t l_cap, const int32_t* mix_len, const int32_t* row_pos,
+                            void* O, float* LSE, const float* weight, float* weight_out, void* workspace, size_t workspace_bytes,
+                            vxl_stream stream) {
+    vxl_status st;
+    if (!desc_ok(d, &st)) return st;
+    if (batch <= 0 || n_q_tokens <= 0 || l_cap <= 0 || !mix_len || (weight && !weight_out) || !q_pos != !row_pos) return VXL_ERR_INVALID_ARG;
+    for (const void* p : {Qd, Kmix, Vmix, (const void*)O})
+        if (!p || !aligned16(p)) return VXL_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)q_pos, (const void*)mix_len, (const void*)row_pos, (const void*)LSE, (const void*)weight, (const void*)weight_out})
+        if (!aligned4(p)) return VXL_ERR_INVALID_ARG;
+    const float scale = resolve_scale(d);
+    if (rule) {
+        if (!(rule->softcap >= 0.f) || !std::isfinite(rule->softcap) || rule->window < 0 || rule->n_always < 0 || !aligned4(rule->slopes))
+            return VXL_ERR_INVALID_ARG;
+        if (rule->softcap > 0.f && !std::isfinite(scale / rule->softcap)) return VXL_ERR_INVALID_ARG;
+        if ((rule->causal || rule->window || rule->slopes) && !q_pos) return VXL_ERR_INVALID_ARG;
+    }
+    if (!mixed_sizes_ok(d, batch, n_q_tokens)) return VXL_ERR_UNSUPPORTED;
+    const MixedPlan p = mixed_plan(d, batch, n_q_tokens, l_cap);
+    if (!workspace || workspace_bytes < p.total || !aligned16(workspace)) return VXL_ERR_WORKSPACE;
+    const size_t q_rows = (size_t)batch * n_q_tokens * d->n_q_heads, q_bytes = q_rows * d->head_dim * elem_bytes(d);
+    const size_t set = mixed_bytes(d, batch, l_cap), rows = row_bytes(d, batch, l_cap);
+    if (outputs_meet({range(O, q_bytes), range(LSE, q_rows * sizeof(float)), range(weight_out, rows), range(workspace, p.total)},
+                     {range(Qd, q_bytes), range(Kmix, set), range(Vmix, set), range(mix_len, batch * sizeof(int32_t)), range(row_pos, rows),
+                      range(q_pos, (size_t)batch * n_q_tokens * sizeof(int32_t)), weight == weight_out ? Range{} : range(weight, rows),
+                      rule ? range(rule->slopes, d->n_q_heads * sizeof(float)) : Range{}}))
+        return VXL_ERR_INVALID_ARG;
+    const MixedCall c{d, rule, scale, Qd, q_pos, batch, n_q_tokens, Kmix, Vmix, l_cap, mix_len, row_pos, O, LSE, weight, weight_out, (char*)workspace};
+    return launch_mixed_attend(p, c, g_force_simple != 0, (hipStream_t)stream);
+}
+
+vxl_status vxl_mixed_evict(const vxl_attn_desc* d, const void* Kmix, const void* Vmix, int32_t l_cap, const int32_t* mix_len, const float* weight,
+                           const int32_t* row_pos, const int32_t* newest, int32_t batch, int32_t keep, int32_t n_first, int32_t n_recent,
+                           void* Kout, void* Vout, int32_t out_cap, float* weight_out, int32_t* pos_out, int32_t* kept, void* workspace,
+                           size_t workspace_bytes, vxl_stream stream) {
+    vxl_status st;
+    if (!desc_ok(d, &st)) return st;
+    if (batch <= 0 || l_cap <= 0 || keep < 0 || n_first < 0 || n_recent < 0 || out_cap <= 0 || out_cap < std::min(keep, l_cap)) return VXL_ERR_INVALID_ARG;
+    for (const void* p : {Kmix, Vmix, (const void*)Kout, (const void*)Vout})
+        if (!p || !aligned16(p)) return VXL_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)mix_len, (const void*)weight, (const void*)row_pos, (const void*)weight_out, (const void*)pos_out, (const void*)kept})
+        if (!p || !aligned4(p)) return VXL_ERR_INVALID_ARG;
+    if ((n_recent > 0 && !newest) || !aligned4(newest)) return VXL_ERR_INVALID_ARG;
+    if (!mixed_sizes_ok(d, batch, 1)) return VXL_ERR_UNSUPPORTED;
+    const EvictPlan p = evict_plan(d, batch, l_cap);
+    if (!workspace || workspace_bytes < p.total || !aligned16(workspace)) return VXL_ERR_WORKSPACE;
+    const bool in_place = Kout == Kmix;
+    if (in_place && (Vout != Vmix || weight_out != weight || pos_out != row_pos || out_cap != l_cap)) return VXL_ERR_INVALID_ARG;
+    const size_t set = mixed_bytes(d, batch, l_cap), rows = row_bytes(d, batch, l_cap);
+    const size_t set_out = mixed_bytes(d, batch, out_cap), rows_out = row_bytes(d, batch, out_cap), lens = batch * sizeof(int32_t);
+    const Range lengths = kept == mix_len ? Range{} : range(mix_len, lens);
+    const std::initializer_list<Range> out = {range(Kout, set_out), range(Vout, set_out), range(weight_out, rows_out), range(pos_out, rows_out),
+                                              range(kept, lens), range(workspace, p.total)};
+    if (in_place ? outputs_meet(out, {lengths, range(newest, lens)})
+                 : outputs_meet(out, {lengths, range(newest, lens), range(Kmix, set), range(Vmix, set), range(weight, rows), range(row_pos, rows)}))
+        return VXL_ERR_INVALID_ARG;
+    const EvictCall c{d, Kmix, Vmix, l_cap, mix_len, weight, row_pos, newest, batch, keep, n_first, n_recent, Kout, Vout, out_cap, weight_out, pos_out,
+                      kept, (char*)workspace};
+    return launch_mixed_evict(p, c, (hipStream_t)stream);
 }
 
 vxl_status vxl_bilevel_decode_static(const vxl_attn_desc* d, const void* Qd, int32_t batch,

@@ -13,6 +13,7 @@
 
 #include <algorithm>
 #include <exception>
+#include <initializer_list>
 
 #include "vxl.h"
 
@@ -23,12 +24,14 @@ namespace {
 #define VXL_PATH(X)                                                                                               \
     X(chunk_prefill) X(chunk_score_topk) X(chunk_score_topk_mass) X(gather_bilevel_kv) X(pool_sparse_kv)          \
     X(gather_bilevel_kv_pooled) X(bilevel_decode) X(bilevel_decode_inplace) X(kvq_write) X(kvq_read)              \
-    X(gather_bilevel_kvq) X(bilevel_decode_kvq)
+    X(gather_bilevel_kvq) X(bilevel_decode_kvq) X(rotate) X(mixed_append) X(mixed_attend) X(mixed_evict)
 
 // Of one module object: a vxl.py that is loaded twice has two.
 struct State {
     PyObject *desc_type, *handle_type, *stream_of, *cache_type;
     PyObject *rows, *scales, *format;                         // names of a cache's attributes
+    PyObject *rotary_type, *rule_type, *device_of;
+    PyObject *freqs, *slopes, *arg;                           // names of a rotary's and a rule's attributes
 #define VXL_DECLARE(name) decltype(&vxl_##name) name;
     VXL_PATH(VXL_DECLARE)
 };
@@ -37,7 +40,9 @@ struct State {
 // (its tensors as they are at the call, and its format) or None, a null pointer; a tensor (its
 // data pointer; a contiguous CUDA tensor or AssertionError) or None, a null pointer; a number.  Python does not pass
 // kNumel, the number of elements of the tensor before it (0 for None), and size(i, d), dimension d of its argument i.
-enum Kind { kLayout, kDesc, kCache, kTensor, kInt, kNumel, kSize };
+// The calls on rotary positions and growing sets hold their tensors to more: of the descriptor's type, float32 or int32, on one device, the
+// current one; beside them a rotary or a rule, or None, a null pointer.
+enum Kind { kLayout, kDesc, kCache, kTensor, kInt, kRotary, kRule, kOfDesc, kFloats, kInts, kNumel, kSize };
 constexpr int size(int arg, int dim) { return kSize | arg << 8 | dim << 16; }
 
 // A number that an object answers with (a new reference, or null where it raised).
@@ -144,10 +149,15 @@ struct CacheArg {
     long long n_kv_heads, head_dim;
 };
 
-// What a call keeps until it returns: the place of the next argument, the caches given, references to their tensors.
+// What a call keeps until it returns: the place of the next argument, the caches given, references to their tensors; a rotary, a
+// rule; the descriptor, and the device of the tensors that are held to one.
 struct Frame {
     int next = 0, n_caches = 0, n_held = 0;
     CacheArg caches[2];
+    vxl_rotary rotary;
+    vxl_score_rule rule;
+    const vxl_attn_desc* desc = nullptr;
+    int device = -1;
     PyObject* held[4];
     ~Frame() { while (n_held > 0) Py_DECREF(held[--n_held]); }
 };
@@ -193,6 +203,68 @@ bool cache_of(const State& st, Frame& f, PyObject* o, long long* out) {
     return true;
 }
 
+// Pointer of a tensor of this type on the device of the others, or null for None.
+bool typed_of(Frame& f, PyObject* o, at::ScalarType type, const char* name, long long* out) {
+    if (!tensor_of(o, out) || o == Py_None) return !PyErr_Occurred();
+    bool ok;
+    if (THPVariable_Check(o)) {
+        const at::Tensor& t = THPVariable_Unpack(o);
+        ok = t.scalar_type() == type;
+        const int device = t.device().index();
+        if (f.device >= 0 && device != f.device) { PyErr_SetString(PyExc_ValueError, "the tensors are on several devices"); return false; }
+        f.device = device;
+    } else {
+        PyObject* dtype = PyObject_GetAttrString(o, "dtype");
+        if (!dtype) return false;
+        ok = THPDtype_Check(dtype) && ((THPDtype*)dtype)->scalar_type == type;
+        Py_DECREF(dtype);
+    }
+    if (!ok) PyErr_Format(PyExc_ValueError, "a %s tensor expected", name);
+    return ok;
+}
+
+bool data_of(Frame& f, PyObject* o, long long* out) {
+    const bool f32 = f.desc && f.desc->dtype == VXL_F32;
+    return typed_of(f, o, f32 ? at::kFloat : at::kBFloat16, f32 ? "float32" : "bfloat16", out);
+}
+
+// The struct of a rotary or a rule, copied, and the pointer and size of its tensor as they are at the call.
+template <typename S>
+bool struct_of(const State& st, Frame& f, PyObject* o, PyObject* type, PyObject* name, at::ScalarType of, const char* of_name, S* to,
+               long long* tensor, long long* numel) {
+    if (!type || !PyObject_TypeCheck(o, (PyTypeObject*)type)) return refuse(o, name == st.freqs ? "a Rotary" : "a ScoreRule");
+    PyObject* arg = PyObject_GetAttr(o, st.arg);
+    void* p = nullptr;
+    const bool ok = arg && memory_of(arg, &p);
+    if (ok) *to = *(const S*)p;
+    Py_XDECREF(arg);
+    if (!ok) return false;
+    PyObject* t = PyObject_GetAttr(o, name);
+    if (!t) return false;
+    f.held[f.n_held++] = t;
+    return typed_of(f, t, of, of_name, tensor) && numel_of(t, numel);
+}
+
+bool rotary_of(const State& st, Frame& f, PyObject* o, long long* out) {
+    if (o == Py_None) { *out = 0; return true; }
+    long long freqs, n;
+    if (!struct_of(st, f, o, st.rotary_type, st.freqs, at::kDouble, "float64", &f.rotary, &freqs, &n)) return false;
+    f.rotary.freqs = (const double*)freqs;
+    if (2 * n != f.rotary.rotary_dim) { PyErr_SetString(PyExc_ValueError, "the frequencies of a rotary have changed their number"); return false; }
+    *out = (long long)&f.rotary;
+    return true;
+}
+
+bool rule_of(const State& st, Frame& f, PyObject* o, long long* out) {
+    if (o == Py_None) { *out = 0; return true; }
+    long long slopes, n;
+    if (!struct_of(st, f, o, st.rule_type, st.slopes, at::kFloat, "float32", &f.rule, &slopes, &n)) return false;
+    f.rule.slopes = (const float*)slopes;
+    if (slopes && f.desc && n != f.desc->n_q_heads) { PyErr_SetString(PyExc_ValueError, "a slope per query head expected"); return false; }
+    *out = (long long)&f.rule;
+    return true;
+}
+
 constexpr bool passed(int kind) { return kind < kNumel; }
 
 // The argument of this kind: the next of Python's, or a number read off one.
@@ -202,7 +274,15 @@ bool convert(const State& st, PyObject* const* args, Frame& f, long long* out) {
     if constexpr ((KIND & 255) == kSize) return size_of(args[KIND >> 8 & 255], KIND >> 16, out);
     else if constexpr (KIND == kNumel) return numel_of(args[*next - 1], out);
     else if constexpr (KIND == kLayout) return layout_of(st, args[(*next)++], out);
-    else if constexpr (KIND == kDesc) return desc_of(st, args[(*next)++], out);
+    else if constexpr (KIND == kDesc) {
+        if (!desc_of(st, args[(*next)++], out)) return false;
+        f.desc = (const vxl_attn_desc*)*out;
+        return true;
+    } else if constexpr (KIND == kRotary) return rotary_of(st, f, args[(*next)++], out);
+    else if constexpr (KIND == kRule) return rule_of(st, f, args[(*next)++], out);
+    else if constexpr (KIND == kOfDesc) return data_of(f, args[(*next)++], out);
+    else if constexpr (KIND == kFloats) return typed_of(f, args[(*next)++], at::kFloat, "float32", out);
+    else if constexpr (KIND == kInts) return typed_of(f, args[(*next)++], at::kInt, "int32", out);
     else if constexpr (KIND == kCache) return cache_of(st, f, args[(*next)++], out);
     else if constexpr (KIND == kTensor) return tensor_of(args[(*next)++], out);
     else return int_of(args[(*next)++], out);
@@ -222,6 +302,11 @@ PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n, F f) {
     } catch (const std::exception& e) {                       // (a tensor without memory)
         PyErr_SetString(PyExc_RuntimeError, e.what());
         return nullptr;
+    }
+    if (frame.device >= 0) {
+        long long current;
+        if (!take(PyObject_CallNoArgs(st.device_of), &current)) return nullptr;
+        if (current != frame.device) { PyErr_SetString(PyExc_ValueError, "the tensors are on another device than the current one"); return nullptr; }
     }
     PyObject* s = PyObject_CallFunctionObjArgs(st.stream_of, args[n - 1], nullptr);
     if (!s) return nullptr;
@@ -350,6 +435,89 @@ PyObject* bilevel_decode_kvq(PyObject* self, PyObject* const* args, Py_ssize_t n
                                       ptr<int32_t>(a[12]), ptr<void>(a[13]), (size_t)a[14], (vxl_stream)a[15]);
     });
 }
+
+// Whether a tensor (0 elements: there is none) has as many elements as the call takes off it.
+bool has(long long numel, std::initializer_list<long long> dims) {
+    __int128 n = 1;
+    for (long long x : dims) n *= x;
+    return numel == 0 || n == numel;
+}
+// Whether one of queries or keys holds the rows of n tokens, by the descriptor's layout.
+bool holds_rows(const vxl_attn_desc* d, long long n, long long numel, bool queries) {
+    if (!queries) return holds(d, n, numel);
+    vxl_attn_desc q = *d;
+    q.n_kv_heads = d->n_q_heads;
+    q.kv_stride_head = d->q_stride_head;
+    q.kv_stride_tok = d->q_stride_tok;
+    return holds(&q, n, numel);
+}
+
+PyObject* rotate(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    return call<kDesc, kRotary, kInts, kNumel, kOfDesc, kNumel, kOfDesc, kNumel, kOfDesc, kNumel, kOfDesc, kNumel>(
+        self, args, n, [](const State& lib, const long long* a) {
+        const long long tokens = a[3];
+        if (!in_32_bits(tokens)) return VXL_ERR_INVALID_ARG;
+        for (int i : {4, 6, 8, 10})
+            if (a[i] && !holds_rows(desc(a[0]), tokens, a[i + 1], i == 4 || i == 8)) return VXL_ERR_INVALID_ARG;
+        return lib.rotate(desc(a[0]), ptr<vxl_rotary>(a[1]), ptr<int32_t>(a[2]), (int32_t)tokens, ptr<void>(a[4]), ptr<void>(a[6]),
+                          ptr<void>(a[8]), ptr<void>(a[10]), (vxl_stream)a[12]);
+    });
+}
+// (batch and new tokens: of positions; rows: of kmix)
+PyObject* mixed_append(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    return call<kDesc, kRotary, kInts, size(2, 0), size(2, 1), kOfDesc, kNumel, kOfDesc, kNumel, kOfDesc, kNumel, kOfDesc, kNumel, kOfDesc, kNumel,
+                kOfDesc, kNumel, size(7, 2), kInts, kNumel, kInts, kNumel, kFloats, kNumel>(
+        self, args, n, [](const State& lib, const long long* a) {
+        const vxl_attn_desc* d = desc(a[0]);
+        const long long batch = a[3], tokens = a[4], cap = a[17], hkv = d->n_kv_heads;
+        if (!in_32_bits(batch) || !in_32_bits(tokens) || !in_32_bits(batch * tokens) || !in_32_bits(cap)) return VXL_ERR_INVALID_ARG;
+        for (int i : {5, 7, 9})
+            if (!holds_rows(d, batch * tokens, a[i + 1], i == 5)) return VXL_ERR_INVALID_ARG;
+        if (!has(a[12], {batch, tokens, d->n_q_heads, d->head_dim}) || !has(a[14], {batch, hkv, cap, d->head_dim}) ||
+            !has(a[16], {batch, hkv, cap, d->head_dim}) || !has(a[19], {batch}) || !has(a[21], {batch, hkv, cap}) || !has(a[23], {batch, hkv, cap}))
+            return VXL_ERR_INVALID_ARG;
+        return lib.mixed_append(d, ptr<vxl_rotary>(a[1]), ptr<int32_t>(a[2]), (int32_t)batch, (int32_t)tokens, ptr<void>(a[5]), ptr<void>(a[7]),
+                                ptr<void>(a[9]), ptr<void>(a[11]), ptr<void>(a[13]), ptr<void>(a[15]), (int32_t)cap, ptr<int32_t>(a[18]),
+                                ptr<int32_t>(a[20]), ptr<float>(a[22]), (vxl_stream)a[24]);
+    });
+}
+// (batch and tokens: of qd; rows: of kmix)
+PyObject* mixed_attend(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    return call<kDesc, kRule, kOfDesc, size(2, 0), size(2, 1), kNumel, kInts, kNumel, kOfDesc, size(4, 2), kNumel, kOfDesc, kNumel, kInts, kNumel,
+                kInts, kNumel, kOfDesc, kNumel, kFloats, kNumel, kFloats, kNumel, kFloats, kNumel, kTensor, kNumel>(
+        self, args, n, [](const State& lib, const long long* a) {
+        const vxl_attn_desc* d = desc(a[0]);
+        const long long batch = a[3], tokens = a[4], cap = a[9], hkv = d->n_kv_heads, hq = d->n_q_heads;
+        if (!in_32_bits(batch) || !in_32_bits(tokens) || !in_32_bits(cap)) return VXL_ERR_INVALID_ARG;
+        if (!has(a[5], {batch, tokens, hq, d->head_dim}) || !has(a[7], {batch, tokens}) || !has(a[10], {batch, hkv, cap, d->head_dim}) ||
+            !has(a[12], {batch, hkv, cap, d->head_dim}) || !has(a[14], {batch}) || !has(a[16], {batch, hkv, cap}) ||
+            !has(a[18], {batch, tokens, hq, d->head_dim}) || !has(a[20], {batch, tokens, hq}) || !has(a[22], {batch, hkv, cap}) ||
+            !has(a[24], {batch, hkv, cap}))
+            return VXL_ERR_INVALID_ARG;
+        return lib.mixed_attend(d, ptr<vxl_score_rule>(a[1]), ptr<void>(a[2]), ptr<int32_t>(a[6]), (int32_t)batch, (int32_t)tokens, ptr<void>(a[8]),
+                                ptr<void>(a[11]), (int32_t)cap, ptr<int32_t>(a[13]), ptr<int32_t>(a[15]), ptr<void>(a[17]), ptr<float>(a[19]),
+                                ptr<float>(a[21]), ptr<float>(a[23]), ptr<void>(a[25]), (size_t)a[26], (vxl_stream)a[27]);
+    });
+}
+// (batch and rows: of kmix; rows of the result: of kout)
+PyObject* mixed_evict(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    return call<kDesc, kOfDesc, size(1, 0), size(1, 2), kNumel, kOfDesc, kNumel, kInts, kNumel, kFloats, kNumel, kInts, kNumel, kInts, kNumel, kInt,
+                kInt, kInt, kOfDesc, size(10, 2), kNumel, kOfDesc, kNumel, kFloats, kNumel, kInts, kNumel, kInts, kNumel, kTensor, kNumel>(
+        self, args, n, [](const State& lib, const long long* a) {
+        const vxl_attn_desc* d = desc(a[0]);
+        const long long batch = a[2], cap = a[3], to = a[19], hkv = d->n_kv_heads, dim = d->head_dim;
+        for (long long x : {batch, cap, to, a[15], a[16], a[17]})
+            if (!in_32_bits(x)) return VXL_ERR_INVALID_ARG;
+        if (!has(a[4], {batch, hkv, cap, dim}) || !has(a[6], {batch, hkv, cap, dim}) || !has(a[8], {batch}) || !has(a[10], {batch, hkv, cap}) ||
+            !has(a[12], {batch, hkv, cap}) || !has(a[14], {batch}) || !has(a[20], {batch, hkv, to, dim}) || !has(a[22], {batch, hkv, to, dim}) ||
+            !has(a[24], {batch, hkv, to}) || !has(a[26], {batch, hkv, to}) || !has(a[28], {batch}))
+            return VXL_ERR_INVALID_ARG;
+        return lib.mixed_evict(d, ptr<void>(a[1]), ptr<void>(a[5]), (int32_t)cap, ptr<int32_t>(a[7]), ptr<float>(a[9]), ptr<int32_t>(a[11]),
+                               ptr<int32_t>(a[13]), (int32_t)batch, (int32_t)a[15], (int32_t)a[16], (int32_t)a[17], ptr<void>(a[18]), ptr<void>(a[21]),
+                               (int32_t)to, ptr<float>(a[23]), ptr<int32_t>(a[25]), ptr<int32_t>(a[27]), ptr<void>(a[29]), (size_t)a[30],
+                               (vxl_stream)a[31]);
+    });
+}
 // setup(type of the descriptor, type of a layout's handle, vxl._stream, the addresses of VXL_PATH)
 PyObject* setup(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 #define VXL_COUNT(name) + 1
@@ -385,6 +553,24 @@ PyObject* setup_cache(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     Py_XSETREF(st.cache_type, args[0]);
     Py_RETURN_NONE;
 }
+// setup_mixed(type of a rotary, type of a rule, function that answers the current device's number)
+PyObject* setup_mixed(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    if (n != 3 || !PyType_Check(args[0]) || !PyType_Check(args[1]) || !PyCallable_Check(args[2])) {
+        PyErr_SetString(PyExc_TypeError, "two types and a function expected");
+        return nullptr;
+    }
+    State& st = *(State*)PyModule_GetState(self);
+    PyObject** const names[] = {&st.freqs, &st.slopes, &st.arg};
+    const char* const text[] = {"freqs", "slopes", "arg"};
+    for (int i = 0; i < 3; ++i)
+        if (!*names[i] && !(*names[i] = PyUnicode_InternFromString(text[i]))) return nullptr;
+    PyObject** to[] = {&st.rotary_type, &st.rule_type, &st.device_of};
+    for (int i = 0; i < 3; ++i) {
+        Py_INCREF(args[i]);
+        Py_XSETREF(*to[i], args[i]);
+    }
+    Py_RETURN_NONE;
+}
 
 int traverse(PyObject* self, visitproc visit, void* arg) {
     const State* st = (const State*)PyModule_GetState(self);
@@ -392,6 +578,9 @@ int traverse(PyObject* self, visitproc visit, void* arg) {
     Py_VISIT(st->desc_type);
     Py_VISIT(st->handle_type);
     Py_VISIT(st->cache_type);
+    Py_VISIT(st->rotary_type);
+    Py_VISIT(st->rule_type);
+    Py_VISIT(st->device_of);
     Py_VISIT(st->stream_of);
     return 0;
 }
@@ -405,13 +594,19 @@ int clear(PyObject* self) {
     Py_CLEAR(st->scales);
     Py_CLEAR(st->format);
     Py_CLEAR(st->stream_of);
+    Py_CLEAR(st->rotary_type);
+    Py_CLEAR(st->rule_type);
+    Py_CLEAR(st->device_of);
+    Py_CLEAR(st->freqs);
+    Py_CLEAR(st->slopes);
+    Py_CLEAR(st->arg);
     return 0;
 }
 
 int exec(PyObject* self) { return PyModule_AddStringConstant(self, "torch_version", VXL_TORCH_VERSION); }
 
 #define VXL_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr},
-PyMethodDef methods[] = {VXL_METHOD(setup) VXL_METHOD(setup_cache) VXL_PATH(VXL_METHOD){nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {VXL_METHOD(setup) VXL_METHOD(setup_cache) VXL_METHOD(setup_mixed) VXL_PATH(VXL_METHOD){nullptr, nullptr, 0, nullptr}};
 PyModuleDef_Slot slots[] = {{Py_mod_exec, (void*)exec}, {0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_vxl_torch", nullptr, sizeof(State), methods, slots, traverse, clear, nullptr};
 

@@ -19,7 +19,7 @@ BINDING_PATH = os.path.join(_PKG, "_vxl_torch" + (sysconfig.get_config_var("EXT_
 
 VXL_OK, VXL_ERR_INVALID_ARG, VXL_ERR_UNSUPPORTED, VXL_ERR_WORKSPACE, VXL_ERR_HIP, VXL_ERR_ALLOC = range(6)
 VXL_F32, VXL_BF16 = 0, 1
-OP_PREFILL, OP_SCORE_TOPK, OP_GATHER, OP_DECODE, OP_SCORE_MASS, OP_DECODE_INPLACE, OP_DECODE_KVQ = range(7)
+OP_PREFILL, OP_SCORE_TOPK, OP_GATHER, OP_DECODE, OP_SCORE_MASS, OP_DECODE_INPLACE, OP_DECODE_KVQ, OP_MIXED_ATTEND, OP_MIXED_EVICT = range(9)
 KVQ_FP8, KVQ_FP4 = range(2)
 MAX_CHUNKS = 4096
 
@@ -36,6 +36,17 @@ class KvqCacheArg(C.Structure):
     _fields_ = [("rows", C.c_void_p), ("scales", C.c_void_p), ("format", C.c_int32), ("capacity", C.c_int32)]
 
 
+class RotaryArg(C.Structure):
+    """vxl_rotary"""
+    _fields_ = [("freqs", C.c_void_p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float),
+                ("transpose", C.c_int32)]
+
+
+class ScoreRuleArg(C.Structure):
+    """vxl_score_rule"""
+    _fields_ = [("softcap", C.c_float), ("causal", C.c_int32), ("window", C.c_int32), ("n_always", C.c_int32), ("slopes", C.c_void_p)]
+
+
 class VxlError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -49,7 +60,7 @@ _native = None
 # The calls of the path, in the order in which the binding takes their addresses.
 _PATH = ("chunk_prefill", "chunk_score_topk", "chunk_score_topk_mass", "gather_bilevel_kv", "pool_sparse_kv",
          "gather_bilevel_kv_pooled", "bilevel_decode", "bilevel_decode_inplace", "kvq_write", "kvq_read", "gather_bilevel_kvq",
-         "bilevel_decode_kvq")
+         "bilevel_decode_kvq", "rotate", "mixed_append", "mixed_attend", "mixed_evict")
 
 
 def lib() -> C.CDLL:
@@ -118,6 +129,15 @@ def lib() -> C.CDLL:
     L.vxl_gather_bilevel_kvq.argtypes = [vp, dp, cp, cp, vp, i32, vp, vp, i32, vp, vp, vp]
     L.vxl_bilevel_decode_kvq.restype = C.c_int
     L.vxl_bilevel_decode_kvq.argtypes = [vp, dp, vp, i32, i32, cp, cp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
+    rp, sp = C.POINTER(RotaryArg), C.POINTER(ScoreRuleArg)
+    L.vxl_rotate.restype = C.c_int
+    L.vxl_rotate.argtypes = [dp, rp, vp, i32, vp, vp, vp, vp, vp]
+    L.vxl_mixed_append.restype = C.c_int
+    L.vxl_mixed_append.argtypes = [dp, rp, vp, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
+    L.vxl_mixed_attend.restype = C.c_int
+    L.vxl_mixed_attend.argtypes = [dp, sp, vp, vp, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.vxl_mixed_evict.restype = C.c_int
+    L.vxl_mixed_evict.argtypes = [dp, vp, vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, sz, vp]
     L.vxl_debug_force_simple.argtypes = [C.c_int]
     L.vxl_debug_prefill_variant.argtypes = [C.c_int]
     L.vxl_debug_prefill_events.argtypes = [vp, vp]
@@ -163,6 +183,7 @@ def native():
                                f"{build} again")
         module.setup(AttnDesc, C.c_void_p, _stream, *(C.cast(getattr(L, "vxl_" + n), C.c_void_p).value for n in _PATH))
         module.setup_cache(KvqCache)
+        module.setup_mixed(Rotary, ScoreRule, _current_device or torch.cuda.current_device)
         _native = module
     return _native
 
@@ -388,6 +409,80 @@ def bilevel_decode_kvq(layout: Layout, desc: AttnDesc, qd, cache: KvqCache, spar
                                                   out, lse, mix_len, workspace, stream)
     _check(st, "vxl_bilevel_decode_kvq")
     return out
+
+
+def _int32(x, what: str) -> int:
+    if not -2 ** 31 <= x < 2 ** 31 or x != int(x):
+        raise ValueError(f"{what} {x} is no number of 32 bits")
+    return int(x)
+
+
+class Rotary:
+    """Rotary positions (vxl_rotary): freqs float64 [rotary_dim / 2] on the device, radians per position of every pair.  Read-only; a call takes
+    the frequencies as they are then."""
+
+    def __init__(self, freqs: torch.Tensor, interleaved: bool = False, magnitude: float = 1.0, transpose: bool = False):
+        if freqs.dtype != torch.float64 or freqs.dim() != 1:
+            raise ValueError(f"a float64 tensor of one dimension expected, not {freqs.dtype} of {tuple(freqs.shape)}")
+        _ptr(freqs)
+        self._freqs = freqs
+        self._arg = RotaryArg(None, 2 * freqs.numel(), int(bool(interleaved)), float(magnitude), int(bool(transpose)))
+
+    freqs = property(lambda self: self._freqs)
+    arg = property(lambda self: self._arg)
+
+    def transposed(self) -> "Rotary":
+        """The transpose of this map: the gradient of what it returned to that of what it was given."""
+        a = self._arg
+        return Rotary(self._freqs, a.interleaved, a.magnitude, not a.transpose)
+
+
+class ScoreRule:
+    """Which rows a token sees and what its logits are (vxl_score_rule); slopes float32 [Hq] on the device, or None.  Read-only."""
+
+    def __init__(self, softcap: float = 0.0, causal: bool = False, window: int = 0, n_always: int = 0, slopes: Optional[torch.Tensor] = None):
+        if slopes is not None and (slopes.dtype != torch.float32 or slopes.dim() != 1):
+            raise ValueError(f"a float32 tensor of one dimension expected, not {slopes.dtype} of {tuple(slopes.shape)}")
+        _ptr(slopes)
+        self._slopes = slopes
+        self._arg = ScoreRuleArg(float(softcap), int(bool(causal)), _int32(window, "window"), _int32(n_always, "n_always"), None)
+
+    slopes = property(lambda self: self._slopes)
+    arg = property(lambda self: self._arg)
+
+
+def rotate(desc: AttnDesc, rotary: Rotary, positions, q, k, q_out, k_out, stream=None):
+    """vxl_rotate: positions int32 [N]; q/q_out and k/k_out (or None, both) in the descriptor's layouts, in place or not."""
+    st = (_native or native()).rotate(desc, rotary, positions, q, k, q_out, k_out, stream)
+    _check(st, "vxl_rotate")
+    return q_out, k_out
+
+
+def mixed_append(desc: AttnDesc, rotary: Optional[Rotary], positions, q, k, v, qd, kmix, vmix, mix_len, row_pos=None, row_weight=None,
+                 stream=None):
+    """vxl_mixed_append: positions int32 [B,T]; q, k, v of B * T tokens in the descriptor's layouts; qd [B,T,Hq,D]; kmix/vmix
+    [B,Hkv,Lcap,D]; mix_len int32 [B], the new rows among them; row_pos int32, row_weight float32 [B,Hkv,Lcap]."""
+    st = (_native or native()).mixed_append(desc, rotary, positions, q, k, v, qd, kmix, vmix, mix_len, row_pos, row_weight, stream)
+    _check(st, "vxl_mixed_append")
+    return qd
+
+
+def mixed_attend(desc: AttnDesc, rule: Optional[ScoreRule], qd, q_pos, kmix, vmix, mix_len, row_pos, out, lse=None, weight=None,
+                 weight_out=None, workspace=None, stream=None):
+    """vxl_mixed_attend: qd/out [B,T,Hq,D]; q_pos int32 [B,T] and row_pos int32 [B,Hkv,Lcap], or None both; lse float32 [B,T,Hq];
+    weight, weight_out float32 [B,Hkv,Lcap] (one tensor: in place)."""
+    st = (_native or native()).mixed_attend(desc, rule, qd, q_pos, kmix, vmix, mix_len, row_pos, out, lse, weight, weight_out, workspace, stream)
+    _check(st, "vxl_mixed_attend")
+    return out
+
+
+def mixed_evict(desc: AttnDesc, kmix, vmix, mix_len, weight, row_pos, newest, keep: int, n_first: int, n_recent: int, kout, vout,
+                weight_out, pos_out, kept, workspace=None, stream=None):
+    """vxl_mixed_evict: sets of kmix/vmix [B,Hkv,Lcap,D] cut back to kout/vout [B,Hkv,Lout,D], or in place; newest int32 [B] (None where
+    n_recent is 0); kept int32 [B]."""
+    st = (_native or native()).mixed_evict(desc, kmix, vmix, mix_len, weight, row_pos, newest, int(keep), int(n_first), int(n_recent), kout, vout,
+                                           weight_out, pos_out, kept, workspace, stream)
+    _check(st, "vxl_mixed_evict")
 
 
 STATIC_SCRATCH_BYTES = 32 << 20
