@@ -2,6 +2,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <limits>
 #include <type_traits>
 
 #include "vxl_mfma.h"
@@ -155,25 +156,678 @@ __global__ __launch_bounds__(256) void simple_weights_kernel(Sets s, Rule r, con
     if (row < len) weight_out[set + row] = (weight ? weight[set + row] : 0.f) + w;
 }
 
+// ------------------------------------------------------------------------------------------
+// Many stacked query rows (rho = t * G + head of the group): 32 per wave, NW waves per workgroup; the 64-key tiles of the workgroup's split
+// stream through a ring of four LDS stages by direct loads, two tiles ahead of the arithmetic, as in the plain decode's ring, whose products
+// and layouts these are.  What a rule adds:
+//   * The positions of a tile come with it, by one wave's load.  A lane has a key's; against the range of positions that the wave's 32 rows
+//     see, a ballot each tells a tile that none sees (skipped), one that all see (nothing more) and one that needs a test per element;
+//     only then, and for a bias, a lane reads the positions of its elements.
+//   * Sums are of the weights as they are, not as rounded to bf16 for the second product, so that the LSE has fp32's error.
+//   * A value that is not a number reaches rows that do not see it, 0 * inf: a row whose result is none is made again by exact_row.
+// ------------------------------------------------------------------------------------------
+constexpr float kLowest = -std::numeric_limits<float>::max();
+
+template <int D, int NW>
+struct RingCfg {
+    static constexpr int NS = 4, ROWS = 32 * NW, TILE = kKeyTile * D, STAGE = 2 * TILE;        // elements
+    static constexpr int PPR = D / 8, RPI = 64 / PPR, IPW = kKeyTile / RPI / NW;               // pieces of a row; rows, loads of a wave
+    static constexpr int POS_AT = NS * STAGE * 2, LDS_BYTES = POS_AT + NS * kKeyTile * 4;      // bytes: the positions behind the stages
+};
+
+// What kernels that cut the keys leave for the merge: unnormalised O, and per row the reference (base 2) and the sum.
+struct Partials {
+    float* o;                  // [unit][split][rows][D]
+    float2* ml;                // [unit][split][rows]
+};
+
+// Workgroups that read the same keys are neighbours on one XCD (workgroups go to the XCDs in turn): grid.x = XCDs.
+__device__ __forceinline__ bool place(int units, int n_split, int n_rtile, int* unit, int* split, int* rtile) {
+    const unsigned all = (unsigned)(units * n_split * n_rtile), each = (all + gridDim.x - 1) / gridDim.x;
+    const unsigned own = blockIdx.z * gridDim.y + blockIdx.y, id = blockIdx.x * each + own;
+    if (own >= each || id >= all) return false;
+    *rtile = (int)(id % n_rtile);
+    *split = (int)(id / n_rtile % n_split);
+    *unit = (int)(id / n_rtile / n_split);
+    return true;
+}
+
+// The positions that the 32 rows of a wave see, at most and at least.
+struct Reach {
+    Span most, least;
+    __device__ __forceinline__ void of(const Span& s) {
+        most = least = s;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            most.lo = min(most.lo, __shfl_xor(most.lo, o));
+            most.hi = max(most.hi, __shfl_xor(most.hi, o));
+            most.na = max(most.na, (unsigned)__shfl_xor((int)most.na, o));
+            least.lo = max(least.lo, __shfl_xor(least.lo, o));
+            least.hi = min(least.hi, __shfl_xor(least.hi, o));
+            least.na = min(least.na, (unsigned)__shfl_xor((int)least.na, o));
+        }
+    }
+};
+
+// softcap tanh(s / softcap) in units of log 2.  tanh u for |u| < 0.4 by its odd series to u^13 (the next term is 1.5e-3 u^14 of it, 4e-9
+// there), which has no cancellation and is cheaper than the exponential and the quotient beyond, where they have little.
+__device__ __forceinline__ float tanh_small(float u) {
+    const float z = u * u;
+    float p = fmaf(z, 3.59212803657e-3f, -8.86323552990e-3f);
+    p = fmaf(p, z, 2.18694885362e-2f);
+    p = fmaf(p, z, -5.39682539683e-2f);
+    p = fmaf(p, z, 1.33333333333e-1f);
+    p = fmaf(p, z, -3.33333333333e-1f);
+    return fmaf(u * z, p, u);
+}
+__device__ __forceinline__ float tanh_any(float u) {
+    asm("" : "+v"(u));                                        // (its series is not hoisted out of both branches below: registers)
+    float t = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(fabsf(u) * (2.f * kLog2e)) + 1.f), u), few = tanh_small(u);
+    asm("" : "+v"(t), "+v"(few));                             // (both there: a selection, not a branch per element)
+    return fabsf(u) < 0.4f ? few : t;
+}
+// (one decision for the wave's elements)
+template <int N>
+__device__ __forceinline__ void cap_logits(float (&x)[N], const Rule& r) {
+    float top = 0.f;                                          // (NaN is NaN either way)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] *= r.cap_in;
+        top = fmaxf(top, fabsf(x[i]));
+    }
+    if (__builtin_amdgcn_ballot_w64(!(top < 0.4f)) == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = r.cap2 * tanh_small(x[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            x[i] = r.cap2 * tanh_any(x[i]);
+            if (i % 2) __builtin_amdgcn_sched_barrier(0);     // (two at a time: all at once need more registers than there are)
+        }
+    }
+}
+
+template <int D, int NW, bool POS>
+__global__ __launch_bounds__(64 * NW, 2) void attend_ring_kernel(Sets s, Rule r, Partials part, uint16_t* __restrict__ O, float* __restrict__ LSE,
+                                                                 float* __restrict__ lse2, int units, int n_split, int n_rtile) {
+    using C = RingCfg<D, NW>;
+    extern __shared__ __attribute__((aligned(16))) uint16_t lds[];
+    __shared__ __attribute__((aligned(16))) float q_lds[NW][D];          // (of rows made again)
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hi = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int unit, split, rtile;
+    if (!place(units, n_split, n_rtile, &unit, &split, &rtile)) return;
+    const int g = unit % s.n_kv, b = unit / s.n_kv, group = s.n_q / s.n_kv, n_rows = group * s.T;
+    const int len = __builtin_amdgcn_readfirstlane(min(max(s.len[b], 0), s.cap));
+    // the split's tiles: an even share of the set's
+    const int tiles = (len + kKeyTile - 1) / kKeyTile, share = tiles / n_split, more = tiles % n_split;
+    const int tile0 = split * share + min(split, more), n_t = share + (split < more ? 1 : 0);
+    const int k_lo = tile0 * kKeyTile, k_hi = min((tile0 + n_t) * kKeyTile, len);
+    const int wrow0 = rtile * C::ROWS + wave * 32;
+    const bool wave_active = wrow0 < n_rows;                  // (waves without rows only help with the loads)
+    const size_t set = (size_t)unit * s.cap;
+    const uint16_t *kset = (const uint16_t*)s.k + set * D, *vset = (const uint16_t*)s.v + set * D;
+    const char *kbase = (const char*)(kset + (size_t)k_lo * D), *vbase = (const char*)(vset + (size_t)k_lo * D);
+    const int32_t* pos = POS ? r.row_pos + set : nullptr;
+    const int r_in = lane / C::PPR, pp = lane % C::PPR;
+
+    // Tile t -> stage t % NS; rows past the end of the split are its last row (masked, and V a value that counts).
+    auto issue = [&](int t) __attribute__((always_inline)) {
+        const int row0 = t * kKeyTile, rlim = min(kKeyTile - 1, k_hi - k_lo - 1 - row0);
+        const char *kb = kbase + (size_t)row0 * (D * 2), *vb = vbase + (size_t)row0 * (D * 2);
+        const uint32_t st = lds_base + (uint32_t)(t % C::NS) * (C::STAGE * 2);
+#pragma unroll
+        for (int i = 0; i < C::IPW; ++i) {
+            const int slot = wave + i * NW, row = slot * C::RPI + r_in;
+            const int kp = pp ^ ((row / (16 / C::PPR)) & (C::PPR - 1));
+            constexpr int CPR = D * 2 / 64, RPL = D == 128 ? 1 : 2;
+            const int vp = (((pp >> 2) ^ ((row / RPL) & (CPR - 1))) << 2) | (pp & 3);
+            const uint32_t roff = (uint32_t)min(row, rlim) * (D * 2);
+            dma16(kb, roff + kp * 16, st + slot * 1024);
+            dma16(vb, roff + vp * 16, st + C::TILE * 2 + slot * 1024);
+        }
+        if (POS && wave == 0) dma4(pos + k_lo + row0, (uint32_t)min(lane, rlim) * 4, lds_base + C::POS_AT + (uint32_t)(t % C::NS) * (kKeyTile * 4));
+    };
+    if (n_t > 0) {
+        issue(0);
+        issue(min(1, n_t - 1));
+    }
+    const int rho = min(wrow0 + l32, n_rows - 1), tok = rho / group, h = g * group + rho % group;
+    bf16x8 qreg[1][D / 16];
+    {
+        const uint4* src = (const uint4*)((const uint16_t*)s.q + (((size_t)b * s.T + tok) * s.n_q + h) * D);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) qreg[0][ks] = __builtin_bit_cast(bf16x8, src[ks * 2 + hi]);
+    }
+    const int pq = POS ? r.q_pos[b * s.T + tok] : 0;
+    const Span span = span_of(r, pq);
+    Reach reach;
+    reach.of(span);
+    const float slope2 = POS ? slope_of(r, h) : 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {                     // complete here: no load that the compiler counts is outstanding behind
+        typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+        asm volatile("" :: "v"(__builtin_bit_cast(u32x4, qreg[0][ks])));
+    }
+    asm volatile("" :: "v"(pq), "v"(slope2));
+    __builtin_amdgcn_sched_barrier(0);
+
+    f32x16 o[1][D / 32];
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) o[0][db] = zero16();
+    const bool capped = r.cap2 > 0.f, biased = POS && r.slopes;
+    const float cu = capped || biased ? 1.f : r.c2;           // units of x below
+    float m_run = -INFINITY, mc_run = kLowest, l_run = 0.f;
+
+    auto process = [&](int ti) __attribute__((always_inline)) {
+        if (!wave_active) return;
+        const int left = k_hi - k_lo - ti * kKeyTile;
+        bool partial = left < kKeyTile;
+        const int32_t* tile_pos = (const int32_t*)((const char*)lds + C::POS_AT) + (ti % C::NS) * kKeyTile;
+        if constexpr (POS) {
+            const int pk = lane < left ? tile_pos[lane] : -1;
+            if (__builtin_amdgcn_ballot_w64(sees(reach.most, pk)) == 0) return;
+            partial = ~__builtin_amdgcn_ballot_w64(sees(reach.least, pk)) != 0;
+        }
+        const uint16_t* kt = lds + (ti % C::NS) * C::STAGE;
+        f32x16 x[1][2];
+        if constexpr (NW == 4) qk_tile_ahead<D, 1>(kt, qreg, l32, hi, x);
+        else qk_tile<D, 1>(kt, qreg, l32, hi, x);
+        if (capped) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                float c[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) c[i] = x[0][kb][i];
+                cap_logits(c, r);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[0][kb][i] = c[i];
+            }
+        }
+        if constexpr (POS) {
+            if (partial || biased) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int rq = 0; rq < 4; ++rq) {
+                        const int4 p4 = *(const int4*)(tile_pos + kb * 32 + rq * 8 + hi * 4);
+                        const int p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float y = x[0][kb][rq * 4 + i];
+                            if (biased) y = fmaf(-slope2, (float)abs(pq - p[i]), capped ? y : y * r.c2);
+                            x[0][kb][rq * 4 + i] = sees(span, p[i]) && acc_key(kb, rq * 4 + i, hi) < left ? y : -INFINITY;
+                        }
+                    }
+            }
+        } else if (partial) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[0][kb][i] = acc_key(kb, i, hi) < left ? x[0][kb][i] : -INFINITY;
+        }
+        // The reference is raised, and sums and O rescaled, only when a logit is more than 2^8 above it.
+        float top = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[0][kb][i]);
+        if (__builtin_amdgcn_ballot_w64(fmaf(top, cu, -mc_run) > 8.f) != 0) {
+            const float m_new = fmaxf(m_run, fmaxf(top, __shfl_xor(top, 32)));
+            const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run - m_new) * cu);
+            l_run *= alpha;
+            m_run = m_new;
+            mc_run = fmaxf(m_new * cu, kLowest);
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[0][db][i] *= alpha;
+        }
+        bf16x8 pb[1][2][2];
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(x[0][kb][i], cu, -mc_run));
+                sum[i & 1] += p;
+                pb[0][kb][i >> 3][i & 7] = (__bf16)p;
+            }
+        l_run += sum[0] + sum[1];
+        if constexpr (NW == 4) pv_tile_ahead<D, 2>(kt + C::TILE, pb, lane, o);
+        else pv_tile<D, 1>(kt + C::TILE, pb, lane, o);
+    };
+    for (int t0 = 0; t0 < n_t; t0 += 2) {
+        wait_vmcnt<0>();                                      // this wave's parts of tiles t0, t0 + 1 have landed
+        __builtin_amdgcn_s_barrier();                         // ... and everyone's; the other two stages are free
+        issue(min(t0 + 2, n_t - 1));
+        process(t0);
+        issue(min(t0 + 3, n_t - 1));
+        if (t0 + 1 < n_t) process(t0 + 1);
+    }
+    wait_vmcnt<0>();                                          // drain the refills before the wave ends
+
+    if (!wave_active) return;
+    const float l = l_run + __shfl_xor(l_run, 32);
+    bool odd = false;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[0][db][i]) < INFINITY);
+    const bool there = wrow0 + l32 < n_rows;
+    unsigned long long again = __builtin_amdgcn_ballot_w64(odd && there);
+    again = (again | again >> 32) & 0xffffffffull;
+    const size_t part_row0 = ((size_t)unit * n_split + split) * n_rows;
+    if (there && !(again >> l32 & 1)) {
+        const size_t out = ((size_t)b * s.T + tok) * s.n_q + h;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int rq = 0; rq < 4; ++rq) {
+                const int d = db * 32 + rq * 8 + hi * 4;
+                const float v[4] = {o[0][db][rq * 4], o[0][db][rq * 4 + 1], o[0][db][rq * 4 + 2], o[0][db][rq * 4 + 3]};
+                if (n_split > 1) {
+                    *(float4*)(part.o + (part_row0 + rho) * D + d) = make_float4(v[0], v[1], v[2], v[3]);
+                } else {
+                    __attribute__((aligned(8))) const uint16_t x[4] = {f32_to_bf16(v[0] * inv), f32_to_bf16(v[1] * inv), f32_to_bf16(v[2] * inv),
+                                                                       f32_to_bf16(v[3] * inv)};
+                    *(uint2*)(O + out * D + d) = *(const uint2*)x;
+                }
+            }
+        if (hi == 0) {
+            if (n_split > 1) {
+                part.ml[part_row0 + rho] = make_float2(l == 0.f ? -INFINITY : mc_run, l);
+            } else {
+                const float y = l == 0.f ? -INFINITY : mc_run + __builtin_amdgcn_logf(l);
+                if (LSE) LSE[out] = y * kLn2;
+                lse2[(size_t)unit * n_rows + rho] = y;
+            }
+        }
+    }
+    if (again == 0) return;
+    float* q_row = q_lds[wave];
+    while (again) {                                           // (uniform)
+        const int row = wrow0 + __builtin_ctzll(again);
+        again &= again - 1;
+        const int t = row / group, hq = g * group + row % group;
+        const size_t out = ((size_t)b * s.T + t) * s.n_q + hq;
+        __builtin_amdgcn_wave_barrier();
+        for (int x = lane; x < D; x += 64) q_row[x] = as_float(((const uint16_t*)s.q)[out * D + x]);
+        __builtin_amdgcn_wave_barrier();
+        float m, l2, acc[D / 64];
+        exact_row<uint16_t, D>(r, q_row, kset, vset, r.row_pos ? r.row_pos + set : nullptr, k_lo, k_hi, r.q_pos ? r.q_pos[b * s.T + t] : 0,
+                               slope_of(r, hq), m, l2, acc);
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) {
+            if (n_split > 1) part.o[(part_row0 + row) * D + lane + 64 * x] = acc[x];
+            else O[out * D + lane + 64 * x] = f32_to_bf16(l2 == 0.f ? 0.f : acc[x] / l2);
+        }
+        if (lane == 0) {
+            if (n_split > 1) {
+                part.ml[part_row0 + row] = make_float2(m, l2);
+            } else {
+                const float y = l2 == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l2);
+                if (LSE) LSE[out] = y * kLn2;
+                lse2[(size_t)unit * n_rows + row] = y;
+            }
+        }
+    }
+}
+
+// The merge of the splits, one workgroup per query row: SG groups of D / 4 lanes take every SG-th split, four requested together, and are
+// folded through LDS in their order.
+template <bool F32, int D>
+__global__ __launch_bounds__(256) void attend_merge_kernel(Partials part, typename Storage<F32>::T* __restrict__ O, float* __restrict__ LSE,
+                                                           float* __restrict__ lse2, int T, int n_q, int n_kv, int n_split, long long all) {
+    constexpr int NV = D / 4, SG = 256 / NV, U = 4;
+    __shared__ __attribute__((aligned(16))) float red[SG][D];
+    __shared__ float2 stat[SG];
+    const int group = n_q / n_kv, n_rows = T * group, sg = threadIdx.x / NV, d = threadIdx.x % NV * 4;
+    const long long id = folded_id();
+    if (id >= all) return;
+    const int rho = (int)(id % n_rows);
+    const long long unit = id / n_rows;
+    const int g = (int)(unit % n_kv), b = (int)(unit / n_kv);
+    const size_t base = (size_t)unit * n_split * n_rows + rho;
+    float M = -INFINITY, L = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+    // (a part without weight counts for nothing, whatever it holds; a sum that is not a number stays one)
+    auto part_weight = [](float2 ml, float ref) __attribute__((always_inline)) {
+        return ml.y == 0.f ? 0.f : ml.y != ml.y ? 1.f : __builtin_amdgcn_exp2f(ml.x - ref);
+    };
+    auto add = [](float f, float x, float y) __attribute__((always_inline)) { return f == 0.f ? y : fmaf(f, x, y); };
+    for (int s0 = sg; s0 < n_split; s0 += U * SG) {
+        float2 ml[U];
+        float4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const size_t at = base + (size_t)min(s0 + u * SG, n_split - 1) * n_rows;
+            ml[u] = part.ml[at];
+            v[u] = *(const float4*)(part.o + at * D + d);
+        }
+        float m_new = M;
+#pragma unroll
+        for (int u = 0; u < U; ++u) m_new = fmaxf(m_new, ml[u].x);
+        const float ref = m_new == -INFINITY ? 0.f : m_new, f0 = L == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - ref);
+        M = m_new;
+        L *= f0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[j] = f0 == 0.f ? 0.f : a[j] * f0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float f = s0 + u * SG < n_split ? part_weight(ml[u], ref) : 0.f;
+            L = add(f, ml[u].y, L);
+            a[0] = add(f, v[u].x, a[0]); a[1] = add(f, v[u].y, a[1]); a[2] = add(f, v[u].z, a[2]); a[3] = add(f, v[u].w, a[3]);
+        }
+    }
+    *(float4*)&red[sg][d] = make_float4(a[0], a[1], a[2], a[3]);
+    if (d == 0) stat[sg] = make_float2(M, L);
+    __syncthreads();
+    if (threadIdx.x >= D) return;                             // a column each
+    M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < SG; ++i) M = fmaxf(M, stat[i].x);
+    const float ref = M == -INFINITY ? 0.f : M;
+    float sum = 0.f;
+    L = 0.f;
+#pragma unroll
+    for (int i = 0; i < SG; ++i) {
+        const float f = part_weight(stat[i], ref);
+        L = add(f, stat[i].y, L);
+        sum = add(f, red[i][threadIdx.x], sum);
+    }
+    const size_t row = ((size_t)b * T + rho / group) * n_q + g * group + rho % group;
+    store_as(O + row * D + threadIdx.x, L == 0.f ? 0.f : sum / L);
+    if (threadIdx.x == 0) {
+        const float y = L == 0.f ? -INFINITY : M + __builtin_amdgcn_logf(L);
+        if (LSE) LSE[row] = y * kLn2;
+        lse2[id] = y;
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// The weights of the rows where there are many query rows: the logits once more, against the LSE.  A wave keeps 64 keys in registers as
+// the operand of the first product and goes over query rows, 32 at a time through LDS for the four waves of a workgroup; a lane's sums
+// are of its 32 elements of the tile, folded over the lanes at the end.  Query rows are cut into n_part parts where keys alone do not
+// fill the chip, whose sums a last kernel adds in order.
+// ------------------------------------------------------------------------------------------
+constexpr int kWeightWaves = 4, kWeightKeys = 64 * kWeightWaves, kWeightRows = 32;
+
+template <int D, bool POS>
+__global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Sets s, Rule r, const float* __restrict__ lse2, const float* weight,
+                                                                              float* weight_out, float* __restrict__ part_w, int units, int n_part,
+                                                                              int n_blocks) {
+    constexpr int TILE = kWeightRows * D, PER = kWeightRows * D / 8 / (64 * kWeightWaves);    // 16-byte pieces of a thread
+    __shared__ __attribute__((aligned(16))) uint16_t q_lds[2][TILE];
+    __shared__ __attribute__((aligned(16))) int32_t pos_lds[POS ? kWeightWaves : 1][64];
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int unit, part, block;
+    if (!place(units, n_part, n_blocks, &unit, &part, &block)) return;
+    const int g = unit % s.n_kv, b = unit / s.n_kv, group = s.n_q / s.n_kv, n_rows = group * s.T;
+    const int len = min(max(s.len[b], 0), s.cap);
+    if (block * kWeightKeys >= len) return;
+    const size_t set = (size_t)unit * s.cap;
+    const int key0 = block * kWeightKeys + wave * 64;
+    const bool active = key0 < len;
+    const int row_tiles = (n_rows + kWeightRows - 1) / kWeightRows, share = row_tiles / n_part, more = row_tiles % n_part;
+    const int tile0 = part * share + min(part, more), n_t = share + (part < more ? 1 : 0);
+
+    bf16x8 k[2][D / 16];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+        const uint4* src = (const uint4*)((const uint16_t*)s.k + (set + min(key0 + kb * 32 + l32, len - 1)) * D);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) k[kb][ks] = __builtin_bit_cast(bf16x8, src[ks * 2 + hi]);
+    }
+    int pk = key0 + lane < len ? (POS ? r.row_pos[set + key0 + lane] : 0) : -1, pk_min = pk, pk_max = pk;
+    if constexpr (POS) {
+        pos_lds[wave][lane] = pk;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            pk_min = min(pk_min, __shfl_xor(pk_min, o));
+            pk_max = max(pk_max, __shfl_xor(pk_max, o));
+        }
+    }
+    const bool capped = r.cap2 > 0.f, biased = POS && r.slopes, ragged = key0 + 64 > len;
+    const float cu = capped || biased ? 1.f : r.c2;
+
+    // Query rows of the tile after the next, and what a lane has to know of its row of the next.
+    uint4 piece0, piece1;
+    static_assert(PER <= 2, "pieces of a thread");
+    auto row_of = [&](int rho) __attribute__((always_inline)) { return ((size_t)b * s.T + rho / group) * s.n_q + g * group + rho % group; };
+    auto piece_of = [&](int t, int p) __attribute__((always_inline)) {
+        const int rho = min((tile0 + t) * kWeightRows + p / (D / 8), n_rows - 1);
+        return *(const uint4*)((const uint16_t*)s.q + row_of(rho) * D + p % (D / 8) * 8);
+    };
+    auto request = [&](int t) __attribute__((always_inline)) {
+        piece0 = piece_of(t, tid);
+        if constexpr (PER == 2) piece1 = piece_of(t, 64 * kWeightWaves + tid);
+    };
+    auto put = [&](uint16_t* q, uint4 x, int p) __attribute__((always_inline)) { *(uint4*)(q + k_tile_off<D>(p / (D / 8), p % (D / 8))) = x; };
+    struct Row {
+        float lse, slope2;
+        int pq;
+    };
+    auto row_info = [&](int t) __attribute__((always_inline)) {
+        const int rho = (tile0 + t) * kWeightRows + l32, at = min(rho, n_rows - 1);
+        Row x;
+        x.lse = lse2[(size_t)unit * n_rows + at];
+        x.lse = rho < n_rows && x.lse != -INFINITY ? x.lse : INFINITY;            // (weighs nothing)
+        x.pq = POS ? r.q_pos[b * s.T + at / group] : 0;
+        x.slope2 = POS ? slope_of(r, g * group + at % group) : 0.f;
+        return x;
+    };
+    f32x16 acc[2] = {zero16(), zero16()};
+    if (n_t > 0) {
+        request(0);
+        Row next = row_info(0);
+        for (int t = 0; t < n_t; ++t) {
+            uint16_t* q = q_lds[t & 1];
+            put(q, piece0, tid);
+            if constexpr (PER == 2) put(q, piece1, 64 * kWeightWaves + tid);
+            const Row row = next;
+            request(min(t + 1, n_t - 1));
+            next = row_info(min(t + 1, n_t - 1));
+            __syncthreads();                                  // (the other stage is read by nobody any more: one barrier a tile)
+            if (!active) continue;
+            const Span span = span_of(r, row.pq);
+            bool partial = ragged;
+            if constexpr (POS) {
+                const bool none = (pk_max < span.lo || pk_min > span.hi) && (pk_max < 0 || (unsigned)max(pk_min, 0) >= span.na);
+                if (__builtin_amdgcn_ballot_w64(!none) == 0) continue;
+                const bool all = pk_min >= 0 && ((pk_min >= span.lo && pk_max <= span.hi) || (unsigned)pk_max < span.na);
+                partial = ~__builtin_amdgcn_ballot_w64(all) != 0;
+            }
+            f32x16 x[2] = {zero16(), zero16()};
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+                const bf16x8 a = *(const bf16x8*)(q + k_tile_off<D>(l32, ks * 2 + hi));
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kb][ks], a, x[kb], 0, 0, 0);
+            }
+            if (capped) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    float c[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) c[i] = x[kb][i];
+                    cap_logits(c, r);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[kb][i] = c[i];
+                }
+            }
+            if (partial || biased) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int rq = 0; rq < 4; ++rq) {
+                        int p[4];
+                        if constexpr (POS) {
+                            const int4 p4 = *(const int4*)&pos_lds[wave][kb * 32 + rq * 8 + hi * 4];
+                            p[0] = p4.x; p[1] = p4.y; p[2] = p4.z; p[3] = p4.w;
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) p[i] = key0 + kb * 32 + rq * 8 + hi * 4 + i < len ? 0 : -1;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float y = x[kb][rq * 4 + i];
+                            if (biased) y = fmaf(-row.slope2, (float)abs(row.pq - p[i]), capped ? y : y * r.c2);
+                            acc[kb][rq * 4 + i] += sees(span, p[i]) ? __builtin_amdgcn_exp2f(fmaf(y, cu, -row.lse)) : 0.f;
+                        }
+                    }
+            } else {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[kb][i] += __builtin_amdgcn_exp2f(fmaf(x[kb][i], cu, -row.lse));
+            }
+        }
+    }
+    if (!active) return;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float w = acc[kb][i];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) w += __shfl_xor(w, o);
+            const int key = key0 + acc_key(kb, i, hi);
+            if (l32 != i || key >= len) continue;
+            if (n_part > 1) part_w[((size_t)part * units + unit) * s.cap + key] = w;
+            else weight_out[set + key] = (weight ? weight[set + key] : 0.f) + w;
+        }
+}
+
+// The sum of the parts.
+__global__ __launch_bounds__(256) void weights_sum_kernel(const float* __restrict__ part_w, const int32_t* __restrict__ mix_len, const float* weight,
+                                                          float* weight_out, int units, int n_kv, int cap, int n_part) {
+    const int unit = blockIdx.y, row = blockIdx.x * 256 + threadIdx.x;
+    if (row >= min(mix_len[unit / n_kv], cap)) return;
+    const size_t at = (size_t)unit * cap + row;
+    float w = 0.f;
+    for (int p = 0; p < n_part; ++p) w += part_w[(size_t)p * units * cap + at];
+    weight_out[at] = (weight ? weight[at] : 0.f) + w;
+}
+
 }  // namespace
+
+// Many query rows (ring): estimates in us of a launch of workgroups of 256 and of 128 rows and so many splits.
+static void ring_plan(MixedPlan& p, long long units, long long rows, int D, int l_cap) {
+    const long long tiles = (l_cap + kKeyTile - 1) / kKeyTile;
+    double best = 1e30;
+    for (int nw : {8, 4}) {
+        const long long n_rtile = (rows + 32 * nw - 1) / (32 * nw), base = units * n_rtile;
+        const double tile = nw == 8 ? 1.6 : 1.05;
+        const long long most = std::max<long long>(1, std::min<long long>(tiles, 512 / base));
+        for (long long n = 1; n <= most;) {
+            const long long walk = (tiles + n - 1) / n, rounds = (base * n + 255) / 256;
+            const double mb = 4e-6 * units * n * rows * D;
+            const double us = rounds * (6 + tile * (D == 64 ? 0.6 : 1.0) * walk) + (n > 1 ? 3 + 0.5 * mb : 0);
+            if (us < best) {
+                best = us;
+                p.waves = nw;
+                p.n_split = (int)n;
+            }
+            n = walk > 1 ? (tiles + walk - 2) / (walk - 1) : most + 1;            // the next that shortens the walk
+        }
+    }
+}
 
 MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     MixedPlan p{};
     const long long rows = (long long)(d->n_q_heads / d->n_kv_heads) * T, units = (long long)batch * d->n_kv_heads;
-    p.fits = units <= 65535 && rows <= 1 << 30;
+    const long long key_blocks = (l_cap + kWeightKeys - 1) / kWeightKeys;
+    p.fits = units <= 65535 && rows <= 1 << 30 && (__int128)units * ((rows + 127) / 128) <= INT32_MAX / 2 && units * key_blocks <= INT32_MAX / 64;
     if (!p.fits) return p;
-    p.lse2 = 0;
-    p.total = align_up((size_t)units * rows * sizeof(float), 256);
+    p.n_split = p.n_part = 1;
+    if (d->dtype == VXL_BF16) {
+        ring_plan(p, units, rows, d->head_dim, l_cap);
+        // parts of the query rows: as many as fill rounds of two workgroups on a compute unit
+        const long long row_tiles = (rows + kWeightRows - 1) / kWeightRows, blocks = units * key_blocks;
+        double best = 1e30;
+        for (long long n = 1; n <= std::min<long long>(row_tiles, 16); ++n) {
+            const double us = ((blocks * n + 511) / 512) * (3 + 0.25 * ((row_tiles + n - 1) / n)) + (n > 1 ? 3 : 0);
+            if (us < best) {
+                best = us;
+                p.n_part = (int)n;
+            }
+        }
+    }
+    size_t at = 0;
+    auto put = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
+    p.lse2 = put((size_t)units * rows * sizeof(float));
+    p.part_o = put(p.n_split > 1 ? (size_t)units * p.n_split * rows * d->head_dim * sizeof(float) : 0);
+    p.part_ml = put(p.n_split > 1 ? (size_t)units * p.n_split * rows * sizeof(float2) : 0);
+    p.part_w = put(p.n_part > 1 ? (size_t)p.n_part * units * l_cap * sizeof(float) : 0);
+    p.total = at;
     return p;
 }
 
-vxl_status launch_mixed_attend(const MixedPlan& p, const MixedCall& c, bool force_simple, hipStream_t s) {
+// Workgroups on the XCDs in turn, as place() takes them.
+static dim3 placed_grid(long long all) {
+    const long long xcds = std::min<long long>(all, kXcds), each = (all + xcds - 1) / xcds;
+    return dim3((unsigned)xcds, (unsigned)std::min<long long>(each, 65535), (unsigned)((each + 65534) / 65535));
+}
+
+static vxl_status launch_ring(const MixedPlan& p, const MixedCall& c, const Sets& sets, const Rule& rule, hipStream_t s) {
     const vxl_attn_desc* d = c.d;
-    const vxl_score_rule none{};
-    const vxl_score_rule& u = c.rule ? *c.rule : none;
-    const Rule rule{c.scale * kLog2e, u.softcap > 0.f ? c.scale / u.softcap : 0.f, u.softcap * kLog2e, u.causal, u.window, u.n_always, u.slopes,
-                    c.q_pos, c.row_pos};
-    const Sets sets{c.Qd, c.Kmix, c.Vmix, c.mix_len, c.T, d->n_q_heads, d->n_kv_heads, c.l_cap};
+    const int units = c.batch * d->n_kv_heads, rows = d->n_q_heads / d->n_kv_heads * c.T;
+    const Partials part{(float*)(c.ws + p.part_o), (float2*)(c.ws + p.part_ml)};
+    float* lse2 = (float*)(c.ws + p.lse2);
+    auto run = [&](auto dim, auto nw, auto pos) {
+        using C = RingCfg<dim, nw>;
+        static PerDeviceOnce attr;
+        const vxl_status st = attr.run([&] {
+            VXL_HIP_TRY(hipFuncSetAttribute((const void*)attend_ring_kernel<dim, nw, pos>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES));
+            return VXL_OK;
+        });
+        if (st != VXL_OK) return st;
+        const int n_rtile = (rows + C::ROWS - 1) / C::ROWS;
+        hipLaunchKernelGGL((attend_ring_kernel<dim, nw, pos>), placed_grid((long long)units * p.n_split * n_rtile), dim3(64 * nw), C::LDS_BYTES, s, sets,
+                           rule, part, (uint16_t*)c.O, c.LSE, lse2, units, p.n_split, n_rtile);
+        return mixed_launched();
+    };
+    auto by_pos = [&](auto dim, auto nw) { return rule.q_pos ? run(dim, nw, std::true_type{}) : run(dim, nw, std::false_type{}); };
+    auto by_waves = [&](auto dim) {
+        return p.waves == 8 ? by_pos(dim, std::integral_constant<int, 8>{}) : by_pos(dim, std::integral_constant<int, 4>{});
+    };
+    return d->head_dim == 64 ? by_waves(std::integral_constant<int, 64>{}) : by_waves(std::integral_constant<int, 128>{});
+}
+
+static vxl_status launch_merge(const MixedPlan& p, const MixedCall& c, hipStream_t s) {
+    const vxl_attn_desc* d = c.d;
+    const Partials part{(float*)(c.ws + p.part_o), (float2*)(c.ws + p.part_ml)};
+    const long long all = (long long)c.batch * c.T * d->n_q_heads;
+    return by_storage(d, [&](auto f32, auto dim) {
+        using T = typename Storage<f32>::T;
+        hipLaunchKernelGGL((attend_merge_kernel<f32, dim>), folded_grid(all), dim3(256), 0, s, part, (T*)c.O, c.LSE, (float*)(c.ws + p.lse2), c.T,
+                           d->n_q_heads, d->n_kv_heads, p.n_split, all);
+        return mixed_launched();
+    });
+}
+
+static vxl_status launch_weights(const MixedPlan& p, const MixedCall& c, const Sets& sets, const Rule& rule, hipStream_t s) {
+    const vxl_attn_desc* d = c.d;
+    const int units = c.batch * d->n_kv_heads, n_blocks = (c.l_cap + kWeightKeys - 1) / kWeightKeys;
+    float *lse2 = (float*)(c.ws + p.lse2), *part_w = (float*)(c.ws + p.part_w);
+    auto run = [&](auto dim, auto pos) {
+        hipLaunchKernelGGL((attend_weights_kernel<dim, pos>), placed_grid((long long)units * p.n_part * n_blocks), dim3(64 * kWeightWaves), 0, s, sets,
+                           rule, lse2, c.weight, c.weight_out, part_w, units, p.n_part, n_blocks);
+        return mixed_launched();
+    };
+    auto by_pos = [&](auto dim) { return rule.q_pos ? run(dim, std::true_type{}) : run(dim, std::false_type{}); };
+    const vxl_status st = d->head_dim == 64 ? by_pos(std::integral_constant<int, 64>{}) : by_pos(std::integral_constant<int, 128>{});
+    if (st != VXL_OK || p.n_part == 1) return st;
+    hipLaunchKernelGGL(weights_sum_kernel, dim3((c.l_cap + 255) / 256, units), dim3(256), 0, s, part_w, c.mix_len, c.weight, c.weight_out, units,
+                       d->n_kv_heads, c.l_cap, p.n_part);
+    return mixed_launched();
+}
+
+static vxl_status launch_simple(const MixedPlan& p, const MixedCall& c, const Sets& sets, const Rule& rule, hipStream_t s) {
+    const vxl_attn_desc* d = c.d;
     const long long n_rows = (long long)c.batch * c.T * d->n_q_heads;
     float* lse2 = (float*)(c.ws + p.lse2);
     return by_storage(d, [&](auto f32, auto dim) {
@@ -184,6 +838,20 @@ vxl_status launch_mixed_attend(const MixedPlan& p, const MixedCall& c, bool forc
                            lse2, c.weight, c.weight_out);
         return mixed_launched();
     });
+}
+
+vxl_status launch_mixed_attend(const MixedPlan& p, const MixedCall& c, bool force_simple, hipStream_t s) {
+    const vxl_attn_desc* d = c.d;
+    const vxl_score_rule none{};
+    const vxl_score_rule& u = c.rule ? *c.rule : none;
+    const Rule rule{c.scale * kLog2e, u.softcap > 0.f ? c.scale / u.softcap : 0.f, u.softcap * kLog2e, u.causal, u.window, u.n_always, u.slopes,
+                    c.q_pos, c.row_pos};
+    const Sets sets{c.Qd, c.Kmix, c.Vmix, c.mix_len, c.T, d->n_q_heads, d->n_kv_heads, c.l_cap};
+    if (force_simple || d->dtype != VXL_BF16) return launch_simple(p, c, sets, rule, s);
+    vxl_status st = launch_ring(p, c, sets, rule, s);
+    if (st == VXL_OK && p.n_split > 1) st = launch_merge(p, c, s);
+    if (st == VXL_OK && c.weight_out) st = launch_weights(p, c, sets, rule, s);
+    return st;
 }
 
 }  // namespace vxl

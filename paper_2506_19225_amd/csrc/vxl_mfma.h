@@ -254,7 +254,13 @@ __device__ __forceinline__ void dma16(const void* base, uint32_t off, uint32_t l
                  :: "s"(lds_off), "v"(off), "s"(base) : "memory");
 }
 
-// The same for what is read once: streamed past the caches.
+// 4 bytes per lane, to LDS byte offset lds_off + 4*lane.
+__device__ __forceinline__ void dma4(const void* base, uint32_t off, uint32_t lds_off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                 :: "s"(lds_off), "v"(off), "s"(base) : "memory");
+}
+
+// 16 bytes per lane of what is read once: streamed past the caches.
 __device__ __forceinline__ void dma16_once(const void* base, uint32_t off, uint32_t lds_off) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
                  :: "s"(lds_off), "v"(off), "s"(base) : "memory");

@@ -19,7 +19,12 @@ vxl_status launch_mixed_append(const vxl_attn_desc* d, const vxl_rotary* r, cons
 // ---- attention by position ----
 struct MixedPlan {
     bool fits;                 // the grids of the call are ones that there can be
-    size_t lse2;               // byte offset of the base-2 LSE [batch][Hkv][rows]
+    int waves, n_split;        // of the ring's workgroups; key splits
+    int n_part;                // parts of the query rows in the second pass for the weights
+    // byte offsets into the workspace
+    size_t lse2;               // base-2 LSE [batch][Hkv][rows]
+    size_t part_o, part_ml;    // results of the splits
+    size_t part_w;             // weights of the parts [n_part][batch][Hkv][l_cap]
     size_t total;
 };
 MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap);
