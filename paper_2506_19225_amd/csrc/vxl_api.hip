@@ -439,6 +439,13 @@ int32_t vxl_mixed_kv_capacity(const vxl_layout* L, int32_t k) {
 
 int64_t vxl_prefill_pair_count(const vxl_layout* L) { return L ? L->pair_count : 0; }
 
+// Whether the sizes of a call on mixed sets are ones that its kernels count: a batch and its KV heads in a grid's second dimension, its
+// tokens and query rows in 32 bits, and the rows of a set with a tile behind them too.
+static bool mixed_sizes_ok(const vxl_attn_desc* d, int32_t batch, int32_t tokens, int32_t l_cap) {
+    return l_cap <= INT32_MAX - 4096 && (long long)batch * d->n_kv_heads <= 65535 && (long long)batch * tokens <= INT32_MAX &&
+           (long long)(d->n_q_heads / d->n_kv_heads) * tokens <= 1 << 30;
+}
+
 size_t vxl_workspace_bytes(vxl_op op, const vxl_layout* L, const vxl_attn_desc* d, int32_t batch,
                            int32_t n_q_tokens, int32_t l_cap) {
     vxl_status st;
@@ -468,9 +475,9 @@ size_t vxl_workspace_bytes(vxl_op op, const vxl_layout* L, const vxl_attn_desc* 
             return inplace_workspace(batch, l_cap, kvq_plan(d, batch, n_q_tokens, l_cap).total).total;
         case VXL_OP_MIXED_ATTEND:
             if (batch <= 0 || n_q_tokens <= 0 || l_cap <= 0) return 0;
-            return mixed_plan(d, batch, n_q_tokens, l_cap).total;
+            return mixed_sizes_ok(d, batch, n_q_tokens, l_cap) ? mixed_plan(d, batch, n_q_tokens, l_cap).total : 0;
         case VXL_OP_MIXED_EVICT:
-            if (batch <= 0 || l_cap <= 0) return 0;
+            if (batch <= 0 || l_cap <= 0 || !mixed_sizes_ok(d, batch, 1, l_cap)) return 0;
             return evict_plan(d, batch, l_cap).total;
     }
     return 0;
@@ -867,13 +874,6 @@ static size_t mixed_bytes(const vxl_attn_desc* d, int32_t batch, int32_t rows) {
 }
 static size_t row_bytes(const vxl_attn_desc* d, int32_t batch, int32_t rows) { return (size_t)batch * d->n_kv_heads * rows * sizeof(float); }
 
-// Whether the sizes of a call on mixed sets are ones that its kernels count: a batch and its KV heads in a grid's second dimension, its
-// tokens and query rows in 32 bits, its elements far below 64.
-static bool mixed_sizes_ok(const vxl_attn_desc* d, int32_t batch, int32_t tokens) {
-    return (long long)batch * d->n_kv_heads <= 65535 && (long long)batch * tokens <= INT32_MAX &&
-           (long long)(d->n_q_heads / d->n_kv_heads) * tokens <= 1 << 30;
-}
-
 vxl_status vxl_mixed_append(const vxl_attn_desc* d, const vxl_rotary* r, const int32_t* positions, int32_t batch, int32_t n_new, const void* Q,
                             const void* K, const void* V, void* Qd, void* Kmix, void* Vmix, int32_t l_cap, const int32_t* mix_len,
                             int32_t* row_pos, float* row_weight, vxl_stream stream) {
@@ -884,7 +884,7 @@ vxl_status vxl_mixed_append(const vxl_attn_desc* d, const vxl_rotary* r, const i
         if (!p || !aligned16(p)) return VXL_ERR_INVALID_ARG;
     for (const void* p : {(const void*)positions, (const void*)mix_len, (const void*)row_pos, (const void*)row_weight})
         if (!aligned4(p)) return VXL_ERR_INVALID_ARG;
-    if (!mixed_sizes_ok(d, batch, n_new)) return VXL_ERR_UNSUPPORTED;
+    if (!mixed_sizes_ok(d, batch, n_new, l_cap)) return VXL_ERR_UNSUPPORTED;
     const int n = batch * n_new;
     const size_t set = mixed_bytes(d, batch, l_cap), rows = row_bytes(d, batch, l_cap);
     const Range out[] = {range(Qd, (size_t)n * d->n_q_heads * d->head_dim * elem_bytes(d)), range(Kmix, set), range(Vmix, set),
@@ -919,8 +919,9 @@ vxl_status vxl_mixed_attend(const vxl_attn_desc* d, const vxl_score_rule* rule, 
         if (rule->softcap > 0.f && !std::isfinite(scale / rule->softcap)) return VXL_ERR_INVALID_ARG;
         if ((rule->causal || rule->window || rule->slopes) && !q_pos) return VXL_ERR_INVALID_ARG;
     }
-    if (!mixed_sizes_ok(d, batch, n_q_tokens)) return VXL_ERR_UNSUPPORTED;
+    if (!mixed_sizes_ok(d, batch, n_q_tokens, l_cap)) return VXL_ERR_UNSUPPORTED;
     const MixedPlan p = mixed_plan(d, batch, n_q_tokens, l_cap);
+    if (!p.fits) return VXL_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < p.total || !aligned16(workspace)) return VXL_ERR_WORKSPACE;
     const size_t q_rows = (size_t)batch * n_q_tokens * d->n_q_heads, q_bytes = q_rows * d->head_dim * elem_bytes(d);
     const size_t set = mixed_bytes(d, batch, l_cap), rows = row_bytes(d, batch, l_cap);
@@ -945,7 +946,7 @@ vxl_status vxl_mixed_evict(const vxl_attn_desc* d, const void* Kmix, const void*
     for (const void* p : {(const void*)mix_len, (const void*)weight, (const void*)row_pos, (const void*)weight_out, (const void*)pos_out, (const void*)kept})
         if (!p || !aligned4(p)) return VXL_ERR_INVALID_ARG;
     if ((n_recent > 0 && !newest) || !aligned4(newest)) return VXL_ERR_INVALID_ARG;
-    if (!mixed_sizes_ok(d, batch, 1)) return VXL_ERR_UNSUPPORTED;
+    if (!mixed_sizes_ok(d, batch, 1, std::max(l_cap, out_cap))) return VXL_ERR_UNSUPPORTED;
     const EvictPlan p = evict_plan(d, batch, l_cap);
     if (!workspace || workspace_bytes < p.total || !aligned16(workspace)) return VXL_ERR_WORKSPACE;
     const bool in_place = Kout == Kmix;

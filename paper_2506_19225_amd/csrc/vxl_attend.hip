@@ -65,18 +65,19 @@ __device__ __forceinline__ float exact_logit(const Rule& r, float dot, float slo
     return y;
 }
 
+// (rows [lo, hi), `width` <= 64 of every `step`)
 template <typename T, int D>
-__device__ __forceinline__ void exact_row(const Rule& r, const float* q, const T* k, const T* v, const int32_t* pos, int lo, int hi, int pq,
-                                          float slope2, float& m, float& l, float (&acc)[D / 64]) {
+__device__ __forceinline__ void exact_row(const Rule& r, const float* q, const T* k, const T* v, const int32_t* pos, int lo, int hi, int width,
+                                          int step, int pq, float slope2, float& m, float& l, float (&acc)[D / 64]) {
     const int lane = threadIdx.x & 63;
     const Span span = span_of(r, pq);
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
     for (int x = 0; x < D / 64; ++x) acc[x] = 0.f;
-    for (int base = lo; base < hi; base += 64) {
+    for (int base = lo; base < hi; base += step) {
         const int row = base + lane;
-        const int pk = row < hi ? (pos ? pos[row] : 0) : -1;
+        const int pk = row < hi && lane < width ? (pos ? pos[row] : 0) : -1;
         float y = -INFINITY;
         if (sees(span, pk)) y = exact_logit(r, dot_row<T, D>(q, k + (size_t)row * D), slope2, pq, pk);
         float m_new = y;
@@ -89,7 +90,7 @@ __device__ __forceinline__ void exact_row(const Rule& r, const float* q, const T
         l = l * alpha + sum;
 #pragma unroll
         for (int x = 0; x < D / 64; ++x) acc[x] = acc[x] == 0.f ? 0.f : acc[x] * alpha;
-        for (int j = 0; j < 64; ++j) {
+        for (int j = 0; j < width; ++j) {
             const float pj = __shfl(p, j);
             if (pj == 0.f) continue;
             const T* vr = v + (size_t)(base + j) * D;
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(256) void simple_attend_kernel(Sets s, Rule r, void
     const int len = min(max(s.len[b], 0), s.cap), pq = r.q_pos ? r.q_pos[b * s.T + t] : 0;
     const size_t set = ((size_t)b * s.n_kv + g) * s.cap;
     float m, l, acc[D / 64];
-    exact_row<T, D>(r, q_lds[wave], (const T*)s.k + set * D, (const T*)s.v + set * D, r.row_pos ? r.row_pos + set : nullptr, 0, len, pq,
+    exact_row<T, D>(r, q_lds[wave], (const T*)s.k + set * D, (const T*)s.v + set * D, r.row_pos ? r.row_pos + set : nullptr, 0, len, 64, 64, pq,
                     slope_of(r, h), m, l, acc);
 #pragma unroll
     for (int x = 0; x < D / 64; ++x) store_as((T*)O + row * D + lane + 64 * x, l == 0.f ? 0.f : acc[x] / l);
@@ -457,7 +458,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_ring_kernel(Sets s, Rule r,
         for (int x = lane; x < D; x += 64) q_row[x] = as_float(((const uint16_t*)s.q)[out * D + x]);
         __builtin_amdgcn_wave_barrier();
         float m, l2, acc[D / 64];
-        exact_row<uint16_t, D>(r, q_row, kset, vset, r.row_pos ? r.row_pos + set : nullptr, k_lo, k_hi, r.q_pos ? r.q_pos[b * s.T + t] : 0,
+        exact_row<uint16_t, D>(r, q_row, kset, vset, r.row_pos ? r.row_pos + set : nullptr, k_lo, k_hi, 64, 64, r.q_pos ? r.q_pos[b * s.T + t] : 0,
                                slope_of(r, hq), m, l2, acc);
 #pragma unroll
         for (int x = 0; x < D / 64; ++x) {
@@ -476,27 +477,250 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_ring_kernel(Sets s, Rule r,
     }
 }
 
-// The merge of the splits, one workgroup per query row: SG groups of D / 4 lanes take every SG-th split, four requested together, and are
+// Of a part with reference and sum ml, against a reference: its weight in the whole, 0 if it has none, whatever it holds (and then nothing of
+// it is added); 1 if its sum is not a number, which the whole then is not either.
+__device__ __forceinline__ float part_weight(float2 ml, float ref) {
+    return ml.y == 0.f ? 0.f : ml.y != ml.y ? 1.f : __builtin_amdgcn_exp2f(ml.x - ref);
+}
+__device__ __forceinline__ float add_part(float f, float x, float sum) { return f == 0.f ? sum : fmaf(f, x, sum); }
+
+// ------------------------------------------------------------------------------------------
+// At most 32 stacked query rows, the generated tokens: bound by memory, or by latency.  Every wave walks 32-key tiles of its own, in turn with
+// the other waves of all splits, from two pairs of LDS areas filled by direct loads and counted by hand; the waves' (reference, sum,
+// O) are merged through LDS.  The logits, in units of log 2, are kept in the workspace (4 bytes per query row and key beside 4 D of key and
+// value), so that the weights need no second pass over the keys: -inf where the row is not seen, kLowest for a seen one of -inf.
+// ------------------------------------------------------------------------------------------
+constexpr int kStepTile = 32, kStepWaves = 4, kStepRows = 32;
+
+template <int D>
+struct StepCfg {
+    static constexpr int TILE = kStepTile * D, AREA = 2 * 2 * TILE;               // elements: of a tile, of a wave's two pairs
+    static constexpr int POS_AT = kStepWaves * AREA * 2, LDS_BYTES = POS_AT + kStepWaves * 2 * 64 * 4;
+    static constexpr int PPR = D / 8, RPI = 64 / PPR, NL = kStepTile / RPI;       // pieces of a row; rows, loads of a tile
+};
+
+template <int D, bool POS>
+__global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s, Rule r, Partials part, uint16_t* __restrict__ O, float* __restrict__ LSE,
+                                                                         float* __restrict__ logits, int stride, int n_split) {
+    using C = StepCfg<D>;
+    constexpr int NW = kStepWaves, TK = kStepTile, PPR = C::PPR, NL = C::NL;
+    extern __shared__ __attribute__((aligned(16))) uint16_t lds[];
+    __shared__ float2 stats[NW][kStepRows];
+    __shared__ __attribute__((aligned(16))) float q_lds[NW][D];                   // (of rows made again)
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int split = blockIdx.x, unit = blockIdx.y, g = unit % s.n_kv, b = unit / s.n_kv, group = s.n_q / s.n_kv, n_rows = group * s.T;
+    const size_t set = (size_t)unit * s.cap;
+    const uint16_t *kset = (const uint16_t*)s.k + set * D, *vset = (const uint16_t*)s.v + set * D;
+    const int32_t* pos = POS ? r.row_pos + set : nullptr;
+    uint16_t* const area = lds + wave * C::AREA;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
+    const uint32_t lds_w = lds_base + wave * (C::AREA * 2), lds_pos = lds_base + C::POS_AT + wave * (2 * 64 * 4);
+    const int tile0 = split * NW + wave, every = n_split * NW;                    // the wave's tiles: tile0, tile0 + every, ...
+    const int r_in = lane / PPR, pp = lane % PPR;
+
+    // `rows`: rows that may be read, the capacity for the first request, which does not wait for the length
+    auto request = [&](int tile, int buf, int rows) __attribute__((always_inline)) {
+        const int key0 = tile * TK, rlim = min(TK - 1, rows - 1 - key0);
+        const char *kb = (const char*)(kset + (size_t)key0 * D), *vb = (const char*)(vset + (size_t)key0 * D);
+#pragma unroll
+        for (int x = 0; x < NL; ++x) {
+            const int row = x * C::RPI + r_in;
+            const int kp = pp ^ ((row / (16 / PPR)) & (PPR - 1));
+            constexpr int CPR = D * 2 / 64, RPL = D == 128 ? 1 : 2;
+            const int vp = (((pp >> 2) ^ ((row / RPL) & (CPR - 1))) << 2) | (pp & 3);
+            const uint32_t kdst = lds_w + (uint32_t)buf * (4 * C::TILE) + x * 1024, roff = (uint32_t)min(row, rlim) * (D * 2);
+            dma16(kb, roff + kp * 16, kdst);
+            dma16(vb, roff + vp * 16, kdst + 2 * C::TILE);
+        }
+        if constexpr (POS) dma4(pos + key0, (uint32_t)min(lane, rlim) * 4, lds_pos + buf * 256);
+    };
+    constexpr int LOADS = 2 * NL + (POS ? 1 : 0);
+    if (tile0 * TK < s.cap) request(tile0, 0, s.cap);
+
+    const int rho = min(l32, n_rows - 1), tok = rho / group, h = g * group + rho % group;
+    bf16x8 qreg[1][D / 16];
+    {
+        const uint4* src = (const uint4*)((const uint16_t*)s.q + (((size_t)b * s.T + tok) * s.n_q + h) * D);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) qreg[0][ks] = __builtin_bit_cast(bf16x8, src[ks * 2 + hi]);
+    }
+    const int pq = POS ? r.q_pos[b * s.T + tok] : 0;
+    const float slope2 = POS ? slope_of(r, h) : 0.f;
+    const int len = min(max(s.len[b], 0), s.cap);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {                     // complete here, with the older request of the first tile
+        typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+        asm volatile("" :: "v"(__builtin_bit_cast(u32x4, qreg[0][ks])));
+    }
+    asm volatile("" :: "v"(pq), "v"(slope2), "v"(len));
+    wait_vmcnt<0>();
+    const Span span = span_of(r, pq);
+    const int n_tiles = (len + TK - 1) / TK, n = tile0 < n_tiles ? (n_tiles - tile0 + every - 1) / every : 0;
+    // Rows past the length may hold anything (0 * NaN): the one tile that straddles it is fetched again, its rows the last one.
+    if (n > 0 && tile0 * TK + TK > len) {
+        request(tile0, 0, len);
+        wait_vmcnt<0>();
+    }
+    f32x16 o[1][D / 32];
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) o[0][db] = zero16();
+    const bool capped = r.cap2 > 0.f, biased = POS && r.slopes;
+    const float cu = capped || biased ? 1.f : r.c2;
+    float m_run = -INFINITY, mc_run = kLowest, l_run = 0.f;
+    float* const kept = logits ? logits + ((size_t)unit * n_rows + rho) * stride : nullptr;
+
+    if (n > 1) request(tile0 + every, 1, len);
+    for (int i = 0; i < n; ++i) {
+        const int tile = tile0 + i * every, left = len - tile * TK;
+        if (i >= 1) {
+            const bool more = i + 1 < n;
+            if (more) request(tile + every, (i + 1) & 1, len);
+            if (more) wait_vmcnt<LOADS>(); else wait_vmcnt<0>();                 // tile i has landed
+        }
+        __builtin_amdgcn_wave_barrier();
+        const uint16_t *kt = area + (i & 1) * 2 * C::TILE, *vt = kt + C::TILE;
+        const int32_t* tile_pos = (const int32_t*)((const char*)lds + C::POS_AT) + (wave * 2 + (i & 1)) * 64;
+        f32x16 x[1][1];
+        qk_tile<D, 1, 1>(kt, qreg, l32, hi, x);
+        float y[16], seen[16];                                // logits; the same as kept for the weights
+#pragma unroll
+        for (int j = 0; j < 16; ++j) y[j] = x[0][0][j];
+        if (capped) cap_logits(y, r);
+#pragma unroll
+        for (int jq = 0; jq < 4; ++jq) {
+            int p[4] = {0, 0, 0, 0};
+            if constexpr (POS) {
+                const int4 p4 = *(const int4*)(tile_pos + jq * 8 + hi * 4);
+                p[0] = p4.x; p[1] = p4.y; p[2] = p4.z; p[3] = p4.w;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = jq * 4 + e;
+                if (biased) y[j] = fmaf(-slope2, (float)abs(pq - p[e]), capped ? y[j] : y[j] * r.c2);
+                const bool sees_it = sees(span, p[e]) && acc_key(0, j, hi) < left;
+                const float kept_as = y[j] * cu;
+                seen[j] = !sees_it ? -INFINITY : kept_as == -INFINITY ? kLowest : kept_as;
+                y[j] = sees_it ? y[j] : -INFINITY;
+            }
+            if (kept && l32 < n_rows)
+                *(float4*)(kept + tile * TK + jq * 8 + hi * 4) = make_float4(seen[jq * 4], seen[jq * 4 + 1], seen[jq * 4 + 2], seen[jq * 4 + 3]);
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) top = fmaxf(top, y[j]);
+        if (__builtin_amdgcn_ballot_w64(fmaf(top, cu, -mc_run) > 8.f) != 0) {
+            const float m_new = fmaxf(m_run, fmaxf(top, __shfl_xor(top, 32)));
+            const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run - m_new) * cu);
+            l_run *= alpha;
+            m_run = m_new;
+            mc_run = fmaxf(m_new * cu, kLowest);
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[0][db][j] *= alpha;
+        }
+        bf16x8 pb[1][1][2];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(y[j], cu, -mc_run));
+            l_run += p;
+            pb[0][0][j >> 3][j & 7] = (__bf16)p;
+        }
+        pv_tile<D, 1, 1>(vt, pb, lane, o);
+        __builtin_amdgcn_wave_barrier();
+    }
+    wait_vmcnt<0>();                                           // (a wave without tiles: its request of the first one)
+
+    // ---- merge the waves: 16-byte piece c of a row lies at c ^ row (mod the pieces) of the wave's area, which is free now ----
+    static_assert(kStepRows * D * 4 <= C::AREA * 2, "the merge fits a wave's area");
+    constexpr int PPR4 = D / 4;
+    float* red = (float*)area;
+    const float l = l_run + __shfl_xor(l_run, 32);
+    bool odd = false;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) odd |= !(fabsf(o[0][db][j]) < INFINITY);
+    unsigned long long again = __builtin_amdgcn_ballot_w64(odd && l32 < n_rows);
+    again = (again | again >> 32) & 0xffffffffull;
+    if (l32 < n_rows && !(again >> l32 & 1)) {
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int rq = 0; rq < 4; ++rq)
+                *(float4*)(red + (l32 * PPR4 + ((db * 8 + rq * 2 + hi) ^ (l32 & (PPR4 - 1)))) * 4) =
+                    make_float4(o[0][db][rq * 4], o[0][db][rq * 4 + 1], o[0][db][rq * 4 + 2], o[0][db][rq * 4 + 3]);
+        if (hi == 0) stats[wave][l32] = make_float2(l == 0.f ? -INFINITY : mc_run, l);
+    }
+    while (again) {                                            // (uniform in the wave)
+        const int row = __builtin_ctzll(again);
+        again &= again - 1;
+        const int t = row / group, hq = g * group + row % group;
+        __builtin_amdgcn_wave_barrier();
+        for (int x = lane; x < D; x += 64) q_lds[wave][x] = as_float(((const uint16_t*)s.q)[(((size_t)b * s.T + t) * s.n_q + hq) * D + x]);
+        __builtin_amdgcn_wave_barrier();
+        float m, l2, acc[D / 64];
+        exact_row<uint16_t, D>(r, q_lds[wave], kset, vset, r.row_pos ? r.row_pos + set : nullptr, tile0 * TK, len, TK, every * TK,
+                               r.q_pos ? r.q_pos[b * s.T + t] : 0, slope_of(r, hq), m, l2, acc);
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) {
+            const int d = lane + 64 * x;
+            red[(row * PPR4 + ((d >> 2) ^ (row & (PPR4 - 1)))) * 4 + (d & 3)] = acc[x];
+        }
+        if (lane == 0) stats[wave][row] = make_float2(m, l2);
+    }
+    __syncthreads();
+    const size_t part_row0 = ((size_t)unit * n_split + split) * n_rows;
+    for (int e = tid; e < n_rows * PPR4; e += 64 * NW) {
+        const int row = e / PPR4, c = e % PPR4;
+        float2 st[NW];
+        float M = -INFINITY, L = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            st[w] = stats[w][row];
+            M = fmaxf(M, st[w].x);
+        }
+        const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float4 v = *(const float4*)((const float*)(lds + w * C::AREA) + (row * PPR4 + (c ^ (row & (PPR4 - 1)))) * 4);
+            const float f = part_weight(st[w], ref);
+            L = add_part(f, st[w].y, L);
+            a[0] = add_part(f, v.x, a[0]); a[1] = add_part(f, v.y, a[1]); a[2] = add_part(f, v.z, a[2]); a[3] = add_part(f, v.w, a[3]);
+        }
+        if (c == 0) part.ml[part_row0 + row] = make_float2(M, L);
+        if (n_split > 1) {
+            *(float4*)(part.o + (part_row0 + row) * D + c * 4) = make_float4(a[0], a[1], a[2], a[3]);
+        } else {
+            const size_t out = ((size_t)b * s.T + row / group) * s.n_q + g * group + row % group;
+            __attribute__((aligned(8))) uint16_t v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = f32_to_bf16(L == 0.f ? 0.f : a[j] / L);
+            *(uint2*)(O + out * D + c * 4) = *(const uint2*)v;
+            if (LSE && c == 0) LSE[out] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
+        }
+    }
+}
+
+// The merge of the splits of one query row by a workgroup: SG groups of D / 4 lanes take every SG-th split, four requested together, and are
 // folded through LDS in their order.
 template <bool F32, int D>
-__global__ __launch_bounds__(256) void attend_merge_kernel(Partials part, typename Storage<F32>::T* __restrict__ O, float* __restrict__ LSE,
-                                                           float* __restrict__ lse2, int T, int n_q, int n_kv, int n_split, long long all) {
+struct MergeArea {
+    static constexpr int NV = D / 4, SG = 256 / NV;
+    __attribute__((aligned(16))) float red[SG][D];
+    float2 stat[SG];
+};
+template <bool F32, int D>
+__device__ __forceinline__ void merge_row(MergeArea<F32, D>& area, const Partials& part, typename Storage<F32>::T* O, float* LSE, float* lse2,
+                                          int T, int n_q, int n_kv, int n_split, long long id) {
     constexpr int NV = D / 4, SG = 256 / NV, U = 4;
-    __shared__ __attribute__((aligned(16))) float red[SG][D];
-    __shared__ float2 stat[SG];
     const int group = n_q / n_kv, n_rows = T * group, sg = threadIdx.x / NV, d = threadIdx.x % NV * 4;
-    const long long id = folded_id();
-    if (id >= all) return;
     const int rho = (int)(id % n_rows);
     const long long unit = id / n_rows;
     const int g = (int)(unit % n_kv), b = (int)(unit / n_kv);
     const size_t base = (size_t)unit * n_split * n_rows + rho;
     float M = -INFINITY, L = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
-    // (a part without weight counts for nothing, whatever it holds; a sum that is not a number stays one)
-    auto part_weight = [](float2 ml, float ref) __attribute__((always_inline)) {
-        return ml.y == 0.f ? 0.f : ml.y != ml.y ? 1.f : __builtin_amdgcn_exp2f(ml.x - ref);
-    };
-    auto add = [](float f, float x, float y) __attribute__((always_inline)) { return f == 0.f ? y : fmaf(f, x, y); };
     for (int s0 = sg; s0 < n_split; s0 += U * SG) {
         float2 ml[U];
         float4 v[U];
@@ -509,7 +733,7 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(Partials part, typena
         float m_new = M;
 #pragma unroll
         for (int u = 0; u < U; ++u) m_new = fmaxf(m_new, ml[u].x);
-        const float ref = m_new == -INFINITY ? 0.f : m_new, f0 = L == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - ref);
+        const float ref = m_new == -INFINITY ? 0.f : m_new, f0 = part_weight(make_float2(M, L), ref);
         M = m_new;
         L *= f0;
 #pragma unroll
@@ -517,33 +741,106 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(Partials part, typena
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const float f = s0 + u * SG < n_split ? part_weight(ml[u], ref) : 0.f;
-            L = add(f, ml[u].y, L);
-            a[0] = add(f, v[u].x, a[0]); a[1] = add(f, v[u].y, a[1]); a[2] = add(f, v[u].z, a[2]); a[3] = add(f, v[u].w, a[3]);
+            L = add_part(f, ml[u].y, L);
+            a[0] = add_part(f, v[u].x, a[0]); a[1] = add_part(f, v[u].y, a[1]); a[2] = add_part(f, v[u].z, a[2]); a[3] = add_part(f, v[u].w, a[3]);
         }
     }
-    *(float4*)&red[sg][d] = make_float4(a[0], a[1], a[2], a[3]);
-    if (d == 0) stat[sg] = make_float2(M, L);
+    *(float4*)&area.red[sg][d] = make_float4(a[0], a[1], a[2], a[3]);
+    if (d == 0) area.stat[sg] = make_float2(M, L);
     __syncthreads();
     if (threadIdx.x >= D) return;                             // a column each
     M = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < SG; ++i) M = fmaxf(M, stat[i].x);
+    for (int i = 0; i < SG; ++i) M = fmaxf(M, area.stat[i].x);
     const float ref = M == -INFINITY ? 0.f : M;
     float sum = 0.f;
     L = 0.f;
 #pragma unroll
     for (int i = 0; i < SG; ++i) {
-        const float f = part_weight(stat[i], ref);
-        L = add(f, stat[i].y, L);
-        sum = add(f, red[i][threadIdx.x], sum);
+        const float f = part_weight(area.stat[i], ref);
+        L = add_part(f, area.stat[i].y, L);
+        sum = add_part(f, area.red[i][threadIdx.x], sum);
     }
     const size_t row = ((size_t)b * T + rho / group) * n_q + g * group + rho % group;
     store_as(O + row * D + threadIdx.x, L == 0.f ? 0.f : sum / L);
     if (threadIdx.x == 0) {
         const float y = L == 0.f ? -INFINITY : M + __builtin_amdgcn_logf(L);
         if (LSE) LSE[row] = y * kLn2;
-        lse2[id] = y;
+        if (lse2) lse2[id] = y;
     }
+}
+
+template <bool F32, int D>
+__global__ __launch_bounds__(256) void attend_merge_kernel(Partials part, typename Storage<F32>::T* __restrict__ O, float* __restrict__ LSE,
+                                                           float* __restrict__ lse2, int T, int n_q, int n_kv, int n_split, long long all) {
+    __shared__ MergeArea<F32, D> area;
+    const long long id = folded_id();
+    if (id < all) merge_row<F32, D>(area, part, O, LSE, lse2, T, n_q, n_kv, n_split, id);
+}
+
+// What follows on the kernels that keep their logits: the first n_merge workgroups merge the splits of a query row, the others add up the
+// weights of 1,024 rows of a set, each with the LSE of its (at most R) query rows made from the splits' sums again.  One launch instead of
+// two, and neither part waits for the other.
+template <bool F32, int D, int R>
+__global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typename Storage<F32>::T* __restrict__ O, float* __restrict__ LSE,
+                                                            const float* __restrict__ logits, const int32_t* __restrict__ mix_len,
+                                                            const float* weight, float* weight_out, int T, int n_q, int n_kv, int cap, int stride,
+                                                            int n_split, int n_merge, int n_blocks, long long all) {
+    __shared__ MergeArea<F32, D> area;
+    __shared__ float2 ml_lds[256 / R][R];
+    __shared__ float lse_lds[R];
+    long long id = folded_id();
+    if (id >= all) return;
+    if (id < n_merge) {
+        merge_row<F32, D>(area, part, O, LSE, nullptr, T, n_q, n_kv, n_split, id);
+        return;
+    }
+    id -= n_merge;
+    const int unit = (int)(id / n_blocks), key = ((int)(id % n_blocks) * 256 + (int)threadIdx.x) * 4, n_rows = n_q / n_kv * T;
+    const int len = min(max(mix_len[unit / n_kv], 0), cap);
+    if ((int)(id % n_blocks) * 1024 >= len) return;
+    const float* y = logits + (size_t)unit * n_rows * stride + min(key, (len - 1) / 4 * 4);
+    float4 first[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) first[i] = *(const float4*)(y + (size_t)min(i, n_rows - 1) * stride);
+    // LSE of the query rows: R threads each take every (256 / R)-th split
+    constexpr int SG = 256 / R;
+    const int row = threadIdx.x % R, sg = threadIdx.x / R;
+    float M = -INFINITY, L = 0.f;
+    for (int sp = sg; sp < n_split; sp += SG) {
+        const float2 ml = part.ml[((size_t)unit * n_split + sp) * n_rows + min(row, n_rows - 1)];
+        const float m_new = fmaxf(M, ml.x), ref = m_new == -INFINITY ? 0.f : m_new;
+        L = L * part_weight(make_float2(M, L), ref);
+        L = add_part(part_weight(ml, ref), ml.y, L);
+        M = m_new;
+    }
+    ml_lds[sg][row] = make_float2(M, L);
+    __syncthreads();
+    if (threadIdx.x < R) {
+        M = -INFINITY;
+        L = 0.f;
+        for (int i = 0; i < SG; ++i) M = fmaxf(M, ml_lds[i][row].x);
+        const float ref = M == -INFINITY ? 0.f : M;
+        for (int i = 0; i < SG; ++i) L = add_part(part_weight(ml_lds[i][row], ref), ml_lds[i][row].y, L);
+        lse_lds[row] = L == 0.f || row >= n_rows ? INFINITY : M + __builtin_amdgcn_logf(L);          // (weighs nothing)
+    }
+    __syncthreads();
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](float4 v, float lse) __attribute__((always_inline)) {
+        const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] += x[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[j] - lse);
+    };
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n_rows) add(first[i], lse_lds[i]);
+    if constexpr (R > 8)
+#pragma unroll 4
+        for (int i = 8; i < n_rows; ++i) add(*(const float4*)(y + (size_t)i * stride), lse_lds[i]);
+    const size_t set = (size_t)unit * cap;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (key + j < len) weight_out[set + key + j] = (weight ? weight[set + key + j] : 0.f) + w[j];
 }
 
 // ------------------------------------------------------------------------------------------
@@ -743,7 +1040,12 @@ MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     p.fits = units <= 65535 && rows <= 1 << 30 && (__int128)units * ((rows + 127) / 128) <= INT32_MAX / 2 && units * key_blocks <= INT32_MAX / 64;
     if (!p.fits) return p;
     p.n_split = p.n_part = 1;
-    if (d->dtype == VXL_BF16) {
+    p.stride = (l_cap + kStepTile - 1) / kStepTile * kStepTile;
+    p.few = d->dtype == VXL_BF16 && rows <= kStepRows;
+    if (p.few) {
+        const long long tiles = (l_cap + kStepTile - 1) / kStepTile;
+        p.n_split = (int)std::max<long long>(1, std::min<long long>((tiles + kStepWaves - 1) / kStepWaves, 256 / units));
+    } else if (d->dtype == VXL_BF16) {
         ring_plan(p, units, rows, d->head_dim, l_cap);
         // parts of the query rows: as many as fill rounds of two workgroups on a compute unit
         const long long row_tiles = (rows + kWeightRows - 1) / kWeightRows, blocks = units * key_blocks;
@@ -760,7 +1062,8 @@ MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     auto put = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
     p.lse2 = put((size_t)units * rows * sizeof(float));
     p.part_o = put(p.n_split > 1 ? (size_t)units * p.n_split * rows * d->head_dim * sizeof(float) : 0);
-    p.part_ml = put(p.n_split > 1 ? (size_t)units * p.n_split * rows * sizeof(float2) : 0);
+    p.part_ml = put(p.n_split > 1 || p.few ? (size_t)units * p.n_split * rows * sizeof(float2) : 0);
+    p.logits = put(p.few ? (size_t)units * rows * p.stride * sizeof(float) : 0);
     p.part_w = put(p.n_part > 1 ? (size_t)p.n_part * units * l_cap * sizeof(float) : 0);
     p.total = at;
     return p;
@@ -795,6 +1098,38 @@ static vxl_status launch_ring(const MixedPlan& p, const MixedCall& c, const Sets
         return p.waves == 8 ? by_pos(dim, std::integral_constant<int, 8>{}) : by_pos(dim, std::integral_constant<int, 4>{});
     };
     return d->head_dim == 64 ? by_waves(std::integral_constant<int, 64>{}) : by_waves(std::integral_constant<int, 128>{});
+}
+
+// One row per merging workgroup, 1,024 rows of a set per workgroup of the weights.
+static vxl_status launch_step(const MixedPlan& p, const MixedCall& c, const Sets& sets, const Rule& rule, hipStream_t s) {
+    const vxl_attn_desc* d = c.d;
+    const int units = c.batch * d->n_kv_heads, rows = d->n_q_heads / d->n_kv_heads * c.T;
+    const Partials part{(float*)(c.ws + p.part_o), (float2*)(c.ws + p.part_ml)};
+    float* logits = c.weight_out ? (float*)(c.ws + p.logits) : nullptr;
+    auto run = [&](auto dim, auto pos) {
+        using C = StepCfg<dim>;
+        static PerDeviceOnce attr;
+        vxl_status st = attr.run([&] {
+            VXL_HIP_TRY(hipFuncSetAttribute((const void*)attend_step_kernel<dim, pos>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES));
+            return VXL_OK;
+        });
+        if (st != VXL_OK) return st;
+        hipLaunchKernelGGL((attend_step_kernel<dim, pos>), dim3(p.n_split, units), dim3(64 * kStepWaves), C::LDS_BYTES, s, sets, rule, part,
+                           (uint16_t*)c.O, c.LSE, logits, p.stride, p.n_split);
+        st = mixed_launched();
+        if (st != VXL_OK || (p.n_split == 1 && !logits)) return st;
+        const long long n_merge = p.n_split > 1 ? (long long)units * rows : 0, n_blocks = logits ? (c.l_cap + 1023) / 1024 : 0;
+        const long long all = n_merge + units * n_blocks;
+        auto finish = [&](auto most) {
+            hipLaunchKernelGGL((attend_finish_kernel<false, dim, most>), folded_grid(all), dim3(256), 0, s, part, (uint16_t*)c.O, c.LSE, logits, c.mix_len,
+                               c.weight, c.weight_out, c.T, d->n_q_heads, d->n_kv_heads, c.l_cap, p.stride, p.n_split, (int)n_merge, (int)n_blocks, all);
+        };
+        if (rows <= 8) finish(std::integral_constant<int, 8>{});
+        else finish(std::integral_constant<int, 32>{});
+        return mixed_launched();
+    };
+    auto by_pos = [&](auto dim) { return rule.q_pos ? run(dim, std::true_type{}) : run(dim, std::false_type{}); };
+    return d->head_dim == 64 ? by_pos(std::integral_constant<int, 64>{}) : by_pos(std::integral_constant<int, 128>{});
 }
 
 static vxl_status launch_merge(const MixedPlan& p, const MixedCall& c, hipStream_t s) {
@@ -848,6 +1183,7 @@ vxl_status launch_mixed_attend(const MixedPlan& p, const MixedCall& c, bool forc
                     c.q_pos, c.row_pos};
     const Sets sets{c.Qd, c.Kmix, c.Vmix, c.mix_len, c.T, d->n_q_heads, d->n_kv_heads, c.l_cap};
     if (force_simple || d->dtype != VXL_BF16) return launch_simple(p, c, sets, rule, s);
+    if (p.few) return launch_step(p, c, sets, rule, s);
     vxl_status st = launch_ring(p, c, sets, rule, s);
     if (st == VXL_OK && p.n_split > 1) st = launch_merge(p, c, s);
     if (st == VXL_OK && c.weight_out) st = launch_weights(p, c, sets, rule, s);

@@ -20,10 +20,13 @@ vxl_status launch_mixed_append(const vxl_attn_desc* d, const vxl_rotary* r, cons
 struct MixedPlan {
     bool fits;                 // the grids of the call are ones that there can be
     int waves, n_split;        // of the ring's workgroups; key splits
+    bool few;                  // at most 32 stacked query rows: the kernel that keeps its logits
+    int stride;                // of a query row's logits
     int n_part;                // parts of the query rows in the second pass for the weights
     // byte offsets into the workspace
     size_t lse2;               // base-2 LSE [batch][Hkv][rows]
     size_t part_o, part_ml;    // results of the splits
+    size_t logits;             // of a few query rows [batch][Hkv][rows][stride]
     size_t part_w;             // weights of the parts [n_part][batch][Hkv][l_cap]
     size_t total;
 };
