@@ -88,6 +88,15 @@ int vxl_debug_read_stream(const void* src, size_t bytes, float* out, int n_workg
  * their own, 0 = the kernel of many rows; *n_split its key splits. */
 int vxl_debug_kvq_plan(const vxl_attn_desc* desc, int batch, int n_q_tokens, int l_cap, int* n_split);
 
+/* The plan of a vxl_mixed_attend call (host only): plan[0] = 0 the kernel of at most 32 stacked query rows, 4 or 8 the waves of the ring's
+ * workgroups (0 also for VXL_F32); plan[1] key splits; plan[2] parts of the query rows in the pass for the weights.  Returns 0 on invalid
+ * arguments. */
+int vxl_debug_mixed_plan(const vxl_attn_desc* desc, int batch, int n_q_tokens, int l_cap, int* plan);
+
+/* Cross-check: the waves (4 or 8), key splits and parts that VXL_BF16 calls of vxl_mixed_attend take where they have a choice (more splits
+ * than key tiles or parts than row tiles: as many as there are), each 0 = the library chooses.  Size the workspace after setting it. */
+void vxl_debug_mixed_force(int waves, int n_split, int n_part);
+
 #ifdef __cplusplus
 }
 #endif

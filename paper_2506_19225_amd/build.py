@@ -39,7 +39,7 @@ def _hipcc() -> str:
 NO_SCRATCH = {"vxl_prefill.hip": ("prefill_dma_kernel",),
               "vxl_decode.hip": ("decode_ring_kernel", "decode_wave_kernel"),
               "vxl_mass.hip": ("mass_partial_kernel",),
-              "vxl_attend.hip": ("attend_ring_kernel", "attend_step_kernel"),
+              "vxl_attend.hip": ("attend_ring_kernel", "attend_step_kernel", "attend_weights_kernel"),
               "vxl_debug.hip": ("tile_loop_kernel",)}
 
 

@@ -2,6 +2,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 #include <limits>
 #include <type_traits>
 
@@ -32,7 +33,14 @@ __device__ __forceinline__ Span span_of(const Rule& r, int pq) {
     if (pq < 0) return {1, 0, 0u};
     return {r.window ? max(pq - r.window + 1, 0) : 0, r.causal ? pq : INT32_MAX, (unsigned)r.n_always};
 }
-__device__ __forceinline__ bool sees(const Span& s, int pk) { return (pk >= s.lo && pk <= s.hi) || (unsigned)pk < s.na; }
+// (Negative where a row of position pk is hidden: by signs alone, as comparisons that are joined go through scalar registers and wait for
+// them.  Differences wrap for negative pk alone, and of a token's span, which is not empty or {1, 0}, never both; of bounds over several tokens,
+// for pk of -1 or more, none does.)
+__device__ __forceinline__ int hides(const Span& s, int pk) {
+    const unsigned p = (unsigned)pk, beyond = (p - (unsigned)s.lo) | ((unsigned)s.hi - p), first = (p - s.na) & ~p;
+    return (int)(beyond & ~first);
+}
+__device__ __forceinline__ bool sees(const Span& s, int pk) { return hides(s, pk) >= 0; }
 
 // Sets as the kernels see them.
 struct Sets {
@@ -318,7 +326,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_ring_kernel(Sets s, Rule r,
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) o[0][db] = zero16();
     const bool capped = r.cap2 > 0.f, biased = POS && r.slopes;
-    const float cu = capped || biased ? 1.f : r.c2;           // units of x below
+    const float cu = capped || biased ? 1.f : r.c2, unit_of = capped ? 1.f : r.c2;       // units of log 2 of x below; of what a bias is put to
     float m_run = -INFINITY, mc_run = kLowest, l_run = 0.f;
 
     auto process = [&](int ti) __attribute__((always_inline)) {
@@ -327,7 +335,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_ring_kernel(Sets s, Rule r,
         bool partial = left < kKeyTile;
         const int32_t* tile_pos = (const int32_t*)((const char*)lds + C::POS_AT) + (ti % C::NS) * kKeyTile;
         if constexpr (POS) {
-            const int pk = lane < left ? tile_pos[lane] : -1;
+            const int pk = lane < left ? max(tile_pos[lane], -1) : -1;
             if (__builtin_amdgcn_ballot_w64(sees(reach.most, pk)) == 0) return;
             partial = ~__builtin_amdgcn_ballot_w64(sees(reach.least, pk)) != 0;
         }
@@ -347,7 +355,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_ring_kernel(Sets s, Rule r,
             }
         }
         if constexpr (POS) {
-            if (partial || biased) {
+            auto by_position = [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -355,13 +363,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_ring_kernel(Sets s, Rule r,
                         const int4 p4 = *(const int4*)(tile_pos + kb * 32 + rq * 8 + hi * 4);
                         const int p[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float y = x[0][kb][rq * 4 + i];
-                            if (biased) y = fmaf(-slope2, (float)abs(pq - p[i]), capped ? y : y * r.c2);
-                            x[0][kb][rq * 4 + i] = sees(span, p[i]) && acc_key(kb, rq * 4 + i, hi) < left ? y : -INFINITY;
-                        }
+                        for (int i = 0; i < 4; ++i) x[0][kb][rq * 4 + i] = f(x[0][kb][rq * 4 + i], p[i], acc_key(kb, rq * 4 + i, hi));
                     }
-            }
+            };
+            if (biased) by_position([&](float y, int p, int) { return fmaf(-slope2, (float)abs(pq - p), y * unit_of); });
+            if (partial) by_position([&](float y, int p, int key) { return (hides(span, p) | (left - 1 - key)) >= 0 ? y : -INFINITY; });
         } else if (partial) {
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
@@ -566,7 +572,7 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s,
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) o[0][db] = zero16();
     const bool capped = r.cap2 > 0.f, biased = POS && r.slopes;
-    const float cu = capped || biased ? 1.f : r.c2;
+    const float cu = capped || biased ? 1.f : r.c2, unit_of = capped ? 1.f : r.c2;       // units of log 2 of y below; of what a bias is put to
     float m_run = -INFINITY, mc_run = kLowest, l_run = 0.f;
     float* const kept = logits ? logits + ((size_t)unit * n_rows + rho) * stride : nullptr;
 
@@ -587,6 +593,10 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s,
 #pragma unroll
         for (int j = 0; j < 16; ++j) y[j] = x[0][0][j];
         if (capped) cap_logits(y, r);
+        if (biased) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) y[j] = fmaf(-slope2, (float)abs(pq - tile_pos[acc_key(0, j, hi)]), y[j] * unit_of);
+        }
 #pragma unroll
         for (int jq = 0; jq < 4; ++jq) {
             int p[4] = {0, 0, 0, 0};
@@ -597,8 +607,7 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s,
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int j = jq * 4 + e;
-                if (biased) y[j] = fmaf(-slope2, (float)abs(pq - p[e]), capped ? y[j] : y[j] * r.c2);
-                const bool sees_it = sees(span, p[e]) && acc_key(0, j, hi) < left;
+                const bool sees_it = (hides(span, p[e]) | (left - 1 - acc_key(0, j, hi))) >= 0;
                 const float kept_as = y[j] * cu;
                 seen[j] = !sees_it ? -INFINITY : kept_as == -INFINITY ? kLowest : kept_as;
                 y[j] = sees_it ? y[j] : -INFINITY;
@@ -845,19 +854,40 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typen
 
 // ------------------------------------------------------------------------------------------
 // The weights of the rows where there are many query rows: the logits once more, against the LSE.  A wave keeps 64 keys in registers as
-// the operand of the first product and goes over query rows, 32 at a time through LDS for the four waves of a workgroup; a lane's sums
-// are of its 32 elements of the tile, folded over the lanes at the end.  Query rows are cut into n_part parts where keys alone do not
+// the operand of the first product and goes over query rows, 64 at a time from a ring of four LDS stages, which direct loads fill three tiles
+// ahead for the four waves of a workgroup (counted by hand); a lane's sums are of its elements of the tiles, folded over the lanes at the end.  Query rows are cut into n_part parts where keys alone do not
 // fill the chip, whose sums a last kernel adds in order.
 // ------------------------------------------------------------------------------------------
-constexpr int kWeightWaves = 4, kWeightKeys = 64 * kWeightWaves, kWeightRows = 32;
+// Lanes whose bit N is set keep the upper half of their elements and take their partner's, the others the lower half.
+template <int N>
+__device__ __forceinline__ void fold(const float (&from)[2 * N], float (&to)[N], int lane) {
+    const bool upper = lane & N;
+#pragma unroll
+    for (int j = 0; j < N; ++j) to[j] = (upper ? from[j + N] : from[j]) + __shfl_xor(upper ? from[j] : from[j + N], N);
+}
+
+constexpr int kWeightWaves = 4, kWeightKeys = 64 * kWeightWaves, kWeightRows = 64;
+
+template <int D>
+struct WeightsCfg {
+    static constexpr int NS = 4, TILE = kWeightRows * D, PPR = D / 8, RPI = 64 / PPR, IPW = kWeightRows / RPI / kWeightWaves;   // as the ring's
+    static constexpr int LOADS = IPW + 1;                     // of a wave and tile: its rows, and one of LSE, position and slope
+    static constexpr int INFO_AT = NS * TILE * 2, LDS_BYTES = INFO_AT + NS * kWeightWaves * 64 * 4;
+};
 
 template <int D, bool POS>
 __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Sets s, Rule r, const float* __restrict__ lse2, const float* weight,
                                                                               float* weight_out, float* __restrict__ part_w, int units, int n_part,
                                                                               int n_blocks) {
-    constexpr int TILE = kWeightRows * D, PER = kWeightRows * D / 8 / (64 * kWeightWaves);    // 16-byte pieces of a thread
-    __shared__ __attribute__((aligned(16))) uint16_t q_lds[2][TILE];
+    using C = WeightsCfg<D>;
+    struct Row {               // of a query row, as a lane needs it
+        float lse, slope2;     // (lse +inf: weighs nothing)
+        Span span;
+        int pq;
+    };
+    extern __shared__ __attribute__((aligned(16))) uint16_t lds[];
     __shared__ __attribute__((aligned(16))) int32_t pos_lds[POS ? kWeightWaves : 1][64];
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int unit, part, block;
@@ -878,7 +908,7 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) k[kb][ks] = __builtin_bit_cast(bf16x8, src[ks * 2 + hi]);
     }
-    int pk = key0 + lane < len ? (POS ? r.row_pos[set + key0 + lane] : 0) : -1, pk_min = pk, pk_max = pk;
+    int pk = key0 + lane < len ? (POS ? max(r.row_pos[set + key0 + lane], -1) : 0) : -1, pk_min = pk, pk_max = pk;
     if constexpr (POS) {
         pos_lds[wave][lane] = pk;
 #pragma unroll
@@ -888,114 +918,171 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
         }
     }
     const bool capped = r.cap2 > 0.f, biased = POS && r.slopes, ragged = key0 + 64 > len;
-    const float cu = capped || biased ? 1.f : r.c2;
+    const float cu = capped || biased ? 1.f : r.c2, unit_of = capped ? 1.f : r.c2;       // units of log 2 of x below; of what a bias is put to
 
-    // Query rows of the tile after the next, and what a lane has to know of its row of the next.
-    uint4 piece0, piece1;
-    static_assert(PER <= 2, "pieces of a thread");
-    auto row_of = [&](int rho) __attribute__((always_inline)) { return ((size_t)b * s.T + rho / group) * s.n_q + g * group + rho % group; };
-    auto piece_of = [&](int t, int p) __attribute__((always_inline)) {
-        const int rho = min((tile0 + t) * kWeightRows + p / (D / 8), n_rows - 1);
-        return *(const uint4*)((const uint16_t*)s.q + row_of(rho) * D + p % (D / 8) * 8);
+    // Tile t -> stage t % NS, the tiles in their order; rows behind the last one are it.  Token and head of a lane's first row, and of the row
+    // whose numbers it loads, are carried from tile to tile: divisions by the group took as long as the products.
+    struct Place {
+        int tok, hg;
+        __device__ __forceinline__ void add(int toks, int hgs, int group) {
+            tok += toks;
+            hg += hgs;
+            if (hg >= group) { hg -= group; ++tok; }
+        }
     };
-    auto request = [&](int t) __attribute__((always_inline)) {
-        piece0 = piece_of(t, tid);
-        if constexpr (PER == 2) piece1 = piece_of(t, 64 * kWeightWaves + tid);
+    const char* const q_unit = (const char*)((const uint16_t*)s.q + ((size_t)b * s.T * s.n_q + (size_t)g * group) * D);
+    const int r_in = lane / C::PPR, pp = lane % C::PPR, first = tile0 * kWeightRows + wave * C::RPI + r_in, own = tile0 * kWeightRows + lane;
+    constexpr int BETWEEN = C::RPI * kWeightWaves;            // rows between two loads of a wave
+    const int tile_toks = kWeightRows / group, tile_hgs = kWeightRows % group, load_toks = BETWEEN / group, load_hgs = BETWEEN % group;
+    Place row_at{first / group, first % group}, own_at{own / group, own % group};
+    const bool of_pos = POS && wave == 1, of_slope = POS && wave == 2 && r.slopes;
+    const char* const info = of_pos ? (const char*)(r.q_pos + (size_t)b * s.T) : of_slope ? (const char*)(r.slopes + g * group)
+                                                                                   : (const char*)(lse2 + (size_t)unit * n_rows);
+    int issued = 0;
+    auto issue = [&]() __attribute__((always_inline)) {
+        const int t = min(issued, n_t - 1);
+        const uint32_t st = lds_base + (uint32_t)(t % C::NS) * (C::TILE * 2);
+        Place at = row_at;
+#pragma unroll
+        for (int i = 0; i < C::IPW; ++i) {
+            const int row = (wave + i * kWeightWaves) * C::RPI + r_in, kp = pp ^ ((row / (16 / C::PPR)) & (C::PPR - 1));
+            const bool there = at.tok < s.T;
+            const int tok = there ? at.tok : s.T - 1, hg = there ? at.hg : group - 1;
+            dma16_addr(q_unit + ((size_t)tok * s.n_q + hg) * (D * 2) + kp * 16, st + (wave + i * kWeightWaves) * 1024);
+            at.add(load_toks, load_hgs, group);
+        }
+        const bool there = own_at.tok < s.T;
+        const int tok = there ? own_at.tok : s.T - 1, hg = there ? own_at.hg : group - 1;
+        dma4(info, (uint32_t)(of_pos ? tok : of_slope ? hg : tok * group + hg) * 4, lds_base + C::INFO_AT + (uint32_t)((t % C::NS) * kWeightWaves + wave) * 256);
+        if (++issued < n_t) {
+            row_at.add(tile_toks, tile_hgs, group);
+            own_at.add(tile_toks, tile_hgs, group);
+        }
     };
-    auto put = [&](uint16_t* q, uint4 x, int p) __attribute__((always_inline)) { *(uint4*)(q + k_tile_off<D>(p / (D / 8), p % (D / 8))) = x; };
-    struct Row {
-        float lse, slope2;
-        int pq;
-    };
-    auto row_info = [&](int t) __attribute__((always_inline)) {
-        const int rho = (tile0 + t) * kWeightRows + l32, at = min(rho, n_rows - 1);
-        Row x;
-        x.lse = lse2[(size_t)unit * n_rows + at];
-        x.lse = rho < n_rows && x.lse != -INFINITY ? x.lse : INFINITY;            // (weighs nothing)
-        x.pq = POS ? r.q_pos[b * s.T + at / group] : 0;
-        x.slope2 = POS ? slope_of(r, g * group + at % group) : 0.f;
-        return x;
+    auto product = [&](const uint16_t* q, int half, f32x16 (&x)[2]) __attribute__((always_inline)) {
+        x[0] = x[1] = zero16();
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+            const bf16x8 a = *(const bf16x8*)(q + k_tile_off<D>(half * 32 + l32, ks * 2 + hi));
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kb][ks], a, x[kb], 0, 0, 0);
+        }
     };
     f32x16 acc[2] = {zero16(), zero16()};
+    auto plain = [&](const f32x16 (&x)[2], float lse) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[kb][i] += __builtin_amdgcn_exp2f(fmaf(x[kb][i], cu, -lse));
+    };
+    auto by_position = [&](f32x16 (&x)[2], auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int rq = 0; rq < 4; ++rq) {
+                int p[4];
+                if constexpr (POS) {
+                    const int4 p4 = *(const int4*)&pos_lds[wave][kb * 32 + rq * 8 + hi * 4];
+                    p[0] = p4.x; p[1] = p4.y; p[2] = p4.z; p[3] = p4.w;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[i] = key0 + kb * 32 + rq * 8 + hi * 4 + i < len ? 0 : -1;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[kb][rq * 4 + i] = f(x[kb][rq * 4 + i], p[i]);
+            }
+    };
     if (n_t > 0) {
-        request(0);
-        Row next = row_info(0);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {             // complete here: no load that the compiler counts is outstanding behind
+                typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+                asm volatile("" :: "v"(__builtin_bit_cast(u32x4, k[kb][ks])));
+            }
+        asm volatile("" :: "v"(pk_min), "v"(pk_max));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < C::NS - 1; ++t) issue();
         for (int t = 0; t < n_t; ++t) {
-            uint16_t* q = q_lds[t & 1];
-            put(q, piece0, tid);
-            if constexpr (PER == 2) put(q, piece1, 64 * kWeightWaves + tid);
-            const Row row = next;
-            request(min(t + 1, n_t - 1));
-            next = row_info(min(t + 1, n_t - 1));
-            __syncthreads();                                  // (the other stage is read by nobody any more: one barrier a tile)
+            wait_vmcnt<(C::NS - 2) * C::LOADS>();             // this wave's part of tile t has landed
+            __builtin_amdgcn_s_barrier();                     // ... and everyone's; tile t - 1 is read by nobody any more
+            issue();
             if (!active) continue;
-            const Span span = span_of(r, row.pq);
-            bool partial = ragged;
+            const uint16_t* q = lds + (t % C::NS) * C::TILE;
+            const float* infos = (const float*)((const char*)lds + C::INFO_AT) + (t % C::NS) * (kWeightWaves * 64);
+            auto lse_of = [&](int half) __attribute__((always_inline)) {
+                const float lse = infos[half * 32 + l32];
+                return (tile0 + t) * kWeightRows + half * 32 + l32 < n_rows && lse != -INFINITY ? lse : INFINITY;
+            };
+            auto pos_of = [&](int half) __attribute__((always_inline)) { return POS ? __float_as_int(infos[64 + half * 32 + l32]) : 0; };
+            bool all = !ragged;
             if constexpr (POS) {
-                const bool none = (pk_max < span.lo || pk_min > span.hi) && (pk_max < 0 || (unsigned)max(pk_min, 0) >= span.na);
-                if (__builtin_amdgcn_ballot_w64(!none) == 0) continue;
-                const bool all = pk_min >= 0 && ((pk_min >= span.lo && pk_max <= span.hi) || (unsigned)pk_max < span.na);
-                partial = ~__builtin_amdgcn_ballot_w64(all) != 0;
-            }
-            f32x16 x[2] = {zero16(), zero16()};
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                const bf16x8 a = *(const bf16x8*)(q + k_tile_off<D>(l32, ks * 2 + hi));
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kb][ks], a, x[kb], 0, 0, 0);
-            }
-            if (capped) {
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    float c[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) c[i] = x[kb][i];
-                    cap_logits(c, r);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[kb][i] = c[i];
+                for (int half = 0; half < 2; ++half) {
+                    const Span span = span_of(r, pos_of(half));
+                    all &= ~__builtin_amdgcn_ballot_w64(pk_min >= 0 && ((pk_min >= span.lo && pk_max <= span.hi) || (unsigned)pk_max < span.na)) == 0;
                 }
             }
-            if (partial || biased) {
+            if (all && !capped && !biased) {
+                const float lse[2] = {lse_of(0), lse_of(1)};
+                f32x16 x[2], y[2];                            // (one stretch: a product runs beside the exponentials of the other)
+                product(q, 0, x);
+                product(q, 1, y);
+                plain(x, lse[0]);
+                plain(y, lse[1]);
+                continue;
+            }
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                Row row;
+                row.pq = pos_of(half);
+                row.span = span_of(r, row.pq);
+                if constexpr (POS) {
+                    const bool hidden = (pk_max < row.span.lo || pk_min > row.span.hi) && (pk_max < 0 || (unsigned)max(pk_min, 0) >= row.span.na);
+                    if (__builtin_amdgcn_ballot_w64(!hidden) == 0) continue;
+                }
+                row.lse = lse_of(half);
+                row.slope2 = biased ? infos[128 + half * 32 + l32] * kLog2e : 0.f;
+                f32x16 x[2];
+                product(q, half, x);
+                if (capped) {
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
+                    for (int kb = 0; kb < 2; ++kb) {
+                        float c[16];
 #pragma unroll
-                    for (int rq = 0; rq < 4; ++rq) {
-                        int p[4];
-                        if constexpr (POS) {
-                            const int4 p4 = *(const int4*)&pos_lds[wave][kb * 32 + rq * 8 + hi * 4];
-                            p[0] = p4.x; p[1] = p4.y; p[2] = p4.z; p[3] = p4.w;
-                        } else {
+                        for (int i = 0; i < 16; ++i) c[i] = x[kb][i];
+                        cap_logits(c, r);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) p[i] = key0 + kb * 32 + rq * 8 + hi * 4 + i < len ? 0 : -1;
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float y = x[kb][rq * 4 + i];
-                            if (biased) y = fmaf(-row.slope2, (float)abs(row.pq - p[i]), capped ? y : y * r.c2);
-                            acc[kb][rq * 4 + i] += sees(span, p[i]) ? __builtin_amdgcn_exp2f(fmaf(y, cu, -row.lse)) : 0.f;
-                        }
+                        for (int i = 0; i < 16; ++i) x[kb][i] = c[i];
                     }
-            } else {
+                }
+                if (biased) by_position(x, [&](float y, int p) { return fmaf(-row.slope2, (float)abs(row.pq - p), y * unit_of); });
+                if (all) {
+                    plain(x, row.lse);
+                } else {                                      // (what is not seen has weight 0, also where the LSE is no number)
+                    by_position(x, [&](float y, int p) { return __builtin_amdgcn_exp2f(sees(row.span, p) ? fmaf(y, cu, -row.lse) : -INFINITY); });
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[kb][i] += __builtin_amdgcn_exp2f(fmaf(x[kb][i], cu, -row.lse));
+                    for (int kb = 0; kb < 2; ++kb) acc[kb] += x[kb];
+                }
             }
         }
     }
+    wait_vmcnt<0>();                                          // drain the refills before the wave ends
     if (!active) return;
+    // Element e = 16 kb + i of the 32 lanes of a half to lane e: half of the elements change lanes at every step.
+    float e32[32], e16[16], e8[8], e4[4], e2[2], e1[1];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float w = acc[kb][i];
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) w += __shfl_xor(w, o);
-            const int key = key0 + acc_key(kb, i, hi);
-            if (l32 != i || key >= len) continue;
-            if (n_part > 1) part_w[((size_t)part * units + unit) * s.cap + key] = w;
-            else weight_out[set + key] = (weight ? weight[set + key] : 0.f) + w;
-        }
+    for (int e = 0; e < 32; ++e) e32[e] = acc[e >> 4][e & 15];
+    fold<16>(e32, e16, lane);
+    fold<8>(e16, e8, lane);
+    fold<4>(e8, e4, lane);
+    fold<2>(e4, e2, lane);
+    fold<1>(e2, e1, lane);
+    const int key = key0 + acc_key(l32 >> 4, l32 & 15, hi);
+    if (key >= len) return;
+    if (n_part > 1) part_w[((size_t)part * units + unit) * s.cap + key] = e1[0];
+    else weight_out[set + key] = (weight ? weight[set + key] : 0.f) + e1[0];
 }
 
 // The sum of the parts.
@@ -1011,15 +1098,25 @@ __global__ __launch_bounds__(256) void weights_sum_kernel(const float* __restric
 
 }  // namespace
 
+// Test hook (vxl_debug.h).
+static std::atomic<int> g_force_waves{0}, g_force_split{0}, g_force_part{0};
+extern "C" void vxl_debug_mixed_force(int waves, int n_split, int n_part) {
+    g_force_waves = waves == 4 || waves == 8 ? waves : 0;
+    g_force_split = std::max(0, n_split);
+    g_force_part = std::max(0, n_part);
+}
+
 // Many query rows (ring): estimates in us of a launch of workgroups of 256 and of 128 rows and so many splits.
 static void ring_plan(MixedPlan& p, long long units, long long rows, int D, int l_cap) {
     const long long tiles = (l_cap + kKeyTile - 1) / kKeyTile;
+    const int force_waves = g_force_waves, force_split = g_force_split;
     double best = 1e30;
     for (int nw : {8, 4}) {
+        if (force_waves && nw != force_waves) continue;
         const long long n_rtile = (rows + 32 * nw - 1) / (32 * nw), base = units * n_rtile;
         const double tile = nw == 8 ? 1.6 : 1.05;
-        const long long most = std::max<long long>(1, std::min<long long>(tiles, 512 / base));
-        for (long long n = 1; n <= most;) {
+        const long long most = force_split ? std::min<long long>(tiles, force_split) : std::max<long long>(1, std::min<long long>(tiles, 512 / base));
+        for (long long n = force_split ? most : 1; n <= most;) {
             const long long walk = (tiles + n - 1) / n, rounds = (base * n + 255) / 256;
             const double mb = 4e-6 * units * n * rows * D;
             const double us = rounds * (6 + tile * (D == 64 ? 0.6 : 1.0) * walk) + (n > 1 ? 3 + 0.5 * mb : 0);
@@ -1028,7 +1125,7 @@ static void ring_plan(MixedPlan& p, long long units, long long rows, int D, int 
                 p.waves = nw;
                 p.n_split = (int)n;
             }
-            n = walk > 1 ? (tiles + walk - 2) / (walk - 1) : most + 1;            // the next that shortens the walk
+            n = walk > 1 ? std::max(n + 1, (tiles + walk - 2) / (walk - 1)) : most + 1;           // the next that shortens the walk
         }
     }
 }
@@ -1043,20 +1140,21 @@ MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     p.stride = (l_cap + kStepTile - 1) / kStepTile * kStepTile;
     p.few = d->dtype == VXL_BF16 && rows <= kStepRows;
     if (p.few) {
-        const long long tiles = (l_cap + kStepTile - 1) / kStepTile;
-        p.n_split = (int)std::max<long long>(1, std::min<long long>((tiles + kStepWaves - 1) / kStepWaves, 256 / units));
+        const long long tiles = (l_cap + kStepTile - 1) / kStepTile, most = (tiles + kStepWaves - 1) / kStepWaves;
+        p.n_split = (int)std::max<long long>(1, std::min<long long>(most, g_force_split ? (long long)g_force_split : 256 / units));
     } else if (d->dtype == VXL_BF16) {
         ring_plan(p, units, rows, d->head_dim, l_cap);
         // parts of the query rows: as many as fill rounds of two workgroups on a compute unit
         const long long row_tiles = (rows + kWeightRows - 1) / kWeightRows, blocks = units * key_blocks;
         double best = 1e30;
         for (long long n = 1; n <= std::min<long long>(row_tiles, 16); ++n) {
-            const double us = ((blocks * n + 511) / 512) * (3 + 0.25 * ((row_tiles + n - 1) / n)) + (n > 1 ? 3 : 0);
+            const double us = ((blocks * n + 511) / 512) * (3 + 1.0 * ((row_tiles + n - 1) / n)) + (n > 1 ? 3 : 0);
             if (us < best) {
                 best = us;
                 p.n_part = (int)n;
             }
         }
+        if (g_force_part) p.n_part = (int)std::min<long long>(row_tiles, g_force_part);
     }
     size_t at = 0;
     auto put = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
@@ -1067,6 +1165,15 @@ MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     p.part_w = put(p.n_part > 1 ? (size_t)p.n_part * units * l_cap * sizeof(float) : 0);
     p.total = at;
     return p;
+}
+
+extern "C" int vxl_debug_mixed_plan(const vxl_attn_desc* d, int batch, int n_q_tokens, int l_cap, int* plan) {
+    if (vxl_workspace_bytes(VXL_OP_MIXED_ATTEND, nullptr, d, batch, n_q_tokens, l_cap) == 0) return 0;
+    const MixedPlan p = mixed_plan(d, batch, n_q_tokens, l_cap);
+    plan[0] = p.waves;
+    plan[1] = p.n_split;
+    plan[2] = p.n_part;
+    return 1;
 }
 
 // Workgroups on the XCDs in turn, as place() takes them.
@@ -1149,7 +1256,14 @@ static vxl_status launch_weights(const MixedPlan& p, const MixedCall& c, const S
     const int units = c.batch * d->n_kv_heads, n_blocks = (c.l_cap + kWeightKeys - 1) / kWeightKeys;
     float *lse2 = (float*)(c.ws + p.lse2), *part_w = (float*)(c.ws + p.part_w);
     auto run = [&](auto dim, auto pos) {
-        hipLaunchKernelGGL((attend_weights_kernel<dim, pos>), placed_grid((long long)units * p.n_part * n_blocks), dim3(64 * kWeightWaves), 0, s, sets,
+        constexpr int lds = WeightsCfg<dim>::LDS_BYTES;
+        static PerDeviceOnce attr;
+        const vxl_status st = attr.run([&] {
+            VXL_HIP_TRY(hipFuncSetAttribute((const void*)attend_weights_kernel<dim, pos>, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+            return VXL_OK;
+        });
+        if (st != VXL_OK) return st;
+        hipLaunchKernelGGL((attend_weights_kernel<dim, pos>), placed_grid((long long)units * p.n_part * n_blocks), dim3(64 * kWeightWaves), lds, s, sets,
                            rule, lse2, c.weight, c.weight_out, part_w, units, p.n_part, n_blocks);
         return mixed_launched();
     };

@@ -148,6 +148,9 @@ def lib() -> C.CDLL:
     L.vxl_debug_decode_ring_waves.restype = C.c_int
     L.vxl_debug_kvq_plan.argtypes = [dp, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_int)]
     L.vxl_debug_kvq_plan.restype = C.c_int
+    L.vxl_debug_mixed_plan.argtypes = [dp, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_int * 3)]
+    L.vxl_debug_mixed_plan.restype = C.c_int
+    L.vxl_debug_mixed_force.argtypes = [C.c_int, C.c_int, C.c_int]
     L.vxl_debug_gather_shared.argtypes = [dp, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int]
     L.vxl_debug_gather_shared.restype = C.c_int
     L.vxl_debug_mfma_stream.argtypes = [vp, C.c_int, C.c_int, vp]
@@ -592,6 +595,19 @@ def debug_kvq_plan(desc: AttnDesc, batch: int, n_q_tokens: int, l_cap: int):
     n_split = C.c_int(0)
     kernel = lib().vxl_debug_kvq_plan(C.byref(desc), batch, n_q_tokens, l_cap, C.byref(n_split))
     return kernel, n_split.value
+
+
+def debug_mixed_plan(desc: AttnDesc, batch: int, n_q_tokens: int, l_cap: int):
+    """(waves of the ring, 0 = not the ring; key splits; parts of the pass for the weights) of a mixed_attend call.  Needs no GPU."""
+    plan = (C.c_int * 3)()
+    if not lib().vxl_debug_mixed_plan(C.byref(desc), batch, n_q_tokens, l_cap, C.byref(plan)):
+        raise ValueError("no such call")
+    return tuple(plan)
+
+
+def debug_mixed_force(waves: int = 0, n_split: int = 0, n_part: int = 0) -> None:
+    """Cross-check only: the waves, splits and parts that mixed_attend takes, 0 = the library chooses.  Size the workspace after setting it."""
+    lib().vxl_debug_mixed_force(int(waves), int(n_split), int(n_part))
 
 
 def debug_gather_shared(desc: AttnDesc, n_tokens: int, n_sparse: int, n_chunks: int, batch: int, l_cap: int) -> bool:
