@@ -1,8 +1,7 @@
 // Attention over mixed sets by position: capped or biased logits, rows that a rule hides, and the weight that every row receives.
-#include <math.h>
-
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <limits>
 #include <type_traits>
 
@@ -1096,6 +1095,277 @@ __global__ __launch_bounds__(256) void weights_sum_kernel(const float* __restric
     weight_out[at] = (weight ? weight[at] : 0.f) + w;
 }
 
+// ------------------------------------------------------------------------------------------
+// fp32 sets, on the fp32 matrix instruction: 16 stacked query rows per workgroup, whose four waves take the 32-key tiles of its split in turn;
+// operands come from memory in the order that both products use, as in the plain fp32 decode:
+//   S^T = K Q^T    lane (i = lane % 16, j = lane / 16): K[key i][16 x + 4 j + e] and Q[row i] of the same; result register r: key 4 j + r, row i
+//   O^T = V^T P^T  step r takes the keys 4 j + r, V[key 4 j + r][64 b + 4 i + e]; result register r' of (b, e): O[row i][64 b + 16 j + 4 r' + e]
+// Bound by that instruction (a 1/16 of the bf16 one's rate) where there is enough to do.
+// ------------------------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+constexpr int kF32Block = 16, kF32Tile = 32, kF32Waves = 4;
+
+// Logits in units of log 2 of the four keys 4 j + r of a block, from the products: -inf where hidden, also behind `left` keys.
+template <bool POS>
+__device__ __forceinline__ float f32_logit(const Rule& r, const Span& span, float dot, float slope2, int pq, int pk, bool there) {
+    float y = r.cap2 > 0.f ? r.cap2 * tanhf(dot * r.cap_in) : dot * r.c2;
+    if (POS && r.slopes) y = fmaf(-slope2, (float)abs(pq - pk), y);
+    return there && sees(span, pk) ? y : -INFINITY;
+}
+
+template <int D, bool POS>
+__global__ __launch_bounds__(64 * kF32Waves, 2) void attend_f32_kernel(Sets s, Rule r, Partials part, float* __restrict__ O, float* __restrict__ LSE,
+                                                                       float* __restrict__ lse2, float* __restrict__ logits, int stride, int units,
+                                                                       int n_split, int n_rtile) {
+    constexpr int NW = kF32Waves, X = D / 16;
+    __shared__ __attribute__((aligned(16))) float red[NW][kF32Block][D + 4];      // (+ 4: neighbouring rows in other banks)
+    __shared__ float2 stats[NW][kF32Block];
+    const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, j = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int unit, split, rtile;
+    if (!place(units, n_split, n_rtile, &unit, &split, &rtile)) return;
+    const int g = unit % s.n_kv, b = unit / s.n_kv, group = s.n_q / s.n_kv, n_rows = group * s.T, row0 = rtile * kF32Block;
+    const int len = min(max(s.len[b], 0), s.cap);
+    const size_t set = (size_t)unit * s.cap;
+    const float *kset = (const float*)s.k + set * D, *vset = (const float*)s.v + set * D;
+    const int rho = min(row0 + i, n_rows - 1), tok = rho / group, h = g * group + rho % group;
+    const int pq = POS ? r.q_pos[b * s.T + tok] : 0;
+    const float slope2 = POS ? slope_of(r, h) : 0.f;
+    const Span span = span_of(r, pq);
+    float4 q[X];
+#pragma unroll
+    for (int x = 0; x < X; ++x) q[x] = *(const float4*)((const float*)s.q + (((size_t)b * s.T + tok) * s.n_q + h) * D + 16 * x + 4 * j);
+    float* const kept = logits && row0 + i < n_rows ? logits + ((size_t)unit * n_rows + rho) * stride : nullptr;
+
+    f32x4 o[X];
+#pragma unroll
+    for (int x = 0; x < X; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+    const int tiles = (len + kF32Tile - 1) / kF32Tile, tile0 = split * NW + wave, every = n_split * NW;
+    for (int tile = tile0; tile < tiles; tile += every) {
+        const int key0 = tile * kF32Tile;
+        int pk[2][4];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pk[kb][e] = POS ? r.row_pos[set + min(key0 + kb * 16 + 4 * j + e, len - 1)] : 0;
+        if constexpr (POS) {                                  // (hidden from all 16 rows: nothing to do)
+            bool any = false;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) any |= sees(span, pk[kb][e]);
+            if (__builtin_amdgcn_ballot_w64(any) == 0) {
+                if (kept)
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb) *(float4*)(kept + key0 + kb * 16 + 4 * j) = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                continue;
+            }
+        }
+        float4 k[2][X], v[2][4][D / 64];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const float* p = kset + (size_t)min(key0 + kb * 16 + i, len - 1) * D + 4 * j;
+#pragma unroll
+            for (int x = 0; x < X; ++x) k[kb][x] = *(const float4*)(p + 16 * x);
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float* p = vset + (size_t)min(key0 + kb * 16 + 4 * j + e, len - 1) * D + 4 * i;
+#pragma unroll
+                for (int y = 0; y < D / 64; ++y) v[kb][e][y] = *(const float4*)(p + 64 * y);
+            }
+        f32x4 y[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int x = 0; x < X; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+                    y[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(((const float*)&k[kb][x])[e], ((const float*)&q[x])[e], y[kb], 0, 0, 0);
+        float top = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            float keep[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool there = key0 + kb * 16 + 4 * j + e < len;
+                y[kb][e] = f32_logit<POS>(r, span, y[kb][e], slope2, pq, pk[kb][e], there);
+                keep[e] = there && sees(span, pk[kb][e]) && y[kb][e] == -INFINITY ? kLowest : y[kb][e];
+                top = fmaxf(top, y[kb][e]);
+            }
+            if (kept) *(float4*)(kept + key0 + kb * 16 + 4 * j) = make_float4(keep[0], keep[1], keep[2], keep[3]);
+        }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m_new = fmaxf(m, top), ref = m_new == -INFINITY ? 0.f : m_new, alpha = __builtin_amdgcn_exp2f(m - ref);
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y[kb][e] = __builtin_amdgcn_exp2f(y[kb][e] - ref);
+                l += y[kb][e];
+            }
+#pragma unroll
+        for (int x = 0; x < X; ++x) o[x] *= alpha;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int x = 0; x < X; ++x)
+                    o[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(((const float*)&v[kb][e][x / 4])[x % 4], y[kb][e], o[x], 0, 0, 0);
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    // A value that is no number reaches rows that do not see it, 0 * inf: those whose result is none are made again.
+    bool odd = false;
+#pragma unroll
+    for (int x = 0; x < X; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= !(fabsf(o[x][e]) < INFINITY);
+    unsigned long long again = __builtin_amdgcn_ballot_w64(odd && row0 + i < n_rows);
+    again = (again | again >> 16 | again >> 32 | again >> 48) & 0xffffull;
+    if (!(again >> i & 1)) {
+#pragma unroll
+        for (int x = 0; x < X; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) red[wave][i][64 * (x / 4) + 16 * j + 4 * e + x % 4] = o[x][e];
+        if (j == 0) stats[wave][i] = make_float2(l == 0.f ? -INFINITY : m, l);
+    }
+    while (again) {                                           // (uniform in the wave; a row's place holds its query until its result is there)
+        const int row = __builtin_ctzll(again);
+        again &= again - 1;
+        const int at = row0 + row, t = at / group, hq = g * group + at % group;
+        float* q_row = red[wave][row];
+        __builtin_amdgcn_wave_barrier();
+        for (int x = lane; x < D; x += 64) q_row[x] = ((const float*)s.q)[(((size_t)b * s.T + t) * s.n_q + hq) * D + x];
+        __builtin_amdgcn_wave_barrier();
+        float m1, l1, acc[D / 64];
+        exact_row<float, D>(r, q_row, kset, vset, r.row_pos ? r.row_pos + set : nullptr, tile0 * kF32Tile, len, kF32Tile, every * kF32Tile,
+                            r.q_pos ? r.q_pos[b * s.T + t] : 0, slope_of(r, hq), m1, l1, acc);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) q_row[lane + 64 * x] = acc[x];
+        if (lane == 0) stats[wave][row] = make_float2(m1, l1);
+    }
+    __syncthreads();
+    const size_t part_row0 = ((size_t)unit * n_split + split) * n_rows + row0;
+    for (int e = tid; e < min(kF32Block, n_rows - row0) * (D / 4); e += 64 * NW) {
+        const int row = e / (D / 4), c = e % (D / 4) * 4;
+        float2 st[NW];
+        float M = -INFINITY, L = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            st[w] = stats[w][row];
+            M = fmaxf(M, st[w].x);
+        }
+        const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float4 x = *(const float4*)&red[w][row][c];
+            const float f = part_weight(st[w], ref);
+            L = add_part(f, st[w].y, L);
+            a[0] = add_part(f, x.x, a[0]); a[1] = add_part(f, x.y, a[1]); a[2] = add_part(f, x.z, a[2]); a[3] = add_part(f, x.w, a[3]);
+        }
+        const float y = L == 0.f ? -INFINITY : M + __builtin_amdgcn_logf(L);
+        if (c == 0 && (n_split > 1 || logits)) part.ml[part_row0 + row] = make_float2(M, L);
+        if (n_split > 1) {
+            *(float4*)(part.o + (part_row0 + row) * D + c) = make_float4(a[0], a[1], a[2], a[3]);
+        } else {
+            const int at = row0 + row;
+            const size_t out = ((size_t)b * s.T + at / group) * s.n_q + g * group + at % group;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) a[x] = L == 0.f ? 0.f : a[x] / L;
+            *(float4*)(O + out * D + c) = make_float4(a[0], a[1], a[2], a[3]);
+            if (c == 0) {
+                if (LSE) LSE[out] = y * kLn2;
+                lse2[(size_t)unit * n_rows + at] = y;
+            }
+        }
+    }
+}
+
+// The weights of fp32 sets where there are many query rows: a wave has 32 keys and goes over blocks of 16 query rows, four waves of a workgroup
+// over parts of them, whose sums are folded through LDS.
+template <int D, bool POS>
+__global__ __launch_bounds__(64 * kF32Waves, 2) void weights_f32_kernel(Sets s, Rule r, const float* __restrict__ lse2, const float* weight,
+                                                                        float* weight_out) {
+    constexpr int NW = kF32Waves, X = D / 16;
+    __shared__ float sums[NW][kF32Tile];
+    const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, j = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int unit = blockIdx.y, g = unit % s.n_kv, b = unit / s.n_kv, group = s.n_q / s.n_kv, n_rows = group * s.T;
+    const int len = min(max(s.len[b], 0), s.cap), key0 = (int)blockIdx.x * kF32Tile;
+    if (key0 >= len) return;
+    const size_t set = (size_t)unit * s.cap;
+    float4 k[2][X];
+    int pk[2][4];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+        const float* p = (const float*)s.k + (set + min(key0 + kb * 16 + i, len - 1)) * D + 4 * j;
+#pragma unroll
+        for (int x = 0; x < X; ++x) k[kb][x] = *(const float4*)(p + 16 * x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pk[kb][e] = POS ? r.row_pos[set + min(key0 + kb * 16 + 4 * j + e, len - 1)] : 0;
+    }
+    f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    for (int row0 = wave * kF32Block; row0 < n_rows; row0 += NW * kF32Block) {
+        const int rho = min(row0 + i, n_rows - 1), tok = rho / group, h = g * group + rho % group;
+        const float* src = (const float*)s.q + (((size_t)b * s.T + tok) * s.n_q + h) * D + 4 * j;
+        float4 q[X];
+#pragma unroll
+        for (int x = 0; x < X; ++x) q[x] = *(const float4*)(src + 16 * x);
+        const int pq = POS ? r.q_pos[b * s.T + tok] : 0;
+        const float slope2 = POS ? slope_of(r, h) : 0.f, at = lse2[(size_t)unit * n_rows + rho];
+        const float lse = row0 + i < n_rows && at != -INFINITY ? at : INFINITY;
+        const Span span = span_of(r, pq);
+        if constexpr (POS) {
+            bool any = false;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) any |= sees(span, pk[kb][e]);
+            if (__builtin_amdgcn_ballot_w64(any) == 0) continue;
+        }
+        f32x4 y[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int x = 0; x < X; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+                    y[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(((const float*)&k[kb][x])[e], ((const float*)&q[x])[e], y[kb], 0, 0, 0);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = f32_logit<POS>(r, span, y[kb][e], slope2, pq, pk[kb][e], true);
+                acc[kb][e] += __builtin_amdgcn_exp2f(sees(span, pk[kb][e]) ? x - lse : -INFINITY);
+            }
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float w = acc[kb][e];
+#pragma unroll
+            for (int x = 8; x > 0; x >>= 1) w += __shfl_xor(w, x);
+            if (i == 0) sums[wave][kb * 16 + 4 * j + e] = w;
+        }
+    __syncthreads();
+    if (tid >= kF32Tile || key0 + tid >= len) return;
+    float w = 0.f;
+#pragma unroll
+    for (int x = 0; x < NW; ++x) w += sums[x][tid];
+    const size_t at = set + key0 + tid;
+    weight_out[at] = (weight ? weight[at] : 0.f) + w;
+}
+
 }  // namespace
 
 // Test hook (vxl_debug.h).
@@ -1114,12 +1384,12 @@ static void ring_plan(MixedPlan& p, long long units, long long rows, int D, int 
     for (int nw : {8, 4}) {
         if (force_waves && nw != force_waves) continue;
         const long long n_rtile = (rows + 32 * nw - 1) / (32 * nw), base = units * n_rtile;
-        const double tile = nw == 8 ? 1.6 : 1.05;
+        const double tile = (nw == 8 ? 1.75 : 1.13) * (D == 64 ? 0.75 : 1.0);
         const long long most = force_split ? std::min<long long>(tiles, force_split) : std::max<long long>(1, std::min<long long>(tiles, 512 / base));
         for (long long n = force_split ? most : 1; n <= most;) {
             const long long walk = (tiles + n - 1) / n, rounds = (base * n + 255) / 256;
             const double mb = 4e-6 * units * n * rows * D;
-            const double us = rounds * (6 + tile * (D == 64 ? 0.6 : 1.0) * walk) + (n > 1 ? 3 + 0.5 * mb : 0);
+            const double us = rounds * (8 + tile * walk) + (n > 1 ? 5 + 0.4 * mb : 0);
             if (us < best) {
                 best = us;
                 p.waves = nw;
@@ -1134,21 +1404,29 @@ MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     MixedPlan p{};
     const long long rows = (long long)(d->n_q_heads / d->n_kv_heads) * T, units = (long long)batch * d->n_kv_heads;
     const long long key_blocks = (l_cap + kWeightKeys - 1) / kWeightKeys;
-    p.fits = units <= 65535 && rows <= 1 << 30 && (__int128)units * ((rows + 127) / 128) <= INT32_MAX / 2 && units * key_blocks <= INT32_MAX / 64;
+    p.fits = units <= 65535 && rows <= 1 << 30 && (__int128)units * ((rows + 15) / 16) <= INT32_MAX / 2 && units * key_blocks <= INT32_MAX / 64;
     if (!p.fits) return p;
     p.n_split = p.n_part = 1;
     p.stride = (l_cap + kStepTile - 1) / kStepTile * kStepTile;
-    p.few = d->dtype == VXL_BF16 && rows <= kStepRows;
-    if (p.few) {
+    p.few = rows <= kStepRows;
+    if (d->dtype == VXL_F32) {
+        // as many splits as fill the chip, each wave of one with a tile at least
+        const long long tiles = (l_cap + kF32Tile - 1) / kF32Tile, most = (tiles + kF32Waves - 1) / kF32Waves;
+        const long long base = units * ((rows + kF32Block - 1) / kF32Block);
+        p.n_split = (int)std::max<long long>(1, std::min<long long>(most, g_force_split ? (long long)g_force_split : 512 / base));
+    } else if (p.few) {
         const long long tiles = (l_cap + kStepTile - 1) / kStepTile, most = (tiles + kStepWaves - 1) / kStepWaves;
         p.n_split = (int)std::max<long long>(1, std::min<long long>(most, g_force_split ? (long long)g_force_split : 256 / units));
     } else if (d->dtype == VXL_BF16) {
         ring_plan(p, units, rows, d->head_dim, l_cap);
-        // parts of the query rows: as many as fill rounds of two workgroups on a compute unit
+        // Parts of the query rows, by estimates in us: rounds of two workgroups on a compute unit, but no less than the workgroup whose keys
+        // are visible in part takes (tests per element).  448 rows, 23,872 keys, 1 to 4 parts 33.7, 33.2, 32.9, 37.3; 14,336 rows, 18,688
+        // keys, 1, 3, 5, 7, 12 parts 476, 371, 351, 362, 349.
         const long long row_tiles = (rows + kWeightRows - 1) / kWeightRows, blocks = units * key_blocks;
         double best = 1e30;
         for (long long n = 1; n <= std::min<long long>(row_tiles, 16); ++n) {
-            const double us = ((blocks * n + 511) / 512) * (3 + 1.0 * ((row_tiles + n - 1) / n)) + (n > 1 ? 3 : 0);
+            const double walk = (double)((row_tiles + n - 1) / n), rounds = std::max(1.0, blocks * n / 512.0);
+            const double us = std::max((rounds + std::ceil(rounds)) / 2 * (8 + 2.1 * walk), 8 + 3.3 * walk) + (n > 1 ? 4 : 0);
             if (us < best) {
                 best = us;
                 p.n_part = (int)n;
@@ -1207,7 +1485,24 @@ static vxl_status launch_ring(const MixedPlan& p, const MixedCall& c, const Sets
     return d->head_dim == 64 ? by_waves(std::integral_constant<int, 64>{}) : by_waves(std::integral_constant<int, 128>{});
 }
 
-// One row per merging workgroup, 1,024 rows of a set per workgroup of the weights.
+// Behind a kernel that keeps its logits: one row per merging workgroup, 1,024 rows of a set per workgroup of the weights.
+template <bool F32, int D>
+static vxl_status launch_finish(const MixedPlan& p, const MixedCall& c, const Partials& part, const float* logits, hipStream_t s) {
+    using T = typename Storage<F32>::T;
+    const vxl_attn_desc* d = c.d;
+    const int units = c.batch * d->n_kv_heads, rows = d->n_q_heads / d->n_kv_heads * c.T;
+    if (p.n_split == 1 && !logits) return VXL_OK;
+    const long long n_merge = p.n_split > 1 ? (long long)units * rows : 0, n_blocks = logits ? (c.l_cap + 1023) / 1024 : 0;
+    const long long all = n_merge + units * n_blocks;
+    auto finish = [&](auto most) {
+        hipLaunchKernelGGL((attend_finish_kernel<F32, D, most>), folded_grid(all), dim3(256), 0, s, part, (T*)c.O, c.LSE, logits, c.mix_len, c.weight,
+                           c.weight_out, c.T, d->n_q_heads, d->n_kv_heads, c.l_cap, p.stride, p.n_split, (int)n_merge, (int)n_blocks, all);
+    };
+    if (rows <= 8) finish(std::integral_constant<int, 8>{});
+    else finish(std::integral_constant<int, 32>{});
+    return mixed_launched();
+}
+
 static vxl_status launch_step(const MixedPlan& p, const MixedCall& c, const Sets& sets, const Rule& rule, hipStream_t s) {
     const vxl_attn_desc* d = c.d;
     const int units = c.batch * d->n_kv_heads, rows = d->n_q_heads / d->n_kv_heads * c.T;
@@ -1224,16 +1519,7 @@ static vxl_status launch_step(const MixedPlan& p, const MixedCall& c, const Sets
         hipLaunchKernelGGL((attend_step_kernel<dim, pos>), dim3(p.n_split, units), dim3(64 * kStepWaves), C::LDS_BYTES, s, sets, rule, part,
                            (uint16_t*)c.O, c.LSE, logits, p.stride, p.n_split);
         st = mixed_launched();
-        if (st != VXL_OK || (p.n_split == 1 && !logits)) return st;
-        const long long n_merge = p.n_split > 1 ? (long long)units * rows : 0, n_blocks = logits ? (c.l_cap + 1023) / 1024 : 0;
-        const long long all = n_merge + units * n_blocks;
-        auto finish = [&](auto most) {
-            hipLaunchKernelGGL((attend_finish_kernel<false, dim, most>), folded_grid(all), dim3(256), 0, s, part, (uint16_t*)c.O, c.LSE, logits, c.mix_len,
-                               c.weight, c.weight_out, c.T, d->n_q_heads, d->n_kv_heads, c.l_cap, p.stride, p.n_split, (int)n_merge, (int)n_blocks, all);
-        };
-        if (rows <= 8) finish(std::integral_constant<int, 8>{});
-        else finish(std::integral_constant<int, 32>{});
-        return mixed_launched();
+        return st != VXL_OK ? st : launch_finish<false, dim>(p, c, part, logits, s);
     };
     auto by_pos = [&](auto dim) { return rule.q_pos ? run(dim, std::true_type{}) : run(dim, std::false_type{}); };
     return d->head_dim == 64 ? by_pos(std::integral_constant<int, 64>{}) : by_pos(std::integral_constant<int, 128>{});
@@ -1275,6 +1561,29 @@ static vxl_status launch_weights(const MixedPlan& p, const MixedCall& c, const S
     return mixed_launched();
 }
 
+static vxl_status launch_merge(const MixedPlan& p, const MixedCall& c, hipStream_t s);
+
+static vxl_status launch_f32(const MixedPlan& p, const MixedCall& c, const Sets& sets, const Rule& rule, hipStream_t s) {
+    const vxl_attn_desc* d = c.d;
+    const int units = c.batch * d->n_kv_heads, rows = d->n_q_heads / d->n_kv_heads * c.T, n_rtile = (rows + kF32Block - 1) / kF32Block;
+    const Partials part{(float*)(c.ws + p.part_o), (float2*)(c.ws + p.part_ml)};
+    float *logits = p.few && c.weight_out ? (float*)(c.ws + p.logits) : nullptr, *lse2 = (float*)(c.ws + p.lse2);
+    auto run = [&](auto dim, auto pos) {
+        hipLaunchKernelGGL((attend_f32_kernel<dim, pos>), placed_grid((long long)units * p.n_split * n_rtile), dim3(64 * kF32Waves), 0, s, sets, rule, part,
+                           (float*)c.O, c.LSE, lse2, logits, p.stride, units, p.n_split, n_rtile);
+        vxl_status st = mixed_launched();
+        if (st != VXL_OK) return st;
+        if (p.few) return launch_finish<true, dim>(p, c, part, logits, s);
+        if (p.n_split > 1) st = launch_merge(p, c, s);
+        if (st != VXL_OK || !c.weight_out) return st;
+        hipLaunchKernelGGL((weights_f32_kernel<dim, pos>), dim3((c.l_cap + kF32Tile - 1) / kF32Tile, units), dim3(64 * kF32Waves), 0, s, sets, rule, lse2,
+                           c.weight, c.weight_out);
+        return mixed_launched();
+    };
+    auto by_pos = [&](auto dim) { return rule.q_pos ? run(dim, std::true_type{}) : run(dim, std::false_type{}); };
+    return d->head_dim == 64 ? by_pos(std::integral_constant<int, 64>{}) : by_pos(std::integral_constant<int, 128>{});
+}
+
 static vxl_status launch_simple(const MixedPlan& p, const MixedCall& c, const Sets& sets, const Rule& rule, hipStream_t s) {
     const vxl_attn_desc* d = c.d;
     const long long n_rows = (long long)c.batch * c.T * d->n_q_heads;
@@ -1296,7 +1605,8 @@ vxl_status launch_mixed_attend(const MixedPlan& p, const MixedCall& c, bool forc
     const Rule rule{c.scale * kLog2e, u.softcap > 0.f ? c.scale / u.softcap : 0.f, u.softcap * kLog2e, u.causal, u.window, u.n_always, u.slopes,
                     c.q_pos, c.row_pos};
     const Sets sets{c.Qd, c.Kmix, c.Vmix, c.mix_len, c.T, d->n_q_heads, d->n_kv_heads, c.l_cap};
-    if (force_simple || d->dtype != VXL_BF16) return launch_simple(p, c, sets, rule, s);
+    if (force_simple) return launch_simple(p, c, sets, rule, s);
+    if (d->dtype == VXL_F32) return launch_f32(p, c, sets, rule, s);
     if (p.few) return launch_step(p, c, sets, rule, s);
     vxl_status st = launch_ring(p, c, sets, rule, s);
     if (st == VXL_OK && p.n_split > 1) st = launch_merge(p, c, s);
