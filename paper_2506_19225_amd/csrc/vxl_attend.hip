@@ -1505,7 +1505,7 @@ static vxl_status launch_finish(const MixedPlan& p, const MixedCall& c, const Pa
 
 static vxl_status launch_step(const MixedPlan& p, const MixedCall& c, const Sets& sets, const Rule& rule, hipStream_t s) {
     const vxl_attn_desc* d = c.d;
-    const int units = c.batch * d->n_kv_heads, rows = d->n_q_heads / d->n_kv_heads * c.T;
+    const int units = c.batch * d->n_kv_heads;
     const Partials part{(float*)(c.ws + p.part_o), (float2*)(c.ws + p.part_ml)};
     float* logits = c.weight_out ? (float*)(c.ws + p.logits) : nullptr;
     auto run = [&](auto dim, auto pos) {

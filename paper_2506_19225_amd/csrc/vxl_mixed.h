@@ -53,6 +53,7 @@ vxl_status launch_mixed_attend(const MixedPlan& p, const MixedCall& c, bool forc
 struct EvictPlan {
     size_t map;                // byte offset of [batch][Hkv][l_cap] source rows
     size_t n;                  // of [batch] numbers of rows kept
+    size_t states;             // of what the launches of long sets leave each other
     size_t total;
 };
 EvictPlan evict_plan(const vxl_attn_desc* d, int batch, int l_cap);
