@@ -504,7 +504,7 @@ struct StepCfg {
     static constexpr int PPR = D / 8, RPI = 64 / PPR, NL = kStepTile / RPI;       // pieces of a row; rows, loads of a tile
 };
 
-template <int D, bool POS>
+template <int D, bool POS, bool ONCE>
 __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s, Rule r, Partials part, uint16_t* __restrict__ O, float* __restrict__ LSE,
                                                                          float* __restrict__ logits, int stride, int n_split) {
     using C = StepCfg<D>;
@@ -535,8 +535,8 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s,
             constexpr int CPR = D * 2 / 64, RPL = D == 128 ? 1 : 2;
             const int vp = (((pp >> 2) ^ ((row / RPL) & (CPR - 1))) << 2) | (pp & 3);
             const uint32_t kdst = lds_w + (uint32_t)buf * (4 * C::TILE) + x * 1024, roff = (uint32_t)min(row, rlim) * (D * 2);
-            dma16(kb, roff + kp * 16, kdst);
-            dma16(vb, roff + vp * 16, kdst + 2 * C::TILE);
+            dma16_as<ONCE>(kb, roff + kp * 16, kdst);
+            dma16_as<ONCE>(vb, roff + vp * 16, kdst + 2 * C::TILE);
         }
         if constexpr (POS) dma4(pos + key0, (uint32_t)min(lane, rlim) * 4, lds_pos + buf * 256);
     };
@@ -711,7 +711,7 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s,
     }
 }
 
-// The merge of the splits of one query row by a workgroup: SG groups of D / 4 lanes take every SG-th split, four requested together, and are
+// The merge of the splits of one query row by a workgroup: SG groups of D / 4 lanes take every SG-th split, six requested together, and are
 // folded through LDS in their order.
 template <bool F32, int D>
 struct MergeArea {
@@ -722,7 +722,7 @@ struct MergeArea {
 template <bool F32, int D>
 __device__ __forceinline__ void merge_row(MergeArea<F32, D>& area, const Partials& part, typename Storage<F32>::T* O, float* LSE, float* lse2,
                                           int T, int n_q, int n_kv, int n_split, long long id) {
-    constexpr int NV = D / 4, SG = 256 / NV, U = 4;
+    constexpr int NV = D / 4, SG = 256 / NV, U = 6;
     const int group = n_q / n_kv, n_rows = T * group, sg = threadIdx.x / NV, d = threadIdx.x % NV * 4;
     const int rho = (int)(id % n_rows);
     const long long unit = id / n_rows;
@@ -795,7 +795,7 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typen
                                                             const float* weight, float* weight_out, int T, int n_q, int n_kv, int cap, int stride,
                                                             int n_split, int n_merge, int n_blocks, long long all) {
     __shared__ MergeArea<F32, D> area;
-    __shared__ float2 ml_lds[256 / R][R];
+    __shared__ float2 ml_lds[4][R];
     __shared__ float lse_lds[R];
     long long id = folded_id();
     if (id >= all) return;
@@ -804,40 +804,48 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typen
         return;
     }
     id -= n_merge;
-    const int unit = (int)(id / n_blocks), key = ((int)(id % n_blocks) * 256 + (int)threadIdx.x) * 4, n_rows = n_q / n_kv * T;
-    const int len = min(max(mix_len[unit / n_kv], 0), cap);
-    if ((int)(id % n_blocks) * 1024 >= len) return;
-    const float* y = logits + (size_t)unit * n_rows * stride + min(key, (len - 1) / 4 * 4);
+    const int unit = (int)(id / n_blocks), key0 = (int)(id % n_blocks) * 1024, key = key0 + (int)threadIdx.x * 4, n_rows = n_q / n_kv * T;
+    const size_t set = (size_t)unit * cap;
+    // Everything is requested before anything is waited for: logits and weights of rows up to the capacity, whatever the length.
+    const float* y = logits + (size_t)unit * n_rows * stride + min(key, stride - 4);
     float4 first[8];
+    float w_in[4];
 #pragma unroll
     for (int i = 0; i < 8; ++i) first[i] = *(const float4*)(y + (size_t)min(i, n_rows - 1) * stride);
-    // LSE of the query rows: R threads each take every (256 / R)-th split
-    constexpr int SG = 256 / R;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w_in[j] = weight ? weight[set + min(key + j, cap - 1)] : 0.f;
+    // LSE of the query rows: every (256 / R)-th split by each of R threads, four requested together, joined over the lanes and waves.
+    constexpr int SG = 256 / R, U = 4;
     const int row = threadIdx.x % R, sg = threadIdx.x / R;
-    float M = -INFINITY, L = 0.f;
-    for (int sp = sg; sp < n_split; sp += SG) {
-        const float2 ml = part.ml[((size_t)unit * n_split + sp) * n_rows + min(row, n_rows - 1)];
-        const float m_new = fmaxf(M, ml.x), ref = m_new == -INFINITY ? 0.f : m_new;
-        L = L * part_weight(make_float2(M, L), ref);
-        L = add_part(part_weight(ml, ref), ml.y, L);
-        M = m_new;
+    const float2* ml = part.ml + (size_t)unit * n_split * n_rows + min(row, n_rows - 1);
+    float2 sum = make_float2(-INFINITY, 0.f);
+    auto join = [](float2 a, float2 b) __attribute__((always_inline)) {
+        const float M = fmaxf(a.x, b.x), ref = M == -INFINITY ? 0.f : M;
+        return make_float2(M, add_part(part_weight(a, ref), a.y, add_part(part_weight(b, ref), b.y, 0.f)));
+    };
+    for (int s0 = sg; s0 < n_split; s0 += U * SG) {
+        float2 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = ml[(size_t)min(s0 + u * SG, n_split - 1) * n_rows];
+#pragma unroll
+        for (int u = 0; u < U; ++u) sum = join(sum, s0 + u * SG < n_split ? v[u] : make_float2(-INFINITY, 0.f));
     }
-    ml_lds[sg][row] = make_float2(M, L);
+    const int len = min(max(mix_len[unit / n_kv], 0), cap);
+    if (key0 >= len) return;
+#pragma unroll
+    for (int o = R; o < 64; o <<= 1) sum = join(sum, make_float2(__shfl_xor(sum.x, o), __shfl_xor(sum.y, o)));
+    if (threadIdx.x % 64 < R) ml_lds[threadIdx.x / 64][row] = sum;
     __syncthreads();
     if (threadIdx.x < R) {
-        M = -INFINITY;
-        L = 0.f;
-        for (int i = 0; i < SG; ++i) M = fmaxf(M, ml_lds[i][row].x);
-        const float ref = M == -INFINITY ? 0.f : M;
-        for (int i = 0; i < SG; ++i) L = add_part(part_weight(ml_lds[i][row], ref), ml_lds[i][row].y, L);
-        lse_lds[row] = L == 0.f || row >= n_rows ? INFINITY : M + __builtin_amdgcn_logf(L);          // (weighs nothing)
+        sum = join(join(ml_lds[0][row], ml_lds[1][row]), join(ml_lds[2][row], ml_lds[3][row]));
+        lse_lds[row] = sum.y == 0.f || row >= n_rows ? INFINITY : sum.x + __builtin_amdgcn_logf(sum.y);          // (weighs nothing)
     }
     __syncthreads();
     float w[4] = {0.f, 0.f, 0.f, 0.f};
     auto add = [&](float4 v, float lse) __attribute__((always_inline)) {
         const float x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] += x[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[j] - lse);
+        for (int j = 0; j < 4; ++j) w[j] += __builtin_amdgcn_exp2f(x[j] == -INFINITY ? -INFINITY : x[j] - lse);
     };
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -845,10 +853,9 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typen
     if constexpr (R > 8)
 #pragma unroll 4
         for (int i = 8; i < n_rows; ++i) add(*(const float4*)(y + (size_t)i * stride), lse_lds[i]);
-    const size_t set = (size_t)unit * cap;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        if (key + j < len) weight_out[set + key + j] = (weight ? weight[set + key + j] : 0.f) + w[j];
+        if (key + j < len) weight_out[set + key + j] = w_in[j] + w[j];
 }
 
 // ------------------------------------------------------------------------------------------
@@ -1503,25 +1510,28 @@ static vxl_status launch_finish(const MixedPlan& p, const MixedCall& c, const Pa
     return mixed_launched();
 }
 
+constexpr size_t kPastCachesBytes = 32u << 20;
 static vxl_status launch_step(const MixedPlan& p, const MixedCall& c, const Sets& sets, const Rule& rule, hipStream_t s) {
     const vxl_attn_desc* d = c.d;
     const int units = c.batch * d->n_kv_heads;
     const Partials part{(float*)(c.ws + p.part_o), (float2*)(c.ws + p.part_ml)};
     float* logits = c.weight_out ? (float*)(c.ws + p.logits) : nullptr;
-    auto run = [&](auto dim, auto pos) {
+    auto run = [&](auto dim, auto pos, auto once) {
         using C = StepCfg<dim>;
         static PerDeviceOnce attr;
         vxl_status st = attr.run([&] {
-            VXL_HIP_TRY(hipFuncSetAttribute((const void*)attend_step_kernel<dim, pos>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES));
+            VXL_HIP_TRY(hipFuncSetAttribute((const void*)attend_step_kernel<dim, pos, once>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES));
             return VXL_OK;
         });
         if (st != VXL_OK) return st;
-        hipLaunchKernelGGL((attend_step_kernel<dim, pos>), dim3(p.n_split, units), dim3(64 * kStepWaves), C::LDS_BYTES, s, sets, rule, part,
+        hipLaunchKernelGGL((attend_step_kernel<dim, pos, once>), dim3(p.n_split, units), dim3(64 * kStepWaves), C::LDS_BYTES, s, sets, rule, part,
                            (uint16_t*)c.O, c.LSE, logits, p.stride, p.n_split);
         st = mixed_launched();
         return st != VXL_OK ? st : launch_finish<false, dim>(p, c, part, logits, s);
     };
-    auto by_pos = [&](auto dim) { return rule.q_pos ? run(dim, std::true_type{}) : run(dim, std::false_type{}); };
+    const bool big = (size_t)units * c.l_cap * d->head_dim * 2 * 2 > kPastCachesBytes;
+    auto by_size = [&](auto dim, auto pos) { return big ? run(dim, pos, std::true_type{}) : run(dim, pos, std::false_type{}); };
+    auto by_pos = [&](auto dim) { return rule.q_pos ? by_size(dim, std::true_type{}) : by_size(dim, std::false_type{}); };
     return d->head_dim == 64 ? by_pos(std::integral_constant<int, 64>{}) : by_pos(std::integral_constant<int, 128>{});
 }
 
