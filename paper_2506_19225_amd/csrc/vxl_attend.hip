@@ -21,25 +21,29 @@ struct Rule {
     const int32_t *q_pos, *row_pos;
 };
 
-// Rows that a token sees: positions lo .. hi and 0 .. na - 1.  A padding token: none.  (Without positions every row of the set has
+// Rows that a token sees: positions lo .. lo + width - 1 and 0 .. na - 1.  A padding token: none.  (Without positions every row of the set has
 // position 0 and every token sees it.)
 struct Span {
-    int lo, hi;
-    unsigned na;
+    int lo;
+    unsigned width, na;
+    __device__ __forceinline__ int hi() const { return (int)((unsigned)lo + width - 1u); }       // (of one that is not empty)
 };
 __device__ __forceinline__ Span span_of(const Rule& r, int pq) {
-    if (!r.q_pos) return {0, 0, 0u};
-    if (pq < 0) return {1, 0, 0u};
-    return {r.window ? max(pq - r.window + 1, 0) : 0, r.causal ? pq : INT32_MAX, (unsigned)r.n_always};
+    if (!r.q_pos) return {0, 1u, 0u};
+    if (pq < 0) return {0, 0u, 0u};
+    const int lo = r.window ? max(pq - r.window + 1, 0) : 0, hi = r.causal ? pq : INT32_MAX;
+    return {lo, (unsigned)hi - (unsigned)lo + 1u, (unsigned)r.n_always};
 }
-// (Negative where a row of position pk is hidden: by signs alone, as comparisons that are joined go through scalar registers and wait for
-// them.  Differences wrap for negative pk alone, and of a token's span, which is not empty or {1, 0}, never both; of bounds over several tokens,
-// for pk of -1 or more, none does.)
-__device__ __forceinline__ int hides(const Span& s, int pk) {
-    const unsigned p = (unsigned)pk, beyond = (p - (unsigned)s.lo) | ((unsigned)s.hi - p), first = (p - s.na) & ~p;
-    return (int)(beyond & ~first);
+// (A negative position is 2^31 or more as it is and with lo taken off.)
+__device__ __forceinline__ bool sees(const Span& s, int pk) { return ((unsigned)pk - (unsigned)s.lo < s.width) | ((unsigned)pk < s.na); }
+// A logit, or -inf where it is hidden; FIRST: there may be an na.  Selections one after the other: comparisons that are joined go through scalar
+// registers and wait for them.
+template <bool FIRST>
+__device__ __forceinline__ float shown(const Span& s, int pk, float y) {
+    float z = (unsigned)pk - (unsigned)s.lo < s.width ? y : -INFINITY;
+    if constexpr (FIRST) z = (unsigned)pk < s.na ? y : z;
+    return z;
 }
-__device__ __forceinline__ bool sees(const Span& s, int pk) { return hides(s, pk) >= 0; }
 
 // Sets as the kernels see them.
 struct Sets {
@@ -204,16 +208,19 @@ __device__ __forceinline__ bool place(int units, int n_split, int n_rtile, int* 
 struct Reach {
     Span most, least;
     __device__ __forceinline__ void of(const Span& s) {
-        most = least = s;
+        int lo = s.width ? s.lo : INT32_MAX, hi = s.width ? s.hi() : -1, lo_most = lo, hi_least = hi;
+        unsigned na = s.na, na_least = s.na;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
-            most.lo = min(most.lo, __shfl_xor(most.lo, o));
-            most.hi = max(most.hi, __shfl_xor(most.hi, o));
-            most.na = max(most.na, (unsigned)__shfl_xor((int)most.na, o));
-            least.lo = max(least.lo, __shfl_xor(least.lo, o));
-            least.hi = min(least.hi, __shfl_xor(least.hi, o));
-            least.na = min(least.na, (unsigned)__shfl_xor((int)least.na, o));
+            lo = min(lo, __shfl_xor(lo, o));
+            hi = max(hi, __shfl_xor(hi, o));
+            na = max(na, (unsigned)__shfl_xor((int)na, o));
+            lo_most = max(lo_most, __shfl_xor(lo_most, o));
+            hi_least = min(hi_least, __shfl_xor(hi_least, o));
+            na_least = min(na_least, (unsigned)__shfl_xor((int)na_least, o));
         }
+        most = {lo, hi >= lo ? (unsigned)hi - (unsigned)lo + 1u : 0u, na};
+        least = {lo_most, hi_least >= lo_most ? (unsigned)hi_least - (unsigned)lo_most + 1u : 0u, na_least};
     }
 };
 
@@ -334,7 +341,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_ring_kernel(Sets s, Rule r,
         bool partial = left < kKeyTile;
         const int32_t* tile_pos = (const int32_t*)((const char*)lds + C::POS_AT) + (ti % C::NS) * kKeyTile;
         if constexpr (POS) {
-            const int pk = lane < left ? max(tile_pos[lane], -1) : -1;
+            const int pk = lane < left ? tile_pos[lane] : -1;
             if (__builtin_amdgcn_ballot_w64(sees(reach.most, pk)) == 0) return;
             partial = ~__builtin_amdgcn_ballot_w64(sees(reach.least, pk)) != 0;
         }
@@ -366,7 +373,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_ring_kernel(Sets s, Rule r,
                     }
             };
             if (biased) by_position([&](float y, int p, int) { return fmaf(-slope2, (float)abs(pq - p), y * unit_of); });
-            if (partial) by_position([&](float y, int p, int key) { return (hides(span, p) | (left - 1 - key)) >= 0 ? y : -INFINITY; });
+            if (partial) {
+                if (r.n_always > 0) by_position([&](float y, int p, int) { return shown<true>(span, p, y); });
+                else by_position([&](float y, int p, int) { return shown<false>(span, p, y); });
+                if (left < kKeyTile) by_position([&](float y, int, int key) { return key < left ? y : -INFINITY; });
+            }
         } else if (partial) {
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
@@ -606,10 +617,10 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s,
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int j = jq * 4 + e;
-                const bool sees_it = (hides(span, p[e]) | (left - 1 - acc_key(0, j, hi))) >= 0;
+                const int pk = acc_key(0, j, hi) < left ? p[e] : -1;
                 const float kept_as = y[j] * cu;
-                seen[j] = !sees_it ? -INFINITY : kept_as == -INFINITY ? kLowest : kept_as;
-                y[j] = sees_it ? y[j] : -INFINITY;
+                seen[j] = shown<true>(span, pk, kept_as == -INFINITY ? kLowest : kept_as);
+                y[j] = shown<true>(span, pk, y[j]);
             }
             if (kept && l32 < n_rows)
                 *(float4*)(kept + tile * TK + jq * 8 + hi * 4) = make_float4(seen[jq * 4], seen[jq * 4 + 1], seen[jq * 4 + 2], seen[jq * 4 + 3]);
@@ -1027,7 +1038,8 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     const Span span = span_of(r, pos_of(half));
-                    all &= ~__builtin_amdgcn_ballot_w64(pk_min >= 0 && ((pk_min >= span.lo && pk_max <= span.hi) || (unsigned)pk_max < span.na)) == 0;
+                    const bool within = ((unsigned)pk_min - (unsigned)span.lo < span.width) & ((unsigned)pk_max - (unsigned)span.lo < span.width);
+                    all &= ~__builtin_amdgcn_ballot_w64((pk_min >= 0) & (within | ((unsigned)pk_max < span.na))) == 0;
                 }
             }
             if (all && !capped && !biased) {
@@ -1045,7 +1057,7 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
                 row.pq = pos_of(half);
                 row.span = span_of(r, row.pq);
                 if constexpr (POS) {
-                    const bool hidden = (pk_max < row.span.lo || pk_min > row.span.hi) && (pk_max < 0 || (unsigned)max(pk_min, 0) >= row.span.na);
+                    const bool hidden = (row.span.width == 0 || pk_max < row.span.lo || pk_min > row.span.hi()) && (pk_max < 0 || (unsigned)max(pk_min, 0) >= row.span.na);
                     if (__builtin_amdgcn_ballot_w64(!hidden) == 0) continue;
                 }
                 row.lse = lse_of(half);
@@ -1067,7 +1079,8 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
                 if (all) {
                     plain(x, row.lse);
                 } else {                                      // (what is not seen has weight 0, also where the LSE is no number)
-                    by_position(x, [&](float y, int p) { return __builtin_amdgcn_exp2f(sees(row.span, p) ? fmaf(y, cu, -row.lse) : -INFINITY); });
+                    if (r.n_always > 0) by_position(x, [&](float y, int p) { return __builtin_amdgcn_exp2f(shown<true>(row.span, p, fmaf(y, cu, -row.lse))); });
+                    else by_position(x, [&](float y, int p) { return __builtin_amdgcn_exp2f(shown<false>(row.span, p, fmaf(y, cu, -row.lse))); });
 #pragma unroll
                     for (int kb = 0; kb < 2; ++kb) acc[kb] += x[kb];
                 }
