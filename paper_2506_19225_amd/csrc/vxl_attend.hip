@@ -894,8 +894,7 @@ struct WeightsCfg {
 
 template <int D, bool POS>
 __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Sets s, Rule r, const float* __restrict__ lse2, const float* weight,
-                                                                              float* weight_out, float* __restrict__ part_w, int units, int n_part,
-                                                                              int n_blocks) {
+                                                                              float* weight_out, float* __restrict__ part_w, int units, int n_part) {
     using C = WeightsCfg<D>;
     struct Row {               // of a query row, as a lane needs it
         float lse, slope2;     // (lse +inf: weighs nothing)
@@ -907,11 +906,12 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int unit, part, block;
-    if (!place(units, n_part, n_blocks, &unit, &part, &block)) return;
-    const int g = unit % s.n_kv, b = unit / s.n_kv, group = s.n_q / s.n_kv, n_rows = group * s.T;
-    const int len = min(max(s.len[b], 0), s.cap);
-    if (block * kWeightKeys >= len) return;
+    // The last rows of a set first: new ones, which later tokens see and earlier ones do not, take longest.
+    const unsigned id = folded_id(), pairs = (unsigned)(units * n_part);
+    const int unit = (int)(id % pairs) / n_part, part = (int)(id % pairs) % n_part, g = unit % s.n_kv, b = unit / s.n_kv;
+    const int group = s.n_q / s.n_kv, n_rows = group * s.T, len = min(max(s.len[b], 0), s.cap);
+    const int block = (len + kWeightKeys - 1) / kWeightKeys - 1 - (int)(id / pairs);
+    if (block < 0) return;
     const size_t set = (size_t)unit * s.cap;
     const int key0 = block * kWeightKeys + wave * 64;
     const bool active = key0 < len;
@@ -1572,8 +1572,8 @@ static vxl_status launch_weights(const MixedPlan& p, const MixedCall& c, const S
             return VXL_OK;
         });
         if (st != VXL_OK) return st;
-        hipLaunchKernelGGL((attend_weights_kernel<dim, pos>), placed_grid((long long)units * p.n_part * n_blocks), dim3(64 * kWeightWaves), lds, s, sets,
-                           rule, lse2, c.weight, c.weight_out, part_w, units, p.n_part, n_blocks);
+        hipLaunchKernelGGL((attend_weights_kernel<dim, pos>), folded_grid((long long)units * p.n_part * n_blocks), dim3(64 * kWeightWaves), lds, s, sets,
+                           rule, lse2, c.weight, c.weight_out, part_w, units, p.n_part);
         return mixed_launched();
     };
     auto by_pos = [&](auto dim) { return rule.q_pos ? run(dim, std::true_type{}) : run(dim, std::false_type{}); };
