@@ -47,6 +47,18 @@ struct Found {
     int left;                  // rows of that bin that are among the n
     int rows;                  // rows of that bin
 };
+// Sums over the lanes up to this one, in the order of lanes (shifts inside rows of 16 lanes, then the last lane of a row, of two, to those behind:
+// a few cycles each, where a shuffle goes through the LDS).
+__device__ __forceinline__ int scan_lanes(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+
 // From counts of this pass's bins, of which thread t has c0 in bin 2047 - 2 t and c1 in the one below.
 struct FindArea {
     int wave_sum[kWaves];
@@ -54,12 +66,7 @@ struct FindArea {
 };
 __device__ __forceinline__ void find_bin(FindArea& a, int c0, int c1, int pass, Found& f) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int run = c0 + c1;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int x = __shfl_up(run, o);
-        if (lane >= o) run += x;
-    }
+    const int run = scan_lanes(c0 + c1);
     if (lane == 63) a.wave_sum[wave] = run;
     __syncthreads();
     int before = run - c0 - c1;
@@ -76,14 +83,24 @@ __device__ __forceinline__ void find_bin(FindArea& a, int c0, int c1, int pass, 
 
 // A row of D elements by ROW16 lanes.
 template <int ROW16>
-__device__ __forceinline__ void move_row(const Cut& c, const Move& m, size_t from, size_t to, int part) {
-    const uint4 k = m.k[from * ROW16 + part], v = m.v[from * ROW16 + part];
+__device__ __forceinline__ void load_row(const Move& m, size_t from, int part, uint4& k, uint4& v) {
+    k = m.k[from * ROW16 + part];
+    v = m.v[from * ROW16 + part];
+}
+template <int ROW16>
+__device__ __forceinline__ void store_row(const Cut& c, const Move& m, size_t from, size_t to, int part, const uint4& k, const uint4& v) {
     m.k_out[to * ROW16 + part] = k;
     m.v_out[to * ROW16 + part] = v;
     if (part == 0) {
         m.weight_out[to] = c.weight[from];
         m.pos_out[to] = c.row_pos[from];
     }
+}
+template <int ROW16>
+__device__ __forceinline__ void move_row(const Cut& c, const Move& m, size_t from, size_t to, int part) {
+    uint4 k, v;
+    load_row<ROW16>(m, from, part, k, v);
+    store_row<ROW16>(c, m, from, to, part, k, v);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -117,6 +134,11 @@ __global__ __launch_bounds__(kThreads) void evict_set_kernel(Cut c, Move m, int3
         else n_out[b] = n;
     }
     if (n == 0) return;
+    // Most rows stay where they are: the first row of a thread's share is on its way while the set is looked through.
+    constexpr int ROWS = kThreads / ROW16;
+    const int part = tid % ROW16, own = blockIdx.x * ROWS + tid / ROW16;
+    uint4 own_k = make_uint4(0, 0, 0, 0), own_v = own_k;
+    if (MOVES && own < n) load_row<ROW16>(m, set + own, part, own_k, own_v);
     uint32_t x[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) x[i] = preference(w[i], pos[i], c.n_first, latest, c.n_recent);
@@ -195,10 +217,13 @@ __global__ __launch_bounds__(kThreads) void evict_set_kernel(Cut c, Move m, int3
     }
     __syncthreads();
     if constexpr (MOVES) {
-        constexpr int ROWS = kThreads / ROW16;
-        const int part = tid % ROW16;
         const size_t to = (size_t)unit * m.out_cap;
-        for (int row = blockIdx.x * ROWS + tid / ROW16; row < n; row += gridDim.x * ROWS) move_row<ROW16>(c, m, set + source[row], to + row, part);
+        if (own < n) {
+            const int from = source[own];
+            if (from != own) load_row<ROW16>(m, set + from, part, own_k, own_v);
+            store_row<ROW16>(c, m, set + from, to + own, part, own_k, own_v);
+        }
+        for (int row = own + gridDim.x * ROWS; row < n; row += gridDim.x * ROWS) move_row<ROW16>(c, m, set + source[row], to + row, part);
     } else {
         for (int row = tid; row < n; row += kThreads) places[set + row] = source[row];
     }
@@ -330,12 +355,7 @@ __global__ __launch_bounds__(kThreads) void evict_places_kernel(Cut c, const Sta
     int equal, holes, movers;
     {
         const int i = min(lane, kParts - 1), same = lane < kParts ? equals[i] : 0;
-        int upto = same;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int x = __shfl_up(upto, o);
-            if (lane >= o) upto += x;
-        }
+        const int upto = scan_lanes(same);
         const int kept = above[i] + min(max(f.left - (upto - same), 0), same);
         const Part at = part_of(i, first, n, len, part_rows);
         equal = lane < part ? same : 0;
