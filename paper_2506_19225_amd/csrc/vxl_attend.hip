@@ -517,11 +517,13 @@ struct StepCfg {
 
 template <int D, bool POS, bool ONCE>
 __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s, Rule r, Partials part, uint16_t* __restrict__ O, float* __restrict__ LSE,
-                                                                         float* __restrict__ logits, int stride, int n_split) {
+                                                                         float* logits, int stride, int n_split, const float* weight,
+                                                                         float* weight_out) {
     using C = StepCfg<D>;
     constexpr int NW = kStepWaves, TK = kStepTile, PPR = C::PPR, NL = C::NL;
     extern __shared__ __attribute__((aligned(16))) uint16_t lds[];
     __shared__ float2 stats[NW][kStepRows];
+    __shared__ float lse_lds[kStepRows];
     __shared__ __attribute__((aligned(16))) float q_lds[NW][D];                   // (of rows made again)
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hi = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -572,6 +574,9 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s,
     asm volatile("" :: "v"(pq), "v"(slope2), "v"(len));
     wait_vmcnt<0>();
     const Span span = span_of(r, pq);
+    Reach reach;
+    if (s.T == 1) reach.most = reach.least = span;            // (all rows are one token's)
+    else reach.of(span);
     const int n_tiles = (len + TK - 1) / TK, n = tile0 < n_tiles ? (n_tiles - tile0 + every - 1) / every : 0;
     // Rows past the length may hold anything (0 * NaN): the one tile that straddles it is fetched again, its rows the last one.
     if (n > 0 && tile0 * TK + TK > len) {
@@ -597,9 +602,21 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s,
         __builtin_amdgcn_wave_barrier();
         const uint16_t *kt = area + (i & 1) * 2 * C::TILE, *vt = kt + C::TILE;
         const int32_t* tile_pos = (const int32_t*)((const char*)lds + C::POS_AT) + (wave * 2 + (i & 1)) * 64;
+        bool all = left >= TK;                                // all rows see all keys
+        if constexpr (POS) {
+            const int pk = l32 < left ? tile_pos[l32] : -1;
+            if (__builtin_amdgcn_ballot_w64(sees(reach.most, pk)) == 0) {
+                if (kept && l32 < n_rows)
+#pragma unroll
+                    for (int jq = 0; jq < 4; ++jq)
+                        *(float4*)(kept + tile * TK + jq * 8 + hi * 4) = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                continue;
+            }
+            all &= ~__builtin_amdgcn_ballot_w64(sees(reach.least, pk)) == 0;
+        }
         f32x16 x[1][1];
         qk_tile<D, 1, 1>(kt, qreg, l32, hi, x);
-        float y[16], seen[16];                                // logits; the same as kept for the weights
+        float y[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) y[j] = x[0][0][j];
         if (capped) cap_logits(y, r);
@@ -607,24 +624,34 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s,
 #pragma unroll
             for (int j = 0; j < 16; ++j) y[j] = fmaf(-slope2, (float)abs(pq - tile_pos[acc_key(0, j, hi)]), y[j] * unit_of);
         }
-#pragma unroll
-        for (int jq = 0; jq < 4; ++jq) {
-            int p[4] = {0, 0, 0, 0};
-            if constexpr (POS) {
-                const int4 p4 = *(const int4*)(tile_pos + jq * 8 + hi * 4);
-                p[0] = p4.x; p[1] = p4.y; p[2] = p4.z; p[3] = p4.w;
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = jq * 4 + e;
-                const int pk = acc_key(0, j, hi) < left ? p[e] : -1;
-                const float kept_as = y[j] * cu;
-                seen[j] = shown<true>(span, pk, kept_as == -INFINITY ? kLowest : kept_as);
-                y[j] = shown<true>(span, pk, y[j]);
-            }
+        auto keep = [&](const float (&v)[16]) __attribute__((always_inline)) {
             if (kept && l32 < n_rows)
-                *(float4*)(kept + tile * TK + jq * 8 + hi * 4) = make_float4(seen[jq * 4], seen[jq * 4 + 1], seen[jq * 4 + 2], seen[jq * 4 + 3]);
+#pragma unroll
+                for (int jq = 0; jq < 4; ++jq)
+                    *(float4*)(kept + tile * TK + jq * 8 + hi * 4) = make_float4(v[jq * 4], v[jq * 4 + 1], v[jq * 4 + 2], v[jq * 4 + 3]);
+        };
+        auto kept_as = [&](float z) { return z * cu == -INFINITY ? kLowest : z * cu; };
+        float v[16];
+        if (all) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = kept_as(y[j]);
+        } else {
+#pragma unroll
+            for (int jq = 0; jq < 4; ++jq) {
+                int p[4] = {0, 0, 0, 0};
+                if constexpr (POS) {
+                    const int4 p4 = *(const int4*)(tile_pos + jq * 8 + hi * 4);
+                    p[0] = p4.x; p[1] = p4.y; p[2] = p4.z; p[3] = p4.w;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = jq * 4 + e, pk = acc_key(0, j, hi) < left ? p[e] : -1;
+                    v[j] = shown<true>(span, pk, kept_as(y[j]));
+                    y[j] = shown<true>(span, pk, y[j]);
+                }
+            }
         }
+        keep(v);
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 16; ++j) top = fmaxf(top, y[j]);
@@ -691,34 +718,66 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s,
     }
     __syncthreads();
     const size_t part_row0 = ((size_t)unit * n_split + split) * n_rows;
-    for (int e = tid; e < n_rows * PPR4; e += 64 * NW) {
-        const int row = e / PPR4, c = e % PPR4;
-        float2 st[NW];
-        float M = -INFINITY, L = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+    constexpr int ITEMS = kStepRows * PPR4 / (64 * NW);       // pieces of a thread at most: all read before any is worked on
+    float2 st[ITEMS][NW];
+    float4 v[ITEMS][NW];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        if (i * 64 * NW >= n_rows * PPR4) break;
+        const int e = min(i * 64 * NW + tid, n_rows * PPR4 - 1), row = e / PPR4, c = e % PPR4;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            st[w] = stats[w][row];
-            M = fmaxf(M, st[w].x);
+            st[i][w] = stats[w][row];
+            v[i][w] = *(const float4*)((const float*)(lds + w * C::AREA) + (row * PPR4 + (c ^ (row & (PPR4 - 1)))) * 4);
         }
+    }
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int e = i * 64 * NW + tid, row = e / PPR4, c = e % PPR4;
+        if (e >= n_rows * PPR4) break;
+        float M = -INFINITY, L = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) M = fmaxf(M, st[i][w].x);
         const float ref = M == -INFINITY ? 0.f : M;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float4 v = *(const float4*)((const float*)(lds + w * C::AREA) + (row * PPR4 + (c ^ (row & (PPR4 - 1)))) * 4);
-            const float f = part_weight(st[w], ref);
-            L = add_part(f, st[w].y, L);
-            a[0] = add_part(f, v.x, a[0]); a[1] = add_part(f, v.y, a[1]); a[2] = add_part(f, v.z, a[2]); a[3] = add_part(f, v.w, a[3]);
+            const float f = part_weight(st[i][w], ref);
+            L = add_part(f, st[i][w].y, L);
+            a[0] = add_part(f, v[i][w].x, a[0]); a[1] = add_part(f, v[i][w].y, a[1]);
+            a[2] = add_part(f, v[i][w].z, a[2]); a[3] = add_part(f, v[i][w].w, a[3]);
         }
-        if (c == 0) part.ml[part_row0 + row] = make_float2(M, L);
         if (n_split > 1) {
+            if (c == 0) part.ml[part_row0 + row] = make_float2(M, L);
             *(float4*)(part.o + (part_row0 + row) * D + c * 4) = make_float4(a[0], a[1], a[2], a[3]);
         } else {
             const size_t out = ((size_t)b * s.T + row / group) * s.n_q + g * group + row % group;
-            __attribute__((aligned(8))) uint16_t v[4];
+            __attribute__((aligned(8))) uint16_t z[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = f32_to_bf16(L == 0.f ? 0.f : a[j] / L);
-            *(uint2*)(O + out * D + c * 4) = *(const uint2*)v;
-            if (LSE && c == 0) LSE[out] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
+            for (int j = 0; j < 4; ++j) z[j] = f32_to_bf16(L == 0.f ? 0.f : a[j] / L);
+            *(uint2*)(O + out * D + c * 4) = *(const uint2*)z;
+            if (c == 0) {
+                const float y = M + __builtin_amdgcn_logf(L);
+                if (LSE) LSE[out] = L == 0.f ? -INFINITY : y * kLn2;
+                lse_lds[row] = L == 0.f ? INFINITY : y;       // (weighs nothing)
+            }
         }
+    }
+    if (n_split > 1 || !logits) return;
+    // One workgroup had all keys: the weights too, from its waves' logits (complete and in the L2 since their wait for all that was under way).
+    __syncthreads();
+    auto weigh = [&](int key, auto most) __attribute__((always_inline)) {          // (all logits requested together)
+        const float* y = logits + (size_t)unit * n_rows * stride + key;
+        float x[most], w = 0.f;
+#pragma unroll
+        for (int row = 0; row < most; ++row) x[row] = y[(size_t)min(row, n_rows - 1) * stride];
+#pragma unroll
+        for (int row = 0; row < most; ++row)
+            w += __builtin_amdgcn_exp2f(x[row] == -INFINITY || row >= n_rows ? -INFINITY : x[row] - lse_lds[min(row, n_rows - 1)]);
+        weight_out[set + key] = (weight ? weight[set + key] : 0.f) + w;
+    };
+    for (int key = tid; key < len; key += 64 * NW) {
+        if (n_rows <= 8) weigh(key, std::integral_constant<int, 8>{});
+        else weigh(key, std::integral_constant<int, kStepRows>{});
     }
 }
 
@@ -819,10 +878,10 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typen
     const size_t set = (size_t)unit * cap;
     // Everything is requested before anything is waited for: logits and weights of rows up to the capacity, whatever the length.
     const float* y = logits + (size_t)unit * n_rows * stride + min(key, stride - 4);
-    float4 first[8];
+    float4 rows[R];
     float w_in[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) first[i] = *(const float4*)(y + (size_t)min(i, n_rows - 1) * stride);
+    for (int i = 0; i < R; ++i) rows[i] = *(const float4*)(y + (size_t)min(i, n_rows - 1) * stride);
 #pragma unroll
     for (int j = 0; j < 4; ++j) w_in[j] = weight ? weight[set + min(key + j, cap - 1)] : 0.f;
     // LSE of the query rows: every (256 / R)-th split by each of R threads, four requested together, joined over the lanes and waves.
@@ -859,11 +918,7 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typen
         for (int j = 0; j < 4; ++j) w[j] += __builtin_amdgcn_exp2f(x[j] == -INFINITY ? -INFINITY : x[j] - lse);
     };
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < n_rows) add(first[i], lse_lds[i]);
-    if constexpr (R > 8)
-#pragma unroll 4
-        for (int i = 8; i < n_rows; ++i) add(*(const float4*)(y + (size_t)i * stride), lse_lds[i]);
+    for (int i = 0; i < R; ++i) add(rows[i], lse_lds[i]);     // (behind the last row: it again, weighing nothing)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (key + j < len) weight_out[set + key + j] = w_in[j] + w[j];
@@ -1435,8 +1490,12 @@ MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
         const long long base = units * ((rows + kF32Block - 1) / kF32Block);
         p.n_split = (int)std::max<long long>(1, std::min<long long>(most, g_force_split ? (long long)g_force_split : 512 / base));
     } else if (p.few) {
+        // A workgroup on every compute unit, each wave of one with a tile at least.  Short sets by one workgroup each, which needs no second
+        // launch (us, one workgroup and splits, 28 heads on 4, one token: 256 rows 9.0, 10.3, 384 rows 10.7, 10.3; four tokens 12.1, 13.9 and
+        // 14.5, 14.1; D = 64, 14 on 2, 384 rows 8.9, 9.0 and 11.5, 12.1, 512 rows 9.7, 9.2 and 12.4, 12.1).
         const long long tiles = (l_cap + kStepTile - 1) / kStepTile, most = (tiles + kStepWaves - 1) / kStepWaves;
         p.n_split = (int)std::max<long long>(1, std::min<long long>(most, g_force_split ? (long long)g_force_split : 256 / units));
+        if (!g_force_split && tiles <= (d->head_dim == 64 ? 12 : 8)) p.n_split = 1;
     } else if (d->dtype == VXL_BF16) {
         ring_plan(p, units, rows, d->head_dim, l_cap);
         // Parts of the query rows, by estimates in us: rounds of two workgroups on a compute unit, but no less than the workgroup whose keys
@@ -1519,6 +1578,7 @@ static vxl_status launch_finish(const MixedPlan& p, const MixedCall& c, const Pa
                            c.weight_out, c.T, d->n_q_heads, d->n_kv_heads, c.l_cap, p.stride, p.n_split, (int)n_merge, (int)n_blocks, all);
     };
     if (rows <= 8) finish(std::integral_constant<int, 8>{});
+    else if (rows <= 16) finish(std::integral_constant<int, 16>{});
     else finish(std::integral_constant<int, 32>{});
     return mixed_launched();
 }
@@ -1538,9 +1598,9 @@ static vxl_status launch_step(const MixedPlan& p, const MixedCall& c, const Sets
         });
         if (st != VXL_OK) return st;
         hipLaunchKernelGGL((attend_step_kernel<dim, pos, once>), dim3(p.n_split, units), dim3(64 * kStepWaves), C::LDS_BYTES, s, sets, rule, part,
-                           (uint16_t*)c.O, c.LSE, logits, p.stride, p.n_split);
+                           (uint16_t*)c.O, c.LSE, logits, p.stride, p.n_split, c.weight, c.weight_out);
         st = mixed_launched();
-        return st != VXL_OK ? st : launch_finish<false, dim>(p, c, part, logits, s);
+        return st != VXL_OK || p.n_split == 1 ? st : launch_finish<false, dim>(p, c, part, logits, s);
     };
     const bool big = (size_t)units * c.l_cap * d->head_dim * 2 * 2 > kPastCachesBytes;
     auto by_size = [&](auto dim, auto pos) { return big ? run(dim, pos, std::true_type{}) : run(dim, pos, std::false_type{}); };

@@ -12,6 +12,9 @@ namespace {
 // whose elements are pairs among themselves) or copied.  A thread has one item of a token for its heads hg, hg + HG, ..., so
 // the sines and cosines of its pairs are made once (in registers, from an angle in 64 bits) and used for all of them.
 // HBM bound where there is much to do: see launch_rotate.
+// Threads that a launch of few tokens has at least, the heads of a token shared by several of them.  Us in a replayed graph with 2^15, 2^16, 2^17:
+// 512 new tokens 7.1, 5.7, 5.7; 1,000 tokens of a prompt 6.6, 6.4, 7.3, 4,000 19.5, 15.7, 15.9.
+constexpr long long kThreadsWanted = 1 << 16;
 struct Where {                 // element strides between heads and tokens of source and destination
     long long head, tok;
 };
@@ -86,8 +89,6 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
     const bool turned = item < rot;
     const int c0 = !turned ? 2 * item : HALF ? item : 2 * item, c1 = !turned || !HALF ? c0 + 1 : item + rot;
     const int p = a.positions[tok];
-    Turn<T, VEC> turn;
-    if (turned) turn.make(a.freqs, item * VEC, a.magnitude, a.sign, p);
     const int n_heads = a.n_q + (APPEND ? 2 : 1) * a.n_kv;
     int row = 0, b = 0;
     if constexpr (APPEND) {
@@ -95,37 +96,35 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
         const long long r = (long long)a.mix_len[b] - a.n_new + tok % a.n_new;
         row = r >= 0 && r < a.l_cap ? (int)r : -1;
     }
-    for (int h0 = hg; h0 < n_heads; h0 += U * a.head_groups) {
-        V x[U][2];
-        const T* src[U];
-        T* dst[U];
+    auto is_value = [&](int h) { return APPEND && h >= a.n_q + a.n_kv; };
+    auto head_in = [&](int h) { return h < a.n_q ? 0 : (h - a.n_q) % a.n_kv; };
+    auto load = [&](int h0, V (&x)[U][2]) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int h = h0 + u * a.head_groups;
-            src[u] = nullptr;
             if (h >= n_heads) continue;
-            if (h < a.n_q) {
-                src[u] = (const T*)a.q + h * a.qs.head + tok * a.qs.tok;
-                dst[u] = (T*)a.q_out + h * a.qo.head + tok * a.qo.tok;
-            } else {
-                const int g = (h - a.n_q) % a.n_kv;
-                const bool value = APPEND && h >= a.n_q + a.n_kv;
-                const long long from = g * a.ks.head + tok * a.ks.tok;
-                src[u] = (const T*)(value ? a.v : a.k) + from;
-                if constexpr (APPEND) {
-                    dst[u] = row < 0 ? nullptr : (T*)(value ? a.v_out : a.k_out) + (((long long)b * a.n_kv + g) * a.l_cap + row) * D;
-                } else {
-                    dst[u] = (T*)a.k_out + from;
-                }
-            }
-            x[u][0] = *(const V*)(src[u] + c0 * VEC);
-            x[u][1] = *(const V*)(src[u] + c1 * VEC);
+            const T* src = h < a.n_q ? (const T*)a.q + h * a.qs.head + tok * a.qs.tok
+                                     : (const T*)(is_value(h) ? a.v : a.k) + head_in(h) * a.ks.head + tok * a.ks.tok;
+            x[u][0] = *(const V*)(src + c0 * VEC);
+            x[u][1] = *(const V*)(src + c1 * VEC);
         }
+    };
+    V x[U][2] = {};
+    load(hg, x);                                              // (on their way while the angles are made)
+    Turn<T, VEC> turn;
+    if (turned) turn.make(a.freqs, item * VEC, a.magnitude, a.sign, p);
+    for (int h0 = hg; h0 < n_heads; h0 += U * a.head_groups) {
+        if (h0 != hg) load(h0, x);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (!src[u] || !dst[u]) continue;
             const int h = h0 + u * a.head_groups;
-            if (turned && h < a.n_q + a.n_kv) {
+            if (h >= n_heads) continue;
+            T* dst;
+            if (h < a.n_q) dst = (T*)a.q_out + h * a.qo.head + tok * a.qo.tok;
+            else if constexpr (APPEND) dst = (T*)(is_value(h) ? a.v_out : a.k_out) + (((long long)b * a.n_kv + head_in(h)) * a.l_cap + row) * D;
+            else dst = (T*)a.k_out + head_in(h) * a.ks.head + tok * a.ks.tok;
+            if (APPEND && h >= a.n_q && row < 0) continue;
+            if (turned && !is_value(h)) {
                 T lo[VEC], hi[VEC];
                 __builtin_memcpy(lo, &x[u][0], sizeof(V));
                 __builtin_memcpy(hi, &x[u][1], sizeof(V));
@@ -133,10 +132,10 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
                 __builtin_memcpy(&x[u][0], lo, sizeof(V));
                 __builtin_memcpy(&x[u][1], hi, sizeof(V));
             }
-            *(V*)(dst[u] + c0 * VEC) = x[u][0];
-            *(V*)(dst[u] + c1 * VEC) = x[u][1];
-            if (APPEND && item == 0 && h >= a.n_q && h < a.n_q + a.n_kv) {
-                const long long at = ((long long)b * a.n_kv + h - a.n_q) * a.l_cap + row;
+            *(V*)(dst + c0 * VEC) = x[u][0];
+            *(V*)(dst + c1 * VEC) = x[u][1];
+            if (APPEND && item == 0 && h >= a.n_q && !is_value(h)) {
+                const long long at = ((long long)b * a.n_kv + head_in(h)) * a.l_cap + row;
                 if (a.row_pos) a.row_pos[at] = p;
                 if (a.row_weight) a.row_weight[at] = 0.f;
             }
@@ -159,7 +158,7 @@ vxl_status launch(const vxl_attn_desc* d, const vxl_rotary* r, RotateArgs a, hip
             const int n_heads = a.n_q + (APPEND ? 2 : 1) * a.n_kv;
             // few tokens: the heads of one are shared by several threads
             a.head_groups = 1;
-            while (a.head_groups < n_heads && (long long)a.n_tokens * a.head_groups * (dim / (2 * vec)) < 1 << 17) a.head_groups *= 2;
+            while (a.head_groups < n_heads && (long long)a.n_tokens * a.head_groups * (dim / (2 * vec)) < kThreadsWanted) a.head_groups *= 2;
             const long long slots = (long long)a.n_tokens * a.head_groups;
             hipLaunchKernelGGL((rotate_kernel<T, dim, vec, half, APPEND>), folded_grid((slots + PER - 1) / PER), dim3(256), 0, s, a);
             return mixed_launched();
