@@ -251,12 +251,12 @@ __device__ __forceinline__ Part part_of(int i, int first, int n, int len, int pa
 }
 
 // The bin of a pass, from the counts of all parts; counts[p]: of the part's bins 2046 - 2 t and 2047 - 2 t.
-__device__ __forceinline__ void find_from_parts(FindArea& area, const State* st, int pass, int n, Found& f, int2 (&counts)[kParts]) {
+__device__ __forceinline__ void find_from_parts(FindArea& area, const State* st, int pass, int n_parts, int n, Found& f, int2 (&counts)[kParts]) {
     if (pass == 0) f = {0u, n, 0};
     else f = st->found[pass - 1];
     int c0 = 0, c1 = 0;
 #pragma unroll
-    for (int p = 0; p < kParts; ++p) counts[p] = *(const int2*)&st->hist[pass][p][kBins - 2 - 2 * (int)threadIdx.x];
+    for (int p = 0; p < kParts; ++p) counts[p] = p < n_parts ? *(const int2*)&st->hist[pass][p][kBins - 2 - 2 * (int)threadIdx.x] : make_int2(0, 0);
 #pragma unroll
     for (int p = 0; p < kParts; ++p) {
         c1 += counts[p].x;
@@ -297,7 +297,7 @@ __global__ __launch_bounds__(kThreads) void evict_count_kernel(Cut c, State* __r
     if (tid == 0) above = 0;
     if constexpr (PASS > 0) {
         int2 counts[kParts];
-        find_from_parts(area, st, PASS - 1, n, f, counts);
+        find_from_parts(area, st, PASS - 1, gridDim.x, n, f, counts);
         if (part == 0 && tid == 0) st->found[PASS - 1] = f;
         const int top = kBins - 1 - 2 * tid, bin = (int)(f.upper & (bins_of(PASS - 1) - 1));
         int own = 0;
@@ -339,10 +339,10 @@ __global__ __launch_bounds__(kThreads) void evict_places_kernel(Cut c, const Sta
     const int hi = min(lo + per, p.hi);
     Batch rows;
     rows.load(c, set, lo + lane, 64, hi);
-    if (tid < kParts) above[tid] = st->above[0][tid] + st->above[1][tid];
+    if (tid < kParts) above[tid] = tid < (int)gridDim.x ? st->above[0][tid] + st->above[1][tid] : 0;
     Found f;
     int2 counts[kParts];
-    find_from_parts(area, st, 2, n, f, counts);
+    find_from_parts(area, st, 2, gridDim.x, n, f, counts);
     const int top = kBins - 1 - 2 * tid, bin = (int)(f.upper & 1023);
 #pragma unroll
     for (int i = 0; i < kParts; ++i) {                        // (few rows share the 22 bits found before)
@@ -493,7 +493,7 @@ vxl_status launch_mixed_evict(const EvictPlan& p, const EvictCall& e, hipStream_
         } else {
             State* states = (State*)(e.ws + p.states);
             const int part_rows = part_rows_of(e.l_cap);
-            const dim3 grid(kParts, units);
+            const dim3 grid((e.l_cap - 1) / part_rows + 2, units);           // (one more where n cuts a part in two)
             hipLaunchKernelGGL(evict_count_kernel<0>, grid, dim3(kThreads), 0, s, c, states, part_rows);
             hipLaunchKernelGGL(evict_count_kernel<1>, grid, dim3(kThreads), 0, s, c, states, part_rows);
             hipLaunchKernelGGL(evict_count_kernel<2>, grid, dim3(kThreads), 0, s, c, states, part_rows);
