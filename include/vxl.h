@@ -546,7 +546,8 @@ vxl_status vxl_mixed_attend(const vxl_attn_desc* desc, const vxl_score_rule* rul
 /*
  * Cuts every mixed set of a batch back to its n = min(mix_len[b], keep) rows of the largest weight.  Every KV head keeps rows of
  * its own, in this order of preference:
- *   rows of a position below n_first (a prompt's first tokens) or with newest[b] - position < n_recent (the latest), all alike;
+ *   rows of a position below n_first (a prompt's first tokens) or, n_recent > 0, with newest[b] - position < n_recent (the latest),
+ *   all alike;
  *   then by weight, the largest first (+inf before all numbers, -0 as 0, NaN behind -inf);  then empty rows (a negative position)
  * and of equal rows the lower one.  Kept rows below n stay in their place; those above take the places of the dropped ones below, in
  * order.  (The order of rows has no meaning: their positions go with them.)

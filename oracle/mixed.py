@@ -81,7 +81,7 @@ def evict_rows(length, weight, row_pos, newest, keep, n_first=0, n_recent=0):
         p, w = int(row_pos[r]), float(weight[r])
         if p < 0:
             return (3, 0.0, r)
-        if p < n_first or int(newest) - p < n_recent:
+        if p < n_first or (n_recent and int(newest) - p < n_recent):
             return (0, 0.0, r)
         return (2, 0.0, r) if math.isnan(w) else (1, -w, r)
     kept = sorted(sorted(range(length), key=rank)[:n])

@@ -11,7 +11,7 @@ namespace {
 // Order of preference as a number, larger first: 0 an empty row, 1 NaN, then the weights in their order, all ones a protected row.
 __device__ __forceinline__ uint32_t preference(float w, int pos, int n_first, int newest, int n_recent) {
     if (pos < 0) return 0u;
-    if (pos < n_first || (long long)newest - pos < n_recent) return ~0u;
+    if (pos < n_first || (n_recent && (long long)newest - pos < n_recent)) return ~0u;
     if (w != w) return 1u;
     const uint32_t x = __float_as_uint(w == 0.f ? 0.f : w);
     return (x >> 31) ? ~x : x | 0x80000000u;                  // (-inf: 0x007fffff, +inf: 0xff800000)

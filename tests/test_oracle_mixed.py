@@ -67,3 +67,10 @@ def test_eviction_by_hand():
     assert oracle.evict_rows(9, w, pos, 18, 3, n_first=12, n_recent=3).tolist() == [0, 1, 6]
     assert oracle.evict_rows(9, w, pos, 18, 6).tolist() == [0, 8, 2, 3, 4, 5]
     assert oracle.evict_rows(3, w, pos, 18, 9).tolist() == [0, 1, 2] and len(oracle.evict_rows(-4, w, pos, 18, 9)) == 0
+
+
+def test_without_latest_rows_none_is_held_for_its_position():
+    """n_recent = 0: neither without a newest position nor with one that rows lie behind."""
+    w, pos = np.array([3.0, 1.0, 2.0, 5.0], np.float32), np.array([9, 11, 4, 6])
+    for newest in (0, 5, 11):
+        assert oracle.evict_rows(4, w, pos, newest, 2, n_first=0, n_recent=0).tolist() == [0, 3]
