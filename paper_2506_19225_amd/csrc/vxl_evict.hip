@@ -240,6 +240,7 @@ struct State {                 // of a set between the launches, in the workspac
     int above[2][kParts];      // rows above the bin found, by pass and part
     Found found[2];
 };
+static_assert(sizeof(State) % 8 == 0, "pairs of bins are read together");
 struct Part {
     int lo, hi;
 };
@@ -484,7 +485,8 @@ vxl_status launch_mixed_evict(const EvictPlan& p, const EvictCall& e, hipStream_
             };
             auto by_rows = [&](auto in_one) {
                 if (e.l_cap <= 1 * kThreads) return run(std::integral_constant<int, 1>{}, in_one);
-                if (e.l_cap <= 3 * kThreads) return run(std::integral_constant<int, 3>{}, in_one);
+                if (e.l_cap <= 2 * kThreads) return run(std::integral_constant<int, 2>{}, in_one);
+                if (e.l_cap <= 4 * kThreads) return run(std::integral_constant<int, 4>{}, in_one);
                 if (e.l_cap <= 8 * kThreads) return run(std::integral_constant<int, 8>{}, in_one);
                 return run(std::integral_constant<int, 16>{}, in_one);
             };
