@@ -133,9 +133,11 @@ vxl_status vxl_layout_destroy(vxl_layout* layout);
 
 /* Bytes of workspace the given hot call needs (0 on invalid arguments, and for VXL_OP_GATHER,
  * which needs none).  batch, n_q_tokens and l_cap are read by the ops that take them (SCORE_TOPK:
- * batch; SCORE_MASS: batch, n_q_tokens; the DECODEs and MIXED_ATTEND: batch, n_q_tokens, l_cap; MIXED_EVICT: batch, l_cap).  The
- * decode call is sized by the capacity of the mixed buffers it will be given, l_cap, and not by the number k of dense chunks, because it takes no layout: l_cap = vxl_mixed_kv_capacity(layout, k) for the
- * caller's k, or anything larger.  layout may be NULL for VXL_OP_DECODE and is not read for the VXL_OP_MIXED ones. */
+ * batch; SCORE_MASS: batch, n_q_tokens; the DECODEs and MIXED_ATTEND: batch, n_q_tokens, l_cap;
+ * MIXED_EVICT: batch, l_cap).  The decode call is sized by the capacity of the mixed buffers it will
+ * be given, l_cap, and not by the number k of dense chunks, because it takes no layout:
+ * l_cap = vxl_mixed_kv_capacity(layout, k) for the caller's k, or anything larger.  layout may be NULL
+ * for VXL_OP_DECODE and is not read for the VXL_OP_MIXED ones. */
 size_t vxl_workspace_bytes(vxl_op op, const vxl_layout* layout, const vxl_attn_desc* desc,
                            int32_t batch, int32_t n_q_tokens, int32_t l_cap);
 

@@ -19,7 +19,8 @@ extern "C" {
 
 /* on != 0: BF16 calls of vxl_chunk_prefill, vxl_bilevel_decode and vxl_chunk_score_topk_mass run
  * the plain fp32 vector-ALU kernels instead of the matrix-core kernels (the workspace may then be
- * NULL).  An on-device cross-check of the matrix-core path. */
+ * NULL).  An on-device cross-check of the matrix-core path.  vxl_mixed_attend calls of both types run
+ * their row-by-row kernels, in the same workspace. */
 void vxl_debug_force_simple(int on);
 
 /* Pre-filling instance: 0 = the library chooses (8 waves, 256-row bands, one workgroup per compute

@@ -16,6 +16,7 @@ namespace {
 struct Rule {
     float c2;                  // scale log2(e)
     float cap_in, cap2;        // scale / softcap, softcap log2(e); cap2 == 0: no cap
+    float cap_few, cap_k[3];   // below which products the short series holds, and its coefficients (cap_logits)
     int causal, window, n_always;
     const float* slopes;
     const int32_t *q_pos, *row_pos;
@@ -54,7 +55,7 @@ struct Sets {
 
 // ------------------------------------------------------------------------------------------
 // Row by row: one wave, a key per lane for the logits and a column per lane for O, in fp32, over the rows that the token sees and no
-// others.  The cross-check of the matrix-core kernels.
+// others.  The cross-check of the matrix-core kernels, and what makes a row again that they cannot (exact_row).
 // ------------------------------------------------------------------------------------------
 template <typename T, int D>
 __device__ __forceinline__ float dot_row(const float* q, const T* k) {
@@ -177,6 +178,9 @@ __global__ __launch_bounds__(256) void simple_weights_kernel(Sets s, Rule r, con
 //     only then, and for a bias, a lane reads the positions of its elements.
 //   * Sums are of the weights as they are, not as rounded to bf16 for the second product, so that the LSE has fp32's error.
 //   * A value that is not a number reaches rows that do not see it, 0 * inf: a row whose result is none is made again by exact_row.
+// Bound by the matrix instructions, and with a cap by the vector ones.  2,048 tokens of 28 heads on 4 over 18,688 rows, 519 GFLOP
+// of products: 512 us alone, 1.0 PFLOP/s where a library product of 8192^3 reaches 1.24; 64 capped tokens over 23,872 rows: 46 us.  128 and
+// 256 rows a workgroup: see ring_plan.
 // ------------------------------------------------------------------------------------------
 constexpr float kLowest = -std::numeric_limits<float>::max();
 
@@ -241,16 +245,24 @@ __device__ __forceinline__ float tanh_any(float u) {
     asm("" : "+v"(t), "+v"(few));                             // (both there: a selection, not a branch per element)
     return fabsf(u) < 0.4f ? few : t;
 }
-// (one decision for the wave's elements)
+// From products to logits, one decision for the wave's elements.  Where all |u| < 1/8, as with caps of 30 and more, the series to u^7 (the next
+// term is 1.3e-9 of it there) in the product itself: its coefficients have the powers of scale / softcap in them, so that u is not made.
 template <int N>
 __device__ __forceinline__ void cap_logits(float (&x)[N], const Rule& r) {
     float top = 0.f;                                          // (NaN is NaN either way)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        x[i] *= r.cap_in;
-        top = fmaxf(top, fabsf(x[i]));
+    for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(x[i]));
+    if (__builtin_amdgcn_ballot_w64(!(top < r.cap_few)) == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float z = x[i] * x[i], y = x[i] * r.c2;
+            x[i] = fmaf(y * z, fmaf(fmaf(r.cap_k[2], z, r.cap_k[1]), z, r.cap_k[0]), y);
+        }
+        return;
     }
-    if (__builtin_amdgcn_ballot_w64(!(top < 0.4f)) == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] *= r.cap_in;
+    if (__builtin_amdgcn_ballot_w64(!(top * r.cap_in < 0.4f)) == 0) {
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = r.cap2 * tanh_small(x[i]);
     } else {
@@ -505,6 +517,8 @@ __device__ __forceinline__ float add_part(float f, float x, float sum) { return 
 // the other waves of all splits, from two pairs of LDS areas filled by direct loads and counted by hand; the waves' (reference, sum,
 // O) are merged through LDS.  The logits, in units of log 2, are kept in the workspace (4 bytes per query row and key beside 4 D of key and
 // value), so that the weights need no second pass over the keys: -inf where the row is not seen, kLowest for a seen one of -inf.
+// One token of eight queries, 28 heads on 4 of D = 128, 18,177 rows: 50 us for 298 MB of keys, values and numbers of rows, 5.9 TB/s (a 2 GiB copy
+// 4.9); of one query and 4,097 rows 7.0, launch and three dependent trips to memory.
 // ------------------------------------------------------------------------------------------
 constexpr int kStepTile = 32, kStepWaves = 4, kStepRows = 32;
 
@@ -516,9 +530,9 @@ struct StepCfg {
 };
 
 template <int D, bool POS, bool ONCE>
-__global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s, Rule r, Partials part, uint16_t* __restrict__ O, float* __restrict__ LSE,
-                                                                         float* logits, int stride, int n_split, const float* weight,
-                                                                         float* weight_out) {
+__global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s, Rule r, Partials part, uint16_t* __restrict__ O,
+                                                                         float* __restrict__ LSE, float* logits, int stride, int n_split,
+                                                                         const float* weight, float* weight_out) {
     using C = StepCfg<D>;
     constexpr int NW = kStepWaves, TK = kStepTile, PPR = C::PPR, NL = C::NL;
     extern __shared__ __attribute__((aligned(16))) uint16_t lds[];
@@ -858,7 +872,8 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(Partials part, typena
 
 // What follows on the kernels that keep their logits: the first n_merge workgroups merge the splits of a query row, the others add up the
 // weights of 1,024 rows of a set, each with the LSE of its (at most R) query rows made from the splits' sums again.  One launch instead of
-// two, and neither part waits for the other.
+// two, and neither part waits for the other.  4.5 us behind a token over 4,097 rows (a launch and two trips to memory), 7.2 behind eight over
+// 18,177.  R = 8, 16, 32 for the registers that the logits wait in.
 template <bool F32, int D, int R>
 __global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typename Storage<F32>::T* __restrict__ O, float* __restrict__ LSE,
                                                             const float* __restrict__ logits, const int32_t* __restrict__ mix_len,
@@ -927,8 +942,11 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typen
 // ------------------------------------------------------------------------------------------
 // The weights of the rows where there are many query rows: the logits once more, against the LSE.  A wave keeps 64 keys in registers as
 // the operand of the first product and goes over query rows, 64 at a time from a ring of four LDS stages, which direct loads fill three tiles
-// ahead for the four waves of a workgroup (counted by hand); a lane's sums are of its elements of the tiles, folded over the lanes at the end.  Query rows are cut into n_part parts where keys alone do not
-// fill the chip, whose sums a last kernel adds in order.
+// ahead for the four waves of a workgroup (counted by hand); a lane's sums are of its elements of the tiles, folded over the lanes at the
+// end.  Query rows are cut into n_part parts where keys alone do not fill the chip, whose sums a last kernel adds in order.
+// Bound by the vector instructions, an exponential and a sum per element beside one product where the ring has two.  14,336 query rows and 18,688 rows of 4 KV
+// heads: 314 us, 0.83 PFLOP/s; 448 capped ones and 23,872: 33 to 44.  Each wave fed from memory by itself, without the ring: 39 where it takes
+// 30.  Logits kept for this instead of made again would be 4 bytes an element both ways: 171 MB, 70 us, for the 448.
 // ------------------------------------------------------------------------------------------
 // Lanes whose bit N is set keep the upper half of their elements and take their partner's, the others the lower half.
 template <int N>
@@ -1175,7 +1193,8 @@ __global__ __launch_bounds__(256) void weights_sum_kernel(const float* __restric
 // operands come from memory in the order that both products use, as in the plain fp32 decode:
 //   S^T = K Q^T    lane (i = lane % 16, j = lane / 16): K[key i][16 x + 4 j + e] and Q[row i] of the same; result register r: key 4 j + r, row i
 //   O^T = V^T P^T  step r takes the keys 4 j + r, V[key 4 j + r][64 b + 4 i + e]; result register r' of (b, e): O[row i][64 b + 16 j + 4 r' + e]
-// Bound by that instruction (a 1/16 of the bf16 one's rate) where there is enough to do.
+// Bound by that instruction (a 1/16 of the bf16 one's rate) where there is enough to do; three sets of 705 rows with 5 tokens of 4 heads on 2, D = 64,
+// take 6.5 us, of which launch and dependent loads are the most (row by row: 143).
 // ------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 constexpr int kF32Block = 16, kF32Tile = 32, kF32Waves = 4;
@@ -1451,7 +1470,8 @@ extern "C" void vxl_debug_mixed_force(int waves, int n_split, int n_part) {
     g_force_part = std::max(0, n_part);
 }
 
-// Many query rows (ring): estimates in us of a launch of workgroups of 256 and of 128 rows and so many splits.
+// Many query rows (ring): estimates in us of a launch of workgroups of 256 and of 128 rows and so many splits: rounds over 256 compute units, 8 us
+// for one's start and end, 1.75 and 1.13 per tile (0.75 of it for D = 64), 5 and 0.4 per MB for the merge.
 static void ring_plan(MixedPlan& p, long long units, long long rows, int D, int l_cap) {
     const long long tiles = (l_cap + kKeyTile - 1) / kKeyTile;
     const int force_waves = g_force_waves, force_split = g_force_split;
@@ -1583,6 +1603,8 @@ static vxl_status launch_finish(const MixedPlan& p, const MixedCall& c, const Pa
     return mixed_launched();
 }
 
+// Keys and values of more bytes than the L2s have between them are read past the caches: 298 MB 66 -> 60 us; 8 MB, which the next call finds in
+// them, are not.
 constexpr size_t kPastCachesBytes = 32u << 20;
 static vxl_status launch_step(const MixedPlan& p, const MixedCall& c, const Sets& sets, const Rule& rule, hipStream_t s) {
     const vxl_attn_desc* d = c.d;
@@ -1644,8 +1666,6 @@ static vxl_status launch_weights(const MixedPlan& p, const MixedCall& c, const S
     return mixed_launched();
 }
 
-static vxl_status launch_merge(const MixedPlan& p, const MixedCall& c, hipStream_t s);
-
 static vxl_status launch_f32(const MixedPlan& p, const MixedCall& c, const Sets& sets, const Rule& rule, hipStream_t s) {
     const vxl_attn_desc* d = c.d;
     const int units = c.batch * d->n_kv_heads, rows = d->n_q_heads / d->n_kv_heads * c.T, n_rtile = (rows + kF32Block - 1) / kF32Block;
@@ -1685,8 +1705,10 @@ vxl_status launch_mixed_attend(const MixedPlan& p, const MixedCall& c, bool forc
     const vxl_attn_desc* d = c.d;
     const vxl_score_rule none{};
     const vxl_score_rule& u = c.rule ? *c.rule : none;
-    const Rule rule{c.scale * kLog2e, u.softcap > 0.f ? c.scale / u.softcap : 0.f, u.softcap * kLog2e, u.causal, u.window, u.n_always, u.slopes,
-                    c.q_pos, c.row_pos};
+    const float in = u.softcap > 0.f ? c.scale / u.softcap : 0.f, in2 = in * in;
+    const bool few = in > 0x1p-16f && in < 0x1p16f;           // (squares and coefficients are numbers)
+    const Rule rule{c.scale * kLog2e, in, u.softcap * kLog2e, few ? 0.125f / in : 0.f, {in2 * (-1.f / 3), in2 * in2 * (2.f / 15), in2 * in2 * in2 * (-17.f / 315)},
+                    u.causal, u.window, u.n_always, u.slopes, c.q_pos, c.row_pos};
     const Sets sets{c.Qd, c.Kmix, c.Vmix, c.mix_len, c.T, d->n_q_heads, d->n_kv_heads, c.l_cap};
     if (force_simple) return launch_simple(p, c, sets, rule, s);
     if (d->dtype == VXL_F32) return launch_f32(p, c, sets, rule, s);

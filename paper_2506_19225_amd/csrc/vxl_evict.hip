@@ -108,6 +108,9 @@ __device__ __forceinline__ void move_row(const Cut& c, const Move& m, size_t fro
 // side), a workgroup a whole set.  Bound by latency: launch, one trip to memory, and the barriers of two or three passes (the last one is left
 // out when all of the bin's rows are kept, which is so where weights differ).  Out of place every workgroup of a set selects for itself and
 // moves its share, which saves the second launch; in place the rows' places are written down for the kernel behind.
+// 4 KV heads, 2,304 rows to 2,048: 8.8 us; 16 sets of 7,001 fp32 rows to 1,777: 12.8.  Two groups of workgroups a compute unit could hold (512 / units):
+// 23.8.  Counting a wave's most frequent bin by one lane: 28.  PER = 32 (20,000 rows): 33.8 and 48.7 us for a quarter and nearly all kept, the
+// launches below 34.2 and 43.1.
 // ------------------------------------------------------------------------------------------
 template <int PER, int ROW16, bool MOVES>
 __global__ __launch_bounds__(kThreads) void evict_set_kernel(Cut c, Move m, int32_t* __restrict__ places, int32_t* __restrict__ n_out) {
@@ -233,6 +236,7 @@ __global__ __launch_bounds__(kThreads) void evict_set_kernel(Cut c, Move m, int3
 // Longer sets: each in parts of `part_rows` rows below n and of as many from n on (so that a part has holes or movers, never both), at most kParts
 // of them, a workgroup each.  Every pass is a launch: the counts of a part's bins are written down, the next launch adds those of all
 // parts, finds the bin and counts on.  The last one knows from the counts how many rows every part before it keeps.
+// 131,328 rows of 4 KV heads to 16,384: 4.6, 8.0 and 7.9 us for the passes, 13.3 for the places, 12.8 for the moves, which copy 64 MB.
 // ------------------------------------------------------------------------------------------
 constexpr int kParts = 20;
 struct State {                 // of a set between the launches, in the workspace
@@ -448,7 +452,8 @@ __global__ __launch_bounds__(256) void evict_move_kernel(Cut c, Move m, const in
     }
 }
 
-// Rows of a set that one workgroup holds in registers, and of a part of a longer one (two more of them than part_rows go into a set).
+// Rows of a set that one workgroup holds in registers, and of a part of a longer one: a set has at most two parts more than part_rows go into it,
+// one for its end and one where n cuts one in two.
 constexpr int kSetRows = 16 * kThreads;
 int part_rows_of(int l_cap) { return std::max(8 * kThreads, (int)(((long long)l_cap + kParts - 3) / (kParts - 2))); }
 
