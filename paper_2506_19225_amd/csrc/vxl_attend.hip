@@ -179,7 +179,7 @@ __global__ __launch_bounds__(256) void simple_weights_kernel(Sets s, Rule r, con
 //   * Sums are of the weights as they are, not as rounded to bf16 for the second product, so that the LSE has fp32's error.
 //   * A value that is not a number reaches rows that do not see it, 0 * inf: a row whose result is none is made again by exact_row.
 // Bound by the matrix instructions, and with a cap by the vector ones.  2,048 tokens of 28 heads on 4 over 18,688 rows, 519 GFLOP
-// of products: 512 us alone, 1.0 PFLOP/s where a library product of 8192^3 reaches 1.24; 64 capped tokens over 23,872 rows: 46 us.  128 and
+// of products: 512 us alone, 1.0 PFLOP/s where a library product of 8192^3 reaches 1.24; 64 tokens over 23,872 rows: 36 us, capped 43.  128 and
 // 256 rows a workgroup: see ring_plan.
 // ------------------------------------------------------------------------------------------
 constexpr float kLowest = -std::numeric_limits<float>::max();
@@ -945,7 +945,7 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typen
 // ahead for the four waves of a workgroup (counted by hand); a lane's sums are of its elements of the tiles, folded over the lanes at the
 // end.  Query rows are cut into n_part parts where keys alone do not fill the chip, whose sums a last kernel adds in order.
 // Bound by the vector instructions, an exponential and a sum per element beside one product where the ring has two.  14,336 query rows and 18,688 rows of 4 KV
-// heads: 314 us, 0.83 PFLOP/s; 448 capped ones and 23,872: 33 to 44.  Each wave fed from memory by itself, without the ring: 39 where it takes
+// heads: 314 us, 0.83 PFLOP/s; 448 and 23,872: 28, capped 36.  Each wave fed from memory by itself, without the ring: 39 where it takes
 // 30.  Logits kept for this instead of made again would be 4 bytes an element both ways: 171 MB, 70 us, for the 448.
 // ------------------------------------------------------------------------------------------
 // Lanes whose bit N is set keep the upper half of their elements and take their partner's, the others the lower half.
@@ -1058,6 +1058,17 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
             for (int kb = 0; kb < 2; ++kb) x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kb][ks], a, x[kb], 0, 0, 0);
         }
     };
+    auto cap = [&](f32x16 (&x)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            float c[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) c[i] = x[kb][i];
+            cap_logits(c, r);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[kb][i] = c[i];
+        }
+    };
     f32x16 acc[2] = {zero16(), zero16()};
     auto plain = [&](const f32x16 (&x)[2], float lse) __attribute__((always_inline)) {
 #pragma unroll
@@ -1115,13 +1126,23 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
                     all &= ~__builtin_amdgcn_ballot_w64((pk_min >= 0) & (within | ((unsigned)pk_max < span.na))) == 0;
                 }
             }
-            if (all && !capped && !biased) {
+            if (all && !biased && !capped) {
                 const float lse[2] = {lse_of(0), lse_of(1)};
                 f32x16 x[2], y[2];                            // (one stretch: a product runs beside the exponentials of the other)
                 product(q, 0, x);
                 product(q, 1, y);
                 plain(x, lse[0]);
                 plain(y, lse[1]);
+                continue;
+            }
+            if (all && !biased) {                             // (in one stretch too it spills, with one branch for both plain logits are 2 % slower)
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+                    f32x16 x[2];
+                    product(q, half, x);
+                    cap(x);
+                    plain(x, lse_of(half));
+                }
                 continue;
             }
 #pragma unroll 1
@@ -1137,17 +1158,7 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
                 row.slope2 = biased ? infos[128 + half * 32 + l32] * kLog2e : 0.f;
                 f32x16 x[2];
                 product(q, half, x);
-                if (capped) {
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb) {
-                        float c[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) c[i] = x[kb][i];
-                        cap_logits(c, r);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) x[kb][i] = c[i];
-                    }
-                }
+                if (capped) cap(x);
                 if (biased) by_position(x, [&](float y, int p) { return fmaf(-row.slope2, (float)abs(row.pq - p), y * unit_of); });
                 if (all) {
                     plain(x, row.lse);
