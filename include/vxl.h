@@ -509,7 +509,7 @@ vxl_status vxl_mixed_append(const vxl_attn_desc* desc, const vxl_rotary* rotary,
  *   logit    x = softcap > 0 ? softcap * tanh(s / softcap) : s;  with slopes: minus slopes[h] * |pq - pk|
  *   visible  pq >= 0 and pk >= 0 and (pk < n_always or ((not causal or pk <= pq) and (window == 0 or pq - pk < window)))
  * A negative position marks a padding token or an empty row.
- *   softcap  >= 0, finite;  window, n_always >= 0;  slopes device float [n_q_heads], or NULL
+ *   softcap  0, or up to 2^100 with softmax_scale / softcap in [2^-60, 2^60];  window, n_always >= 0;  slopes device float [n_q_heads], or NULL
  * A NULL rule: s as it is, no causal or window rule.
  */
 typedef struct {
@@ -533,7 +533,8 @@ typedef struct {
  *   mix_len         as vxl_bilevel_decode
  *   workspace       sized by vxl_workspace_bytes(VXL_OP_MIXED_ATTEND, NULL, desc, batch, n_q_tokens, l_cap), never less
  * Other arguments as vxl_bilevel_decode.  Results are those of the formulas within the tolerance of the path (VXL_BF16: every weight of O
- * is rounded to bf16, 2^-8 of it at most, LSE and weight_out have fp32's errors); the same call gives the same bits.  A token
+ * is rounded to bf16, 2^-8 of it at most, LSE and weight_out have fp32's errors, a capped logit is off by 2^-22 softcap at most besides those of
+ * its product); the same call gives the same bits.  A token
  * with a visible logit of NaN or +inf has no softmax: its O and LSE are NaN, and so is the weight of the rows that it sees.  What a token
  * does not see never matters to it, whatever its rows hold.
  * Errors: VXL_ERR_INVALID_ARG (also one of q_pos and row_pos without the other, a rule that needs positions without them, outputs

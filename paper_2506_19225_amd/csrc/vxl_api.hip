@@ -916,7 +916,10 @@ vxl_status vxl_mixed_attend(const vxl_attn_desc* d, const vxl_score_rule* rule, 
     if (rule) {
         if (!(rule->softcap >= 0.f) || !std::isfinite(rule->softcap) || rule->window < 0 || rule->n_always < 0 || !aligned4(rule->slopes))
             return VXL_ERR_INVALID_ARG;
-        if (rule->softcap > 0.f && !std::isfinite(scale / rule->softcap)) return VXL_ERR_INVALID_ARG;
+        if (rule->softcap > 0.f) {                            // (what the kernels make of it are numbers)
+            const float in = scale / rule->softcap;
+            if (!(in >= 0x1p-60f && in <= 0x1p60f && rule->softcap <= 0x1p100f)) return VXL_ERR_INVALID_ARG;
+        }
         if ((rule->causal || rule->window || rule->slopes) && !q_pos) return VXL_ERR_INVALID_ARG;
     }
     if (!mixed_sizes_ok(d, batch, n_q_tokens, l_cap)) return VXL_ERR_UNSUPPORTED;

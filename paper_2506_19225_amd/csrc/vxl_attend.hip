@@ -16,7 +16,8 @@ namespace {
 struct Rule {
     float c2;                  // scale log2(e)
     float cap_in, cap2;        // scale / softcap, softcap log2(e); cap2 == 0: no cap
-    float cap_few, cap_k[3];   // below which products the short series holds, and its coefficients (cap_logits)
+    float cap_few, cap_k[3];   // (cap_logits) below which products the series holds, its coefficients,
+    float cap_exp, cap_m2;     // 2 log2(e) scale / softcap, -2 cap2
     int causal, window, n_always;
     const float* slopes;
     const int32_t *q_pos, *row_pos;
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(256) void simple_weights_kernel(Sets s, Rule r, con
 //   * Sums are of the weights as they are, not as rounded to bf16 for the second product, so that the LSE has fp32's error.
 //   * A value that is not a number reaches rows that do not see it, 0 * inf: a row whose result is none is made again by exact_row.
 // Bound by the matrix instructions, and with a cap by the vector ones.  2,048 tokens of 28 heads on 4 over 18,688 rows, 519 GFLOP
-// of products: 512 us alone, 1.0 PFLOP/s where a library product of 8192^3 reaches 1.24; 64 tokens over 23,872 rows: 36 us, capped 43.  128 and
+// of products: 512 us alone, 1.0 PFLOP/s where a library product of 8192^3 reaches 1.24; 64 tokens over 23,872 rows: 36 us, capped 43 (48 by the exponential).  128 and
 // 256 rows a workgroup: see ring_plan.
 // ------------------------------------------------------------------------------------------
 constexpr float kLowest = -std::numeric_limits<float>::max();
@@ -228,25 +229,12 @@ struct Reach {
     }
 };
 
-// softcap tanh(s / softcap) in units of log 2.  tanh u for |u| < 0.4 by its odd series to u^13 (the next term is 1.5e-3 u^14 of it, 4e-9
-// there), which has no cancellation and is cheaper than the exponential and the quotient beyond, where they have little.
-__device__ __forceinline__ float tanh_small(float u) {
-    const float z = u * u;
-    float p = fmaf(z, 3.59212803657e-3f, -8.86323552990e-3f);
-    p = fmaf(p, z, 2.18694885362e-2f);
-    p = fmaf(p, z, -5.39682539683e-2f);
-    p = fmaf(p, z, 1.33333333333e-1f);
-    p = fmaf(p, z, -3.33333333333e-1f);
-    return fmaf(u * z, p, u);
-}
-__device__ __forceinline__ float tanh_any(float u) {
-    asm("" : "+v"(u));                                        // (its series is not hoisted out of both branches below: registers)
-    float t = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(fabsf(u) * (2.f * kLog2e)) + 1.f), u), few = tanh_small(u);
-    asm("" : "+v"(t), "+v"(few));                             // (both there: a selection, not a branch per element)
-    return fabsf(u) < 0.4f ? few : t;
-}
-// From products to logits, one decision for the wave's elements.  Where all |u| < 1/8, as with caps of 30 and more, the series to u^7 (the next
-// term is 1.3e-9 of it there) in the product itself: its coefficients have the powers of scale / softcap in them, so that u is not made.
+// From products s to softcap tanh(u), u = s scale / softcap, in units of log 2; one decision for the wave's elements:
+//   all |u| < 1/8, as with caps of 30 and more: the odd series to u^7 (the next term is 1.3e-9 of it there) in the product itself, its coefficients
+//   with the powers of scale / softcap in them, so that u is not made;
+//   else 1 - 2 / (e^2|u| + 1) with the sign of s, off by 4 roundings of the cap at most: the exponential, the sum and the quotient by one each of
+//   less than the cap, the argument by less than half a one.  The series to u^13 for all |u| < 0.4 is no faster, and both
+//   with a selection, exact to a rounding of the result, took 63 us where this takes 48 (64 tokens over 23,872 rows, a cap of 5).
 template <int N>
 __device__ __forceinline__ void cap_logits(float (&x)[N], const Rule& r) {
     float top = 0.f;                                          // (NaN is NaN either way)
@@ -258,18 +246,12 @@ __device__ __forceinline__ void cap_logits(float (&x)[N], const Rule& r) {
             const float z = x[i] * x[i], y = x[i] * r.c2;
             x[i] = fmaf(y * z, fmaf(fmaf(r.cap_k[2], z, r.cap_k[1]), z, r.cap_k[0]), y);
         }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] *= r.cap_in;
-    if (__builtin_amdgcn_ballot_w64(!(top * r.cap_in < 0.4f)) == 0) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = r.cap2 * tanh_small(x[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            x[i] = r.cap2 * tanh_any(x[i]);
-            if (i % 2) __builtin_amdgcn_sched_barrier(0);     // (two at a time: all at once need more registers than there are)
+            const float q = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(fabsf(x[i] * r.cap_exp)) + 1.f);
+            x[i] = copysignf(fmaf(r.cap_m2, q, r.cap2), x[i]);
+            if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);               // (four at a time: all at once need more registers than there are)
         }
     }
 }
@@ -945,7 +927,7 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typen
 // ahead for the four waves of a workgroup (counted by hand); a lane's sums are of its elements of the tiles, folded over the lanes at the
 // end.  Query rows are cut into n_part parts where keys alone do not fill the chip, whose sums a last kernel adds in order.
 // Bound by the vector instructions, an exponential and a sum per element beside one product where the ring has two.  14,336 query rows and 18,688 rows of 4 KV
-// heads: 314 us, 0.83 PFLOP/s; 448 and 23,872: 28, capped 36.  Each wave fed from memory by itself, without the ring: 39 where it takes
+// heads: 314 us, 0.83 PFLOP/s; 448 and 23,872: 28, capped 37 (43).  Each wave fed from memory by itself, without the ring: 39 where it takes
 // 30.  Logits kept for this instead of made again would be 4 bytes an element both ways: 171 MB, 70 us, for the 448.
 // ------------------------------------------------------------------------------------------
 // Lanes whose bit N is set keep the upper half of their elements and take their partner's, the others the lower half.
@@ -1717,8 +1699,9 @@ vxl_status launch_mixed_attend(const MixedPlan& p, const MixedCall& c, bool forc
     const vxl_score_rule none{};
     const vxl_score_rule& u = c.rule ? *c.rule : none;
     const float in = u.softcap > 0.f ? c.scale / u.softcap : 0.f, in2 = in * in;
-    const bool few = in > 0x1p-16f && in < 0x1p16f;           // (squares and coefficients are numbers)
-    const Rule rule{c.scale * kLog2e, in, u.softcap * kLog2e, few ? 0.125f / in : 0.f, {in2 * (-1.f / 3), in2 * in2 * (2.f / 15), in2 * in2 * in2 * (-17.f / 315)},
+    const float few = in < 0x1p-20f ? 0x1p-6f : in < 0x1p16f ? 0.125f : 0.f;      // (where higher powers are lost they are not needed; coefficients are numbers)
+    const Rule rule{c.scale * kLog2e, in, u.softcap * kLog2e, in > 0.f ? few / in : 0.f, {in2 * (-1.f / 3), in2 * in2 * (2.f / 15), in2 * in2 * in2 * (-17.f / 315)},
+                    2 * kLog2e * in, -2 * kLog2e * u.softcap,
                     u.causal, u.window, u.n_always, u.slopes, c.q_pos, c.row_pos};
     const Sets sets{c.Qd, c.Kmix, c.Vmix, c.mix_len, c.T, d->n_q_heads, d->n_kv_heads, c.l_cap};
     if (force_simple) return launch_simple(p, c, sets, rule, s);

@@ -94,6 +94,18 @@ def test_what_a_window_leaves_out_does_not_matter(t, dtype):
     check_attend(got, qd, k, v, [n], dtype, 0.0, q_pos, pos, weight, **rule)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("t", [1, 40])
+@pytest.mark.parametrize("softcap", [1e-3, 0.25, 2.0, 300.0, 2e7])
+def test_caps(softcap, t, dtype):
+    """From a cap that all logits reach to one that none comes near (a logit of 40 is then off by 40^3 / (3 softcap^2) = 5e-11: the plain ones)."""
+    lens = [300, 45]
+    qd, k, v, q_pos, pos, weight = spread_case(t, 8, 2, 64, 2, t, 310, lens, dtype)
+    k[0, :, 20] = 0.0                                              # (logits of exactly 0)
+    got = attend(qd, k, v, lens, dtype, 0.0, q_pos, pos, weight, softcap=softcap, window=250)
+    check_attend(got, qd, k, v, lens, dtype, 0.0, q_pos, pos, weight, softcap=softcap if softcap < 1e6 else 0.0, window=250)
+
+
 @pytest.mark.parametrize("edge", [1024, 2048, 4096, 8192, 16384])
 @pytest.mark.parametrize("more", [-1, 0, 1])
 def test_eviction_at_the_borders_of_its_variants(edge, more):

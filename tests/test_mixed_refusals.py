@@ -226,3 +226,9 @@ def test_rows_between_rows_do_not_meet():
     assert call(q, k) == vxl.VXL_ERR_HIP
     assert call(q, k + HKV * D * 2) == vxl.VXL_ERR_HIP                        # keys to where the values are: no input of the call
     assert call(q, q + (HQ - 1) * D * 2) == call(k, k) == call(q, k + 16) == call(q + row * 2, k) == vxl.VXL_ERR_INVALID_ARG
+
+
+def test_caps_that_are_refused():
+    """What the kernels make of a cap has to be numbers: beside infinities, caps that are nothing beside the scale, or all."""
+    for softcap in (1e-20, 1e20, 2.0 ** 101):
+        assert refused(attend, rule=vxl.ScoreRule(softcap=softcap)) == vxl.VXL_ERR_INVALID_ARG, softcap
