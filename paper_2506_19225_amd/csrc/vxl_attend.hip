@@ -511,6 +511,28 @@ struct StepCfg {
     static constexpr int PPR = D / 8, RPI = 64 / PPR, NL = kStepTile / RPI;       // pieces of a row; rows, loads of a tile
 };
 
+// The weights of a set of which one workgroup had all keys and query rows, from its waves' logits (complete and in the L2 since their wait for all that
+// was under way); lse: +inf for a row that weighs nothing.
+template <int THREADS>
+__device__ __forceinline__ void weigh_set(const float* logits, int stride, int n_rows, int len, const float* lse, const float* weight,
+                                          float* weight_out) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    auto weigh = [&](int key, auto most) __attribute__((always_inline)) {          // (all logits requested together)
+        float x[most], w = 0.f;
+#pragma unroll
+        for (int row = 0; row < most; ++row) x[row] = logits[(size_t)min(row, n_rows - 1) * stride + key];
+#pragma unroll
+        for (int row = 0; row < most; ++row)
+            w += __builtin_amdgcn_exp2f(x[row] == -INFINITY || row >= n_rows ? -INFINITY : x[row] - lse[min(row, n_rows - 1)]);
+        weight_out[key] = (weight ? weight[key] : 0.f) + w;
+    };
+    for (int key = threadIdx.x; key < len; key += THREADS) {
+        if (n_rows <= 8) weigh(key, std::integral_constant<int, 8>{});
+        else weigh(key, std::integral_constant<int, kStepRows>{});
+    }
+}
+
 template <int D, bool POS, bool ONCE>
 __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s, Rule r, Partials part, uint16_t* __restrict__ O,
                                                                          float* __restrict__ LSE, float* logits, int stride, int n_split,
@@ -759,22 +781,8 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s,
         }
     }
     if (n_split > 1 || !logits) return;
-    // One workgroup had all keys: the weights too, from its waves' logits (complete and in the L2 since their wait for all that was under way).
-    __syncthreads();
-    auto weigh = [&](int key, auto most) __attribute__((always_inline)) {          // (all logits requested together)
-        const float* y = logits + (size_t)unit * n_rows * stride + key;
-        float x[most], w = 0.f;
-#pragma unroll
-        for (int row = 0; row < most; ++row) x[row] = y[(size_t)min(row, n_rows - 1) * stride];
-#pragma unroll
-        for (int row = 0; row < most; ++row)
-            w += __builtin_amdgcn_exp2f(x[row] == -INFINITY || row >= n_rows ? -INFINITY : x[row] - lse_lds[min(row, n_rows - 1)]);
-        weight_out[set + key] = (weight ? weight[set + key] : 0.f) + w;
-    };
-    for (int key = tid; key < len; key += 64 * NW) {
-        if (n_rows <= 8) weigh(key, std::integral_constant<int, 8>{});
-        else weigh(key, std::integral_constant<int, kStepRows>{});
-    }
+    // One workgroup had all keys: the weights too.
+    weigh_set<64 * NW>(logits + (size_t)unit * n_rows * stride, stride, n_rows, len, lse_lds, weight ? weight + set : nullptr, weight_out + set);
 }
 
 // The merge of the splits of one query row by a workgroup: SG groups of D / 4 lanes take every SG-th split, six requested together, and are
@@ -1202,9 +1210,10 @@ __device__ __forceinline__ float f32_logit(const Rule& r, const Span& span, floa
 
 template <int D, bool POS>
 __global__ __launch_bounds__(64 * kF32Waves, 2) void attend_f32_kernel(Sets s, Rule r, Partials part, float* __restrict__ O, float* __restrict__ LSE,
-                                                                       float* __restrict__ lse2, float* __restrict__ logits, int stride, int units,
-                                                                       int n_split, int n_rtile) {
+                                                                       float* __restrict__ lse2, float* logits, int stride, int units,
+                                                                       int n_split, int n_rtile, const float* weight, float* weight_out) {
     constexpr int NW = kF32Waves, X = D / 16;
+    __shared__ float lse_lds[kF32Block];
     __shared__ __attribute__((aligned(16))) float red[NW][kF32Block][D + 4];      // (+ 4: neighbouring rows in other banks)
     __shared__ float2 stats[NW][kF32Block];
     const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, j = lane >> 4;
@@ -1372,9 +1381,12 @@ __global__ __launch_bounds__(64 * kF32Waves, 2) void attend_f32_kernel(Sets s, R
             if (c == 0) {
                 if (LSE) LSE[out] = y * kLn2;
                 lse2[(size_t)unit * n_rows + at] = y;
+                lse_lds[row] = L == 0.f ? INFINITY : y;       // (weighs nothing)
             }
         }
     }
+    if (logits && n_split == 1 && n_rtile == 1)
+        weigh_set<64 * NW>(logits + (size_t)unit * n_rows * stride, stride, n_rows, len, lse_lds, weight ? weight + set : nullptr, weight_out + set);
 }
 
 // The weights of fp32 sets where there are many query rows: a wave has 32 keys and goes over blocks of 16 query rows, four waves of a workgroup
@@ -1498,7 +1510,8 @@ MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     p.stride = (l_cap + kStepTile - 1) / kStepTile * kStepTile;
     p.few = rows <= kStepRows;
     if (d->dtype == VXL_F32) {
-        // as many splits as fill the chip, each wave of one with a tile at least
+        // As many splits as fill the chip, each wave of one with a tile at least: up to 128 rows one workgroup, and of up to 16 query rows one launch (28 heads
+        // on 4, one token, D = 128: 128 rows 9.7 us, with the second launch 12; 192 rows 13.5 by one workgroup, 12.1 by two and the launch).
         const long long tiles = (l_cap + kF32Tile - 1) / kF32Tile, most = (tiles + kF32Waves - 1) / kF32Waves;
         const long long base = units * ((rows + kF32Block - 1) / kF32Block);
         p.n_split = (int)std::max<long long>(1, std::min<long long>(most, g_force_split ? (long long)g_force_split : 512 / base));
@@ -1666,10 +1679,10 @@ static vxl_status launch_f32(const MixedPlan& p, const MixedCall& c, const Sets&
     float *logits = p.few && c.weight_out ? (float*)(c.ws + p.logits) : nullptr, *lse2 = (float*)(c.ws + p.lse2);
     auto run = [&](auto dim, auto pos) {
         hipLaunchKernelGGL((attend_f32_kernel<dim, pos>), placed_grid((long long)units * p.n_split * n_rtile), dim3(64 * kF32Waves), 0, s, sets, rule, part,
-                           (float*)c.O, c.LSE, lse2, logits, p.stride, units, p.n_split, n_rtile);
+                           (float*)c.O, c.LSE, lse2, logits, p.stride, units, p.n_split, n_rtile, c.weight, c.weight_out);
         vxl_status st = mixed_launched();
         if (st != VXL_OK) return st;
-        if (p.few) return launch_finish<true, dim>(p, c, part, logits, s);
+        if (p.few) return p.n_split == 1 && n_rtile == 1 ? st : launch_finish<true, dim>(p, c, part, logits, s);
         if (p.n_split > 1) st = launch_merge(p, c, s);
         if (st != VXL_OK || !c.weight_out) return st;
         hipLaunchKernelGGL((weights_f32_kernel<dim, pos>), dim3((c.l_cap + kF32Tile - 1) / kF32Tile, units), dim3(64 * kF32Waves), 0, s, sets, rule, lse2,
