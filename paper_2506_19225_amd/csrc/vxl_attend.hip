@@ -180,8 +180,8 @@ __global__ __launch_bounds__(256) void simple_weights_kernel(Sets s, Rule r, con
 //   * Sums are of the weights as they are, not as rounded to bf16 for the second product, so that the LSE has fp32's error.
 //   * A value that is not a number reaches rows that do not see it, 0 * inf: a row whose result is none is made again by exact_row.
 // Bound by the matrix instructions, and with a cap by the vector ones.  2,048 tokens of 28 heads on 4 over 18,688 rows, 519 GFLOP
-// of products: 512 us alone, 1.0 PFLOP/s where a library product of 8192^3 reaches 1.24; 64 tokens over 23,872 rows: 36 us, capped 43 (48 by the exponential).  128 and
-// 256 rows a workgroup: see ring_plan.
+// of products: 512 us alone, 1.0 PFLOP/s where a library product of 8192^3 reaches 1.24; 64 tokens over 23,872 rows: 36 us, capped 43
+// (48 by the exponential).  128 and 256 rows a workgroup: see ring_plan.
 // ------------------------------------------------------------------------------------------
 constexpr float kLowest = -std::numeric_limits<float>::max();
 
@@ -934,8 +934,8 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typen
 // the operand of the first product and goes over query rows, 64 at a time from a ring of four LDS stages, which direct loads fill three tiles
 // ahead for the four waves of a workgroup (counted by hand); a lane's sums are of its elements of the tiles, folded over the lanes at the
 // end.  Query rows are cut into n_part parts where keys alone do not fill the chip, whose sums a last kernel adds in order.
-// Bound by the vector instructions, an exponential and a sum per element beside one product where the ring has two.  14,336 query rows and 18,688 rows of 4 KV
-// heads: 314 us, 0.83 PFLOP/s; 448 and 23,872: 28, capped 37 (43).  Each wave fed from memory by itself, without the ring: 39 where it takes
+// Bound by the vector instructions, an exponential and a sum per element beside one product where the ring has two.  14,336 query rows and
+// 18,688 rows of 4 KV heads: 314 us, 0.83 PFLOP/s; 448 and 23,872: 28, capped 37 (43).  Each wave fed from memory by itself, without the ring: 39 where it takes
 // 30.  Logits kept for this instead of made again would be 4 bytes an element both ways: 171 MB, 70 us, for the 448.
 // ------------------------------------------------------------------------------------------
 // Lanes whose bit N is set keep the upper half of their elements and take their partner's, the others the lower half.
