@@ -59,6 +59,8 @@ __device__ __forceinline__ int scan_lanes(int x) {
     return x;
 }
 
+__device__ __forceinline__ int sum_lanes(int x) { return __builtin_amdgcn_readlane(scan_lanes(x), 63); }
+
 // From counts of this pass's bins, of which thread t has c0 in bin 2047 - 2 t and c1 in the one below.
 struct FindArea {
     int wave_sum[kWaves];
@@ -308,8 +310,7 @@ __global__ __launch_bounds__(kThreads) void evict_count_kernel(Cut c, State* __r
         int own = 0;
 #pragma unroll
         for (int p = 0; p < kParts; ++p) own = p == part ? (top > bin ? counts[p].y : 0) + (top - 1 > bin ? counts[p].x : 0) : own;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) own += __shfl_xor(own, o);
+        own = sum_lanes(own);
         if ((tid & 63) == 0) atomicAdd(&above, own);
     }
     __syncthreads();
@@ -363,15 +364,9 @@ __global__ __launch_bounds__(kThreads) void evict_places_kernel(Cut c, const Sta
         const int upto = scan_lanes(same);
         const int kept = above[i] + min(max(f.left - (upto - same), 0), same);
         const Part at = part_of(i, first, n, len, part_rows);
-        equal = lane < part ? same : 0;
-        holes = lane < part && i < first ? at.hi - at.lo - kept : 0;
-        movers = lane < part && i >= first ? kept : 0;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            equal += __shfl_xor(equal, o);
-            holes += __shfl_xor(holes, o);
-            movers += __shfl_xor(movers, o);
-        }
+        equal = sum_lanes(lane < part ? same : 0);
+        holes = sum_lanes(lane < part && i < first ? at.hi - at.lo - kept : 0);
+        movers = sum_lanes(lane < part && i >= first ? kept : 0);
     }
     const unsigned long long below = (1ull << lane) - 1;
     uint32_t first_keys[8];
@@ -400,11 +395,8 @@ __global__ __launch_bounds__(kThreads) void evict_places_kernel(Cut c, const Sta
         own_above += row < hi && x > f.upper ? 1 : 0;
         own_equal += row < hi && x == f.upper ? 1 : 0;
     });
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        own_above += __shfl_xor(own_above, o);
-        own_equal += __shfl_xor(own_equal, o);
-    }
+    own_above = sum_lanes(own_above);
+    own_equal = sum_lanes(own_equal);
     if (lane == 0) { sums[0][wave] = own_above; sums[1][wave] = own_equal; }
     __syncthreads();
     int kept_before = 0;
