@@ -1522,6 +1522,16 @@ MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
         const long long tiles = (l_cap + kStepTile - 1) / kStepTile, most = (tiles + kStepWaves - 1) / kStepWaves;
         p.n_split = (int)std::max<long long>(1, std::min<long long>(most, g_force_split ? (long long)g_force_split : 256 / units));
         if (!g_force_split && tiles <= (d->head_dim == 64 ? 12 : 8)) p.n_split = 1;
+        else if (!g_force_split) {
+            // More where the last round of workgroups would leave many units idle, by estimates in us (28 heads on 4, one token; 132 sets of
+            // 6,000 rows, 1 to 6 parts 119, 123, 97, 107, 95, 104; 300 of 2,500, 1 to 3 parts 112, 95, 93; 144 of 2,500 with four tokens 69, 91, 79).
+            auto us = [&](long long n) {
+                const double walk = (double)((tiles + kStepWaves * n - 1) / (kStepWaves * n)), rounds = (double)((units * n + 255) / 256);
+                return rounds * (3 + (d->head_dim == 64 ? 1.75 : 2.4) * walk) + (n > 1 ? 4 + units * rows / 350. : 0);
+            };
+            for (long long n = p.n_split + 1; n <= std::min(most, 1024 / units); ++n)
+                if (us(n) < 0.9 * us(p.n_split)) p.n_split = (int)n;
+        }
     } else if (d->dtype == VXL_BF16) {
         ring_plan(p, units, rows, d->head_dim, l_cap);
         // Parts of the query rows, by estimates in us: rounds of two workgroups on a compute unit, but no less than the workgroup whose keys
