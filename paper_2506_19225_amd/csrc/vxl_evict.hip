@@ -238,7 +238,7 @@ __global__ __launch_bounds__(kThreads) void evict_set_kernel(Cut c, Move m, int3
 // Longer sets: each in parts of `part_rows` rows below n and of as many from n on (so that a part has holes or movers, never both), at most kParts
 // of them, a workgroup each.  Every pass is a launch: the counts of a part's bins are written down, the next launch adds those of all
 // parts, finds the bin and counts on.  The last one knows from the counts how many rows every part before it keeps.
-// 131,328 rows of 4 KV heads to 16,384: 4.6, 8.0 and 7.9 us for the passes, 13.3 for the places, 12.8 for the moves, which copy 64 MB.
+// 131,328 rows of 4 KV heads to 16,384: 4.4, 7.4 and 7.4 us for the passes, 12.7 for the places, 12.6 for the moves, which copy 64 MB.
 // ------------------------------------------------------------------------------------------
 constexpr int kParts = 20;
 struct State {                 // of a set between the launches, in the workspace
