@@ -1500,6 +1500,17 @@ static void ring_plan(MixedPlan& p, long long units, long long rows, int D, int 
     }
 }
 
+// Splits: as forced, or from `first` on up to `last` the number that an estimate in us says is faster by a tenth (from eight on the first: no more
+// than an eighth of a round is lost, and the search would take longer than it saves).
+template <typename F>
+static int split_by_rounds(int forced, long long first, long long last, F&& us, long long most) {
+    if (forced) return (int)std::min<long long>(most, forced);
+    long long best = first;
+    for (long long n = first + 1; first < 8 && n <= last; ++n)
+        if (us(n) < 0.9 * us(best)) best = n;
+    return (int)best;
+}
+
 MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     MixedPlan p{};
     const long long rows = (long long)(d->n_q_heads / d->n_kv_heads) * T, units = (long long)batch * d->n_kv_heads;
@@ -1514,24 +1525,25 @@ MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
         // on 4, one token, D = 128: 128 rows 9.7 us, with the second launch 12; 192 rows 13.5 by one workgroup, 12.1 by two and the launch).
         const long long tiles = (l_cap + kF32Tile - 1) / kF32Tile, most = (tiles + kF32Waves - 1) / kF32Waves;
         const long long base = units * ((rows + kF32Block - 1) / kF32Block);
-        p.n_split = (int)std::max<long long>(1, std::min<long long>(most, g_force_split ? (long long)g_force_split : 512 / base));
+        // More where the last round would leave many compute units idle, by estimates in us (14 heads on 2 of D = 64: 300 tokens over 5,000 rows, 1 to 5 parts
+        // 134, 109, 96, 94, 91; 80 of four queries over 3,000 84, 73, 66, 64, 62).
+        p.n_split = split_by_rounds(g_force_split, std::min(most, std::max(1ll, 512 / base)), std::min(most, 2048 / base), [&](long long n) {
+            const double walk = (double)((tiles + kF32Waves * n - 1) / (kF32Waves * n)), rounds = (double)((base * n + 511) / 512);
+            return rounds * (5 + (d->head_dim == 64 ? 3 : 5) * walk) + (n > 1 ? 4 + units * rows / 1000. : 0);
+        }, most);
     } else if (p.few) {
         // A workgroup on every compute unit, each wave of one with a tile at least.  Short sets by one workgroup each, which needs no second
         // launch (us, one workgroup and splits, 28 heads on 4, one token: 256 rows 9.0, 10.3, 384 rows 10.7, 10.3; four tokens 12.1, 13.9 and
         // 14.5, 14.1; D = 64, 14 on 2, 384 rows 8.9, 9.0 and 11.5, 12.1, 512 rows 9.7, 9.2 and 12.4, 12.1).
         const long long tiles = (l_cap + kStepTile - 1) / kStepTile, most = (tiles + kStepWaves - 1) / kStepWaves;
-        p.n_split = (int)std::max<long long>(1, std::min<long long>(most, g_force_split ? (long long)g_force_split : 256 / units));
-        if (!g_force_split && tiles <= (d->head_dim == 64 ? 12 : 8)) p.n_split = 1;
-        else if (!g_force_split) {
-            // More where the last round of workgroups would leave many units idle, by estimates in us (28 heads on 4, one token; 132 sets of
-            // 6,000 rows, 1 to 6 parts 119, 123, 97, 107, 95, 104; 300 of 2,500, 1 to 3 parts 112, 95, 93; 144 of 2,500 with four tokens 69, 91, 79).
-            auto us = [&](long long n) {
-                const double walk = (double)((tiles + kStepWaves * n - 1) / (kStepWaves * n)), rounds = (double)((units * n + 255) / 256);
-                return rounds * (3 + (d->head_dim == 64 ? 1.75 : 2.4) * walk) + (n > 1 ? 4 + units * rows / 350. : 0);
-            };
-            for (long long n = p.n_split + 1; n <= std::min(most, 1024 / units); ++n)
-                if (us(n) < 0.9 * us(p.n_split)) p.n_split = (int)n;
-        }
+        // More where the last round of workgroups would leave many units idle, by estimates in us (28 heads on 4, one token; 132 sets of
+        // 6,000 rows, 1 to 6 parts 119, 123, 97, 107, 95, 104; 300 of 2,500, 1 to 3 parts 112, 95, 93; 144 of 2,500 with four tokens 69, 91, 79).
+        const long long full = std::min(most, std::max(1ll, 256 / units));
+        const bool one = tiles <= (d->head_dim == 64 ? 12 : 8);
+        p.n_split = split_by_rounds(g_force_split, one ? 1 : full, one ? 1 : std::min(most, 1024 / units), [&](long long n) {
+            const double walk = (double)((tiles + kStepWaves * n - 1) / (kStepWaves * n)), rounds = (double)((units * n + 255) / 256);
+            return rounds * (3 + (d->head_dim == 64 ? 1.75 : 2.4) * walk) + (n > 1 ? 4 + units * rows / 350. : 0);
+        }, most);
     } else if (d->dtype == VXL_BF16) {
         ring_plan(p, units, rows, d->head_dim, l_cap);
         // Parts of the query rows, by estimates in us: rounds of two workgroups on a compute unit, but no less than the workgroup whose keys
