@@ -536,7 +536,8 @@ typedef struct {
  * is rounded to bf16, 2^-8 of it at most, LSE and weight_out have fp32's errors, a capped logit is off by 2^-22 softcap at most besides those of
  * its product); the same call gives the same bits.  A token
  * with a visible logit of NaN or +inf has no softmax: its O and LSE are NaN, and so is the weight of the rows that it sees.  What a token
- * does not see never matters to it, whatever its rows hold.
+ * does not see never matters to it beyond the tolerance, whatever its rows hold; keys and finite values of rows that no token of the call sees change
+ * no bit (a value that is no finite number makes the rows of O that share a product with it be computed again, in fp32 throughout).
  * Errors: VXL_ERR_INVALID_ARG (also one of q_pos and row_pos without the other, a rule that needs positions without them, outputs
  * or a workspace that overlap each other or an input), VXL_ERR_UNSUPPORTED (also batch * n_kv_heads > 65,535, 2^30 stacked
  * rows of a query and KV head), VXL_ERR_WORKSPACE, VXL_ERR_HIP.

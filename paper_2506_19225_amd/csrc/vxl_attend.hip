@@ -229,18 +229,22 @@ struct Reach {
     }
 };
 
-// From products s to softcap tanh(u), u = s scale / softcap, in units of log 2; one decision for the wave's elements:
+// From products s to softcap tanh(u), u = s scale / softcap, in units of log 2; one decision for the wave's elements that are seen.
+// What the others are has no part in it: where some element is not small, largest_seen(x), the largest magnitude of a lane's seen ones, decides (in
+// tiles seen in part; 64 tokens over 23,872 rows, all tiles in part: 4 % with a cap of 50, 14 % with one of 5).
 //   all |u| < 1/8, as with caps of 30 and more: the odd series to u^7 (the next term is 1.3e-9 of it there) in the product itself, its coefficients
 //   with the powers of scale / softcap in them, so that u is not made;
 //   else 1 - 2 / (e^2|u| + 1) with the sign of s, off by 4 roundings of the cap at most: the exponential, the sum and the quotient by one each of
 //   less than the cap, the argument by less than half a one.  The series to u^13 for all |u| < 0.4 is no faster, and both
 //   with a selection, exact to a rounding of the result, took 63 us where this takes 48 (64 tokens over 23,872 rows, a cap of 5).
-template <int N>
-__device__ __forceinline__ void cap_logits(float (&x)[N], const Rule& r) {
+template <int N, typename F>
+__device__ __forceinline__ void cap_logits(float (&x)[N], const Rule& r, bool all_seen, F&& largest_seen) {
     float top = 0.f;                                          // (NaN is NaN either way)
 #pragma unroll
     for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(x[i]));
-    if (__builtin_amdgcn_ballot_w64(!(top < r.cap_few)) == 0) {
+    bool small = __builtin_amdgcn_ballot_w64(!(top < r.cap_few)) == 0;
+    if (!small && !all_seen) small = __builtin_amdgcn_ballot_w64(!(largest_seen(x) < r.cap_few)) == 0;
+    if (small) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float z = x[i] * x[i], y = x[i] * r.c2;
@@ -254,6 +258,22 @@ __device__ __forceinline__ void cap_logits(float (&x)[N], const Rule& r) {
             if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);               // (four at a time: all at once need more registers than there are)
         }
     }
+}
+
+// Of a token's products with 32 keys, as a lane has them, the largest magnitude of those with keys of a position that it sees.
+__device__ __forceinline__ float largest_of(const Span& span, int n_always, const int32_t* pos, int hi, const float (&x)[16]) {
+    auto of = [&](auto first) __attribute__((always_inline)) {
+        float top = 0.f;
+#pragma unroll
+        for (int rq = 0; rq < 4; ++rq) {
+            const int4 p4 = *(const int4*)(pos + rq * 8 + hi * 4);
+            const int p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, shown<first>(span, p[i], fabsf(x[rq * 4 + i])));
+        }
+        return top;
+    };
+    return n_always > 0 ? of(std::true_type{}) : of(std::false_type{});
 }
 
 template <int D, int NW, bool POS>
@@ -349,7 +369,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_ring_kernel(Sets s, Rule r,
                 float c[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) c[i] = x[0][kb][i];
-                cap_logits(c, r);
+                cap_logits(c, r, !POS || !partial, [&](const float (&y)[16]) __attribute__((always_inline)) {
+                    return largest_of(span, r.n_always, tile_pos + kb * 32, hi, y);
+                });
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[0][kb][i] = c[i];
             }
@@ -637,7 +659,8 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s,
         float y[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) y[j] = x[0][0][j];
-        if (capped) cap_logits(y, r);
+        if (capped)
+            cap_logits(y, r, !POS || all, [&](const float (&z)[16]) __attribute__((always_inline)) { return largest_of(span, r.n_always, tile_pos, hi, z); });
         if (biased) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) y[j] = fmaf(-slope2, (float)abs(pq - tile_pos[acc_key(0, j, hi)]), y[j] * unit_of);
@@ -1048,13 +1071,15 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
             for (int kb = 0; kb < 2; ++kb) x[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kb][ks], a, x[kb], 0, 0, 0);
         }
     };
-    auto cap = [&](f32x16 (&x)[2]) __attribute__((always_inline)) {
+    auto cap = [&](f32x16 (&x)[2], bool all_seen, const Span& span) __attribute__((always_inline)) {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             float c[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) c[i] = x[kb][i];
-            cap_logits(c, r);
+            cap_logits(c, r, all_seen, [&](const float (&y)[16]) __attribute__((always_inline)) {
+                return largest_of(span, r.n_always, pos_lds[POS ? wave : 0] + kb * 32, hi, y);
+            });
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[kb][i] = c[i];
         }
@@ -1130,7 +1155,7 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
                 for (int half = 0; half < 2; ++half) {
                     f32x16 x[2];
                     product(q, half, x);
-                    cap(x);
+                    cap(x, true, Span{});
                     plain(x, lse_of(half));
                 }
                 continue;
@@ -1148,7 +1173,7 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
                 row.slope2 = biased ? infos[128 + half * 32 + l32] * kLog2e : 0.f;
                 f32x16 x[2];
                 product(q, half, x);
-                if (capped) cap(x);
+                if (capped) cap(x, !POS || all, row.span);
                 if (biased) by_position(x, [&](float y, int p) { return fmaf(-row.slope2, (float)abs(row.pq - p), y * unit_of); });
                 if (all) {
                     plain(x, row.lse);
