@@ -248,7 +248,7 @@ __device__ __forceinline__ void cap_logits(float (&x)[N], const Rule& r, bool al
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float z = x[i] * x[i], y = x[i] * r.c2;
-            x[i] = fmaf(y * z, fmaf(fmaf(r.cap_k[2], z, r.cap_k[1]), z, r.cap_k[0]), y);
+            x[i] = fmaf(y, z * fmaf(fmaf(r.cap_k[2], z, r.cap_k[1]), z, r.cap_k[0]), y);     // (y z may be no number: z is up to 2^108)
         }
     } else {
 #pragma unroll

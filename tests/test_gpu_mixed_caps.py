@@ -46,3 +46,27 @@ def test_keys_that_no_token_sees_change_no_bit(rule, t, plan, dtype):
             check_attend(results[0], qd, k, v, [n], dtype, 0.0, q_pos, pos, weight, softcap=cap, **rule)
     for got in results[1:]:
         assert all(np.array_equal(x, y) for x, y in zip(got, results[0]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("t", [1, 4, 50])
+@pytest.mark.parametrize("softcap", [2.0 ** 48, 2.0 ** 50, 2.0 ** 55])
+def test_caps_far_above_large_logits(softcap, t, dtype):
+    """Products of 2^45, whose third power is no number of 32 bits: the one row of such a logit has all the weight, one of its negative none.  The
+    logit is off by the roundings of the scale, its unit and their product, of the series' two last steps, and of the unit that it is given in; from 2^-6 of such a cap
+    on bf16 sets have the exponential, off by 2^-22 softcap."""
+    n = 200
+    rng = np.random.default_rng(t)
+    k, v, _ = sets(rng, 1, 2, n, 64, dtype, [n])
+    qd = np.full((1, t, 8, 64), 2.0 ** 20, np.float32)
+    k[:] = 0.0
+    k[0, 0, 77], k[0, 1, 130], k[0, :, 5] = 2.0 ** 19, 2.0 ** 19, -2.0 ** 19
+    out, lse, weight = attend(qd, k, v, [n], dtype, 0.0, softcap=softcap)
+    for h in range(8):
+        assert (out[0, :, h] == v[0, h // 4, (77, 130)[h // 4]]).all()
+    want = softcap * np.tanh(2.0 ** 42 / softcap)
+    by_exp = dtype == "bf16" and 2.0 ** 42 / softcap >= 2.0 ** -6
+    assert (np.abs(lse - want) <= 8 * E * want + by_exp * 2.0 ** -22 * softcap).all()
+    one = np.zeros((2, n))
+    one[0, 77] = one[1, 130] = 4 * t
+    assert np.array_equal(weight[0], one)
