@@ -724,16 +724,17 @@ struct PlainRows {
             if (steps_into(at + g * head, tok, n, lo - bytes, hi)) return true;
         return false;
     }
-    // Whether one of the rows meets one of the same number of tokens (where these are not as far apart, or the heads very many:
-    // whether the memory from first to last does).
+    // Whether one of the rows meets one of the same number of tokens (where these are not as far apart, or heads that are not are
+    // very many: whether the memory from first to last does).
     bool meet(const PlainRows& o) const {
         if (o.at + o.span() <= at || at + span() <= o.at) return false;
-        if (o.tok != tok || (__int128)heads * o.heads > 1 << 20) return true;
-        if (heads == o.heads && head == o.head) {
-            for (long long g = 1 - heads; g < heads; ++g)
+        if (o.tok != tok) return true;
+        if (head == o.head) {
+            for (long long g = 1 - heads; g < o.heads; ++g)
                 if (steps_into(o.at - at + g * head - (n - 1) * tok, tok, 2 * n - 1, -bytes, bytes)) return true;
             return false;
         }
+        if ((__int128)heads * o.heads > 1 << 20) return true;
         for (long long g = 0; g < heads; ++g)
             for (long long h = 0; h < o.heads; ++h)
                 if (steps_into(o.at + h * o.head - at - g * head - (n - 1) * tok, tok, 2 * n - 1, -bytes, bytes)) return true;
