@@ -442,14 +442,17 @@ bool has(long long numel, std::initializer_list<long long> dims) {
     for (long long x : dims) n *= x;
     return numel == 0 || n == numel;
 }
-// Whether one of queries or keys holds the rows of n tokens, by the descriptor's layout.
+// Whether one of queries or keys holds the rows of n tokens, by the descriptor's layout.  Without strides heads lie n tokens apart, so that several
+// of them in a tensor of more tokens would be taken for rows of others.
 bool holds_rows(const vxl_attn_desc* d, long long n, long long numel, bool queries) {
-    if (!queries) return holds(d, n, numel);
-    vxl_attn_desc q = *d;
-    q.n_kv_heads = d->n_q_heads;
-    q.kv_stride_head = d->q_stride_head;
-    q.kv_stride_tok = d->q_stride_tok;
-    return holds(&q, n, numel);
+    vxl_attn_desc x = *d;
+    if (queries) {
+        x.n_kv_heads = d->n_q_heads;
+        x.kv_stride_head = d->q_stride_head;
+        x.kv_stride_tok = d->q_stride_tok;
+    }
+    if (!x.kv_stride_head && x.n_kv_heads > 1) return (__int128)x.n_kv_heads * n * x.head_dim == numel;
+    return holds(&x, n, numel);
 }
 
 PyObject* rotate(PyObject* self, PyObject* const* args, Py_ssize_t n) {

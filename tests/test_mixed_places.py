@@ -1,0 +1,50 @@
+"""Tensors of more tokens than a call on rotary positions or growing sets takes off its positions, where the layout depends on their number."""
+import pytest
+
+from paper_2506_19225_amd import vxl
+
+from test_binding_native import streams  # noqa: F401
+from test_mixed_refusals import (AT, B, BF, D, DESC, HKV, HQ, I32, K, KO, Q, QD, QO, T, Typed, V, append, launches, refused,  # noqa: F401
+                                 rotate)
+
+HEADS_FIRST = vxl.make_desc(HQ, HKV, D, "bf16")
+
+
+def of(heads, tokens):
+    return Typed((heads, tokens, D), BF)
+
+
+def good(n=B * T):
+    return dict(q=of(HQ, n), k=of(HKV, n), qo=of(HQ, n), ko=of(HKV, n))
+
+
+def test_rotation_of_heads_of_more_tokens_than_positions():
+    """[heads, tokens, D] without strides: rows of a head after the first lie where the number of positions says."""
+    n = B * T
+    assert refused(rotate, desc=HEADS_FIRST, **good()) == vxl.VXL_ERR_HIP
+    assert refused(rotate, desc=HEADS_FIRST, **dict(good(), k=None, ko=None)) == vxl.VXL_ERR_HIP
+    for less in (n - 1, 1, 0):
+        at = Typed((less,), I32)
+        assert refused(rotate, desc=HEADS_FIRST, at=at, **good()) == vxl.VXL_ERR_INVALID_ARG, less
+        for name, x in good().items():
+            assert refused(rotate, desc=HEADS_FIRST, at=at, **dict(good(less), **{name: x})) == vxl.VXL_ERR_INVALID_ARG, (less, name)
+    for name, x in good().items():
+        more = Typed((x.shape[0], n + 1, D), BF)
+        assert refused(rotate, desc=HEADS_FIRST, **dict(good(), **{name: more})) == vxl.VXL_ERR_INVALID_ARG, name
+    # token after token fewer positions are the first tokens, as before
+    assert refused(rotate, at=Typed((n - 1,), I32)) == refused(rotate, at=Typed((1,), I32)) == vxl.VXL_ERR_HIP
+    one = vxl.make_desc(1, 1, D, "bf16")                                      # (one head: the same)
+    assert refused(rotate, desc=one, q=of(1, n + 3), k=of(1, n + 2), qo=of(1, n), ko=of(1, n + 1)) == vxl.VXL_ERR_HIP
+    empty = {name: Typed((x.shape[0], 0, D), BF, 0) for name, x in good().items()}
+    rotate(desc=HEADS_FIRST, at=Typed((0,), I32, 0), **empty)                # (nothing to do)
+    rotate(at=Typed((0,), I32, 0))
+
+
+def test_append_of_heads_of_more_tokens_than_positions():
+    n = B * T
+    fit = dict(q=of(HQ, n), k=of(HKV, n), v=of(HKV, n))
+    assert refused(append, desc=HEADS_FIRST, **fit) == vxl.VXL_ERR_HIP
+    for name, x in fit.items():
+        for tokens in (n + 1, 2 * n):
+            assert refused(append, desc=HEADS_FIRST, **dict(fit, **{name: of(x.shape[0], tokens)})) == vxl.VXL_ERR_INVALID_ARG, name
+    assert refused(append, q=Typed((n + 5, HQ, D), BF), k=Typed((n + 1, HKV, D), BF)) == vxl.VXL_ERR_HIP
