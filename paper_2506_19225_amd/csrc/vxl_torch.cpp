@@ -457,9 +457,9 @@ bool holds_rows(const vxl_attn_desc* d, long long n, long long numel, bool queri
 
 PyObject* rotate(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     return call<kDesc, kRotary, kInts, kNumel, kOfDesc, kNumel, kOfDesc, kNumel, kOfDesc, kNumel, kOfDesc, kNumel>(
-        self, args, n, [](const State& lib, const long long* a) {
+        self, args, n, [&](const State& lib, const long long* a) {
         const long long tokens = a[3];
-        if (!in_32_bits(tokens)) return VXL_ERR_INVALID_ARG;
+        if (args[2] == Py_None || !in_32_bits(tokens)) return VXL_ERR_INVALID_ARG;          // (no positions are not positions of no tokens)
         for (int i : {4, 6, 8, 10})
             if (a[i] && !holds_rows(desc(a[0]), tokens, a[i + 1], i == 4 || i == 8)) return VXL_ERR_INVALID_ARG;
         return lib.rotate(desc(a[0]), ptr<vxl_rotary>(a[1]), ptr<int32_t>(a[2]), (int32_t)tokens, ptr<void>(a[4]), ptr<void>(a[6]),

@@ -48,3 +48,9 @@ def test_append_of_heads_of_more_tokens_than_positions():
         for tokens in (n + 1, 2 * n):
             assert refused(append, desc=HEADS_FIRST, **dict(fit, **{name: of(x.shape[0], tokens)})) == vxl.VXL_ERR_INVALID_ARG, name
     assert refused(append, q=Typed((n + 5, HQ, D), BF), k=Typed((n + 1, HKV, D), BF)) == vxl.VXL_ERR_HIP
+
+
+def test_rotation_without_positions():
+    """Not a call of no tokens, which would leave the results unwritten without a word."""
+    for kw in (dict(), dict(k=None, ko=None), dict(desc=HEADS_FIRST, **good())):
+        assert refused(rotate, at=None, **kw) == vxl.VXL_ERR_INVALID_ARG
