@@ -40,9 +40,9 @@ struct State {
 // (its tensors as they are at the call, and its format) or None, a null pointer; a tensor (its
 // data pointer; a contiguous CUDA tensor or AssertionError) or None, a null pointer; a number.  Python does not pass
 // kNumel, the number of elements of the tensor before it (0 for None), and size(i, d), dimension d of its argument i.
-// The calls on rotary positions and growing sets hold their tensors to more: of the descriptor's type, float32 or int32, on one device, the
-// current one; beside them a rotary or a rule, or None, a null pointer.
-enum Kind { kLayout, kDesc, kCache, kTensor, kInt, kRotary, kRule, kOfDesc, kFloats, kInts, kNumel, kSize };
+// The calls on rotary positions and growing sets hold their tensors to more: of the descriptor's type, float32 or int32 (the workspace: of
+// any), on one device, the current one; beside them a rotary or a rule, or None, a null pointer.
+enum Kind { kLayout, kDesc, kCache, kTensor, kInt, kRotary, kRule, kOfDesc, kFloats, kInts, kWorkspace, kNumel, kSize };
 constexpr int size(int arg, int dim) { return kSize | arg << 8 | dim << 16; }
 
 // A number that an object answers with (a new reference, or null where it raised).
@@ -203,16 +203,22 @@ bool cache_of(const State& st, Frame& f, PyObject* o, long long* out) {
     return true;
 }
 
-// Pointer of a tensor of this type on the device of the others, or null for None.
+// Pointer of a tensor on the device of the others, or null for None.
+bool placed_of(Frame& f, PyObject* o, long long* out) {
+    if (!tensor_of(o, out)) return false;
+    if (!THPVariable_Check(o)) return true;
+    const int device = THPVariable_Unpack(o).device().index();
+    if (f.device >= 0 && device != f.device) { PyErr_SetString(PyExc_ValueError, "the tensors are on several devices"); return false; }
+    f.device = device;
+    return true;
+}
+
+// The same for one of this type.
 bool typed_of(Frame& f, PyObject* o, at::ScalarType type, const char* name, long long* out) {
-    if (!tensor_of(o, out) || o == Py_None) return !PyErr_Occurred();
+    if (!placed_of(f, o, out) || o == Py_None) return !PyErr_Occurred();
     bool ok;
     if (THPVariable_Check(o)) {
-        const at::Tensor& t = THPVariable_Unpack(o);
-        ok = t.scalar_type() == type;
-        const int device = t.device().index();
-        if (f.device >= 0 && device != f.device) { PyErr_SetString(PyExc_ValueError, "the tensors are on several devices"); return false; }
-        f.device = device;
+        ok = THPVariable_Unpack(o).scalar_type() == type;
     } else {
         PyObject* dtype = PyObject_GetAttrString(o, "dtype");
         if (!dtype) return false;
@@ -282,6 +288,7 @@ bool convert(const State& st, PyObject* const* args, Frame& f, long long* out) {
     else if constexpr (KIND == kRule) return rule_of(st, f, args[(*next)++], out);
     else if constexpr (KIND == kOfDesc) return data_of(f, args[(*next)++], out);
     else if constexpr (KIND == kFloats) return typed_of(f, args[(*next)++], at::kFloat, "float32", out);
+    else if constexpr (KIND == kWorkspace) return placed_of(f, args[(*next)++], out);
     else if constexpr (KIND == kInts) return typed_of(f, args[(*next)++], at::kInt, "int32", out);
     else if constexpr (KIND == kCache) return cache_of(st, f, args[(*next)++], out);
     else if constexpr (KIND == kTensor) return tensor_of(args[(*next)++], out);
@@ -487,7 +494,7 @@ PyObject* mixed_append(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 // (batch and tokens: of qd; rows: of kmix)
 PyObject* mixed_attend(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     return call<kDesc, kRule, kOfDesc, size(2, 0), size(2, 1), kNumel, kInts, kNumel, kOfDesc, size(4, 2), kNumel, kOfDesc, kNumel, kInts, kNumel,
-                kInts, kNumel, kOfDesc, kNumel, kFloats, kNumel, kFloats, kNumel, kFloats, kNumel, kTensor, kNumel>(
+                kInts, kNumel, kOfDesc, kNumel, kFloats, kNumel, kFloats, kNumel, kFloats, kNumel, kWorkspace, kNumel>(
         self, args, n, [](const State& lib, const long long* a) {
         const vxl_attn_desc* d = desc(a[0]);
         const long long batch = a[3], tokens = a[4], cap = a[9], hkv = d->n_kv_heads, hq = d->n_q_heads;
@@ -505,7 +512,7 @@ PyObject* mixed_attend(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 // (batch and rows: of kmix; rows of the result: of kout)
 PyObject* mixed_evict(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     return call<kDesc, kOfDesc, size(1, 0), size(1, 2), kNumel, kOfDesc, kNumel, kInts, kNumel, kFloats, kNumel, kInts, kNumel, kInts, kNumel, kInt,
-                kInt, kInt, kOfDesc, size(10, 2), kNumel, kOfDesc, kNumel, kFloats, kNumel, kInts, kNumel, kInts, kNumel, kTensor, kNumel>(
+                kInt, kInt, kOfDesc, size(10, 2), kNumel, kOfDesc, kNumel, kFloats, kNumel, kInts, kNumel, kInts, kNumel, kWorkspace, kNumel>(
         self, args, n, [](const State& lib, const long long* a) {
         const vxl_attn_desc* d = desc(a[0]);
         const long long batch = a[2], cap = a[3], to = a[19], hkv = d->n_kv_heads, dim = d->head_dim;

@@ -1,11 +1,13 @@
-"""Tensors of more tokens than a call on rotary positions or growing sets takes off its positions, where the layout depends on their number."""
+"""Calls on rotary positions and growing sets whose tensors lie elsewhere than they say: of more tokens than there are positions where the layout
+depends on their number, or on another device."""
 import pytest
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
 
 from paper_2506_19225_amd import vxl
 
 from test_binding_native import streams  # noqa: F401
-from test_mixed_refusals import (AT, B, BF, D, DESC, HKV, HQ, I32, K, KO, Q, QD, QO, T, Typed, V, append, launches, refused,  # noqa: F401
-                                 rotate)
+from test_mixed_refusals import B, BF, D, HKV, HQ, I32, T, Typed, append, attend, evict, launches, refused, rotate  # noqa: F401
 
 HEADS_FIRST = vxl.make_desc(HQ, HKV, D, "bf16")
 
@@ -54,3 +56,23 @@ def test_rotation_without_positions():
     """Not a call of no tokens, which would leave the results unwritten without a word."""
     for kw in (dict(), dict(k=None, ko=None), dict(desc=HEADS_FIRST, **good())):
         assert refused(rotate, at=None, **kw) == vxl.VXL_ERR_INVALID_ARG
+
+
+@pytest.mark.filterwarnings("ignore:Accessing the data pointer of FakeTensor")
+@pytest.mark.parametrize("call", [attend, evict])
+def test_a_workspace_of_another_device(call, monkeypatch):
+    """Tensors that say where they are and have no memory: of the current device for the library to refuse, of another one refused here."""
+    def on(device):
+        with FakeTensorMode():
+            return torch.empty(1 << 20, dtype=torch.uint8, device=device)
+    monkeypatch.setattr(vxl, "_native", None)                                # (a binding that asks for the device as it is set here)
+    assert refused(call, ws=on("cuda:0")) == vxl.VXL_ERR_WORKSPACE
+    with pytest.raises(ValueError, match="another device than the current one"):
+        call(ws=on("cuda:1"))
+    monkeypatch.setattr(vxl, "_current_device", lambda: 1)
+    monkeypatch.setattr(vxl, "_native", None)
+    assert refused(call, ws=on("cuda:1")) == vxl.VXL_ERR_WORKSPACE
+    with FakeTensorMode():
+        weight = torch.empty(2, 2, 20, device="cuda:1")
+    with pytest.raises(ValueError, match="several devices"):
+        call(w=weight, ws=on("cuda:0"))
