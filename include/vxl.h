@@ -480,7 +480,9 @@ typedef struct {
  *                       Q, K_out == K); K and K_out may both be NULL
  *   positions           device int32 [n_tokens], any values
  * n_tokens == 0 does nothing.  No workspace.  Errors: VXL_ERR_INVALID_ARG (null or misaligned buffers, a malformed rotary,
- * outputs that meet each other or an input in any other way), VXL_ERR_UNSUPPORTED, VXL_ERR_HIP.
+ * outputs that meet each other or an input in any other way), VXL_ERR_UNSUPPORTED, VXL_ERR_HIP.  Rows of one tensor may lie between
+ * rows of another, as those of a fused projection do, where their stride_tok is the same, and their stride_head too or their heads
+ * multiply to 2^20 at most; else tensors meet if the memory from their first to their last row does.
  */
 vxl_status vxl_rotate(const vxl_attn_desc* desc, const vxl_rotary* rotary, const int32_t* positions, int32_t n_tokens,
                       const void* Q, const void* K, void* Q_out, void* K_out, vxl_stream stream);
@@ -496,6 +498,10 @@ vxl_status vxl_rotate(const vxl_attn_desc* desc, const vxl_rotary* rotary, const
  *   row_pos     device int32 [batch, n_kv_heads, l_cap] or NULL: positions of the rows (written for the new ones)
  *   row_weight  device float [batch, n_kv_heads, l_cap] or NULL: attention weights of the rows (0 for the new ones)
  *   rotary      NULL: queries and keys are copied as they are
+ * A set begins as a gather leaves it, with an l_cap that has room for what is to come: row_pos[b][g][r] = src_idx[b][r] for every
+ * KV head g (the position of a prompt's token is its id; pooled rows, of a negative src_idx, need a position of the caller's choice,
+ * as a row of a negative one counts as empty), row_weight = 0, and before every call mix_len[b] += n_new.  A gather's report of an
+ * overflow (mix_len[b] < 0) has to be looked for before that.
  * No workspace.  Errors: VXL_ERR_INVALID_ARG (null or misaligned buffers, a malformed rotary, outputs that overlap each other or
  * an input), VXL_ERR_UNSUPPORTED, VXL_ERR_HIP.
  */
