@@ -23,8 +23,8 @@ struct Rule {
     const int32_t *q_pos, *row_pos;
 };
 
-// Rows that a token sees: positions lo .. lo + width - 1 and 0 .. na - 1.  A padding token: none.  (Without positions every row of the set has
-// position 0 and every token sees it.)
+// Rows that a token sees: positions lo .. lo + width - 1 and 0 .. na - 1.  A padding token: none.  (Without positions every row of the set
+// has position 0 and every token sees it.)
 struct Span {
     int lo;
     unsigned width, na;
@@ -38,8 +38,8 @@ __device__ __forceinline__ Span span_of(const Rule& r, int pq) {
 }
 // (A negative position is 2^31 or more as it is and with lo taken off.)
 __device__ __forceinline__ bool sees(const Span& s, int pk) { return ((unsigned)pk - (unsigned)s.lo < s.width) | ((unsigned)pk < s.na); }
-// A logit, or -inf where it is hidden; FIRST: there may be an na.  Selections one after the other: comparisons that are joined go through scalar
-// registers and wait for them.
+// A logit, or -inf where it is hidden; FIRST: there may be an na.  Selections one after the other: comparisons that are joined go through
+// scalar registers and wait for them.
 template <bool FIRST>
 __device__ __forceinline__ float shown(const Span& s, int pk, float y) {
     float z = (unsigned)pk - (unsigned)s.lo < s.width ? y : -INFINITY;
@@ -172,16 +172,18 @@ __global__ __launch_bounds__(256) void simple_weights_kernel(Sets s, Rule r, con
 
 // ------------------------------------------------------------------------------------------
 // Many stacked query rows (rho = t * G + head of the group): 32 per wave, NW waves per workgroup; the 64-key tiles of the workgroup's split
-// stream through a ring of four LDS stages by direct loads, two tiles ahead of the arithmetic, as in the plain decode's ring, whose products
-// and layouts these are.  What a rule adds:
+// stream through a ring of four LDS stages by direct loads, two tiles ahead of the arithmetic, as in the plain decode's ring, whose
+// products and layouts these are.  What a rule adds:
 //   * The positions of a tile come with it, by one wave's load.  A lane has a key's; against the range of positions that the wave's 32 rows
 //     see, a ballot each tells a tile that none sees (skipped), one that all see (nothing more) and one that needs a test per element;
 //     only then, and for a bias, a lane reads the positions of its elements.
-//   * Sums are of the weights as they are, not as rounded to bf16 for the second product, so that the LSE has fp32's error.
+//   * The second product takes its weights in bf16, as the plain decode's does (each off by 2^-8 of it at most, what the rounding of a
+//     value or of a result is; the fp32 instruction has a 1/16 of the rate).  Sums are of the weights as they are, so that LSE and row
+//     weights have fp32's error.
 //   * A value that is not a number reaches rows that do not see it, 0 * inf: a row whose result is none is made again by exact_row.
-// Bound by the matrix instructions, and with a cap by the vector ones.  2,048 tokens of 28 heads on 4 over 18,688 rows, 519 GFLOP
-// of products: 512 us alone, 1.0 PFLOP/s where a library product of 8192^3 reaches 1.24; 64 tokens over 23,872 rows: 36 us, capped 43
-// (48 by the exponential).  128 and 256 rows a workgroup: see ring_plan.
+// Bound by the matrix instructions, and with a cap by the vector ones.  In replayed graphs (boxes differ by some 5 %), 2,048 tokens of 28
+// heads on 4 over 18,688 rows, 519 GFLOP of products: 540 us, 0.96 PFLOP/s where a library product of 8192^3 reaches 1.24; 64 tokens over
+// 23,872 rows, with the merge of the splits: 43 us, capped 48 (52 by the exponential).  128 and 256 rows a workgroup: see ring_plan.
 // ------------------------------------------------------------------------------------------
 constexpr float kLowest = -std::numeric_limits<float>::max();
 
@@ -229,14 +231,16 @@ struct Reach {
     }
 };
 
-// From products s to softcap tanh(u), u = s scale / softcap, in units of log 2; one decision for the wave's elements that are seen.
-// What the others are has no part in it: where some element is not small, largest_seen(x), the largest magnitude of a lane's seen ones, decides (in
-// tiles seen in part; 64 tokens over 23,872 rows, all tiles in part: 4 % with a cap of 50, 14 % with one of 5).
-//   all |u| < 1/8, as with caps of 30 and more: the odd series to u^7 (the next term is 1.3e-9 of it there) in the product itself, its coefficients
-//   with the powers of scale / softcap in them, so that u is not made;
-//   else 1 - 2 / (e^2|u| + 1) with the sign of s, off by 4 roundings of the cap at most: the exponential, the sum and the quotient by one each of
-//   less than the cap, the argument by less than half a one.  The series to u^13 for all |u| < 0.4 is no faster, and both
-//   with a selection, exact to a rounding of the result, took 63 us where this takes 48 (64 tokens over 23,872 rows, a cap of 5).
+// From products s to softcap tanh(u), u = s scale / softcap, in units of log 2; one decision for the wave's elements that are seen.  What
+// the others are has no part in it: in a tile seen in part, where some element is not small, largest_seen(x), the largest magnitude of a
+// lane's seen ones, decides (64 tokens over 23,872 rows, all tiles in part: 4 % more with a cap of 50, 14 % with one of 5).
+//   * All |u| < 1/8, as with caps of 30 and more: the odd series to u^7 (the next term is 1.3e-9 of it there) in the product itself, its
+//     coefficients with the powers of scale / softcap in them, so that u is not made.
+//   * Else 1 - 2 / (e^2|u| + 1) with the sign of s, off by 4 roundings of the cap at most: the exponential, the sum and the quotient by one
+//     each of less than the cap, the argument by less than half a one.  That is the error of LSE and row weights too: 9e-6 at most of a
+//     logit below a quarter of a cap of 50, where an fp32 tanh has 2e-6.
+// The series to u^13 for all |u| < 0.4 is no faster, and both with a selection, exact to a rounding of the result, took 63 us where the
+// exponential took 48 (the ring alone, 64 tokens over 23,872 rows, a cap of 5).
 template <int N, typename F>
 __device__ __forceinline__ void cap_logits(float (&x)[N], const Rule& r, bool all_seen, F&& largest_seen) {
     float top = 0.f;                                          // (NaN is NaN either way)
@@ -316,7 +320,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_ring_kernel(Sets s, Rule r,
             dma16(kb, roff + kp * 16, st + slot * 1024);
             dma16(vb, roff + vp * 16, st + C::TILE * 2 + slot * 1024);
         }
-        if (POS && wave == 0) dma4(pos + k_lo + row0, (uint32_t)min(lane, rlim) * 4, lds_base + C::POS_AT + (uint32_t)(t % C::NS) * (kKeyTile * 4));
+        if (POS && wave == 0)
+            dma4(pos + k_lo + row0, (uint32_t)min(lane, rlim) * 4, lds_base + C::POS_AT + (uint32_t)(t % C::NS) * (kKeyTile * 4));
     };
     if (n_t > 0) {
         issue(0);
@@ -490,8 +495,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_ring_kernel(Sets s, Rule r,
         for (int x = lane; x < D; x += 64) q_row[x] = as_float(((const uint16_t*)s.q)[out * D + x]);
         __builtin_amdgcn_wave_barrier();
         float m, l2, acc[D / 64];
-        exact_row<uint16_t, D>(r, q_row, kset, vset, r.row_pos ? r.row_pos + set : nullptr, k_lo, k_hi, 64, 64, r.q_pos ? r.q_pos[b * s.T + t] : 0,
-                               slope_of(r, hq), m, l2, acc);
+        exact_row<uint16_t, D>(r, q_row, kset, vset, r.row_pos ? r.row_pos + set : nullptr, k_lo, k_hi, 64, 64,
+                               r.q_pos ? r.q_pos[b * s.T + t] : 0, slope_of(r, hq), m, l2, acc);
 #pragma unroll
         for (int x = 0; x < D / 64; ++x) {
             if (n_split > 1) part.o[(part_row0 + row) * D + lane + 64 * x] = acc[x];
@@ -509,20 +514,20 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_ring_kernel(Sets s, Rule r,
     }
 }
 
-// Of a part with reference and sum ml, against a reference: its weight in the whole, 0 if it has none, whatever it holds (and then nothing of
-// it is added); 1 if its sum is not a number, which the whole then is not either.
+// Of a part with reference and sum ml, against a reference: its weight in the whole, 0 if it has none, whatever it holds (and then nothing
+// of it is added); 1 if its sum is not a number, which the whole then is not either.
 __device__ __forceinline__ float part_weight(float2 ml, float ref) {
     return ml.y == 0.f ? 0.f : ml.y != ml.y ? 1.f : __builtin_amdgcn_exp2f(ml.x - ref);
 }
 __device__ __forceinline__ float add_part(float f, float x, float sum) { return f == 0.f ? sum : fmaf(f, x, sum); }
 
 // ------------------------------------------------------------------------------------------
-// At most 32 stacked query rows, the generated tokens: bound by memory, or by latency.  Every wave walks 32-key tiles of its own, in turn with
-// the other waves of all splits, from two pairs of LDS areas filled by direct loads and counted by hand; the waves' (reference, sum,
+// At most 32 stacked query rows, the generated tokens: bound by memory, or by latency.  Every wave walks 32-key tiles of its own, in turn
+// with the other waves of all splits, from two pairs of LDS areas filled by direct loads and counted by hand; the waves' (reference, sum,
 // O) are merged through LDS.  The logits, in units of log 2, are kept in the workspace (4 bytes per query row and key beside 4 D of key and
 // value), so that the weights need no second pass over the keys: -inf where the row is not seen, kLowest for a seen one of -inf.
-// One token of eight queries, 28 heads on 4 of D = 128, 18,177 rows: 50 us for 298 MB of keys, values and numbers of rows, 5.9 TB/s (a 2 GiB copy
-// 4.9); of one query and 4,097 rows 7.0, launch and three dependent trips to memory.
+// One token of eight queries, 28 heads on 4 of D = 128, sets of up to 18,177 rows, 120,138 together: 50 us for 252 MB of keys, values and
+// numbers of rows, 5.0 TB/s, the rate of a copy (4.9); of one query and 4,097 rows 7.0, launch and three dependent trips to memory.
 // ------------------------------------------------------------------------------------------
 constexpr int kStepTile = 32, kStepWaves = 4, kStepRows = 32;
 
@@ -533,8 +538,8 @@ struct StepCfg {
     static constexpr int PPR = D / 8, RPI = 64 / PPR, NL = kStepTile / RPI;       // pieces of a row; rows, loads of a tile
 };
 
-// The weights of a set of which one workgroup had all keys and query rows, from its waves' logits (complete and in the L2 since their wait for all that
-// was under way); lse: +inf for a row that weighs nothing.
+// The weights of a set of which one workgroup had all keys and query rows, from its waves' logits (complete and in the L2 since their wait
+// for all that was under way); lse: +inf for a row that weighs nothing.
 template <int THREADS>
 __device__ __forceinline__ void weigh_set(const float* logits, int stride, int n_rows, int len, const float* lse, const float* weight,
                                           float* weight_out) {
@@ -660,7 +665,9 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void attend_step_kernel(Sets s,
 #pragma unroll
         for (int j = 0; j < 16; ++j) y[j] = x[0][0][j];
         if (capped)
-            cap_logits(y, r, !POS || all, [&](const float (&z)[16]) __attribute__((always_inline)) { return largest_of(span, r.n_always, tile_pos, hi, z); });
+            cap_logits(y, r, !POS || all, [&](const float (&z)[16]) __attribute__((always_inline)) {
+                return largest_of(span, r.n_always, tile_pos, hi, z);
+            });
         if (biased) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) y[j] = fmaf(-slope2, (float)abs(pq - tile_pos[acc_key(0, j, hi)]), y[j] * unit_of);
@@ -885,8 +892,8 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(Partials part, typena
 
 // What follows on the kernels that keep their logits: the first n_merge workgroups merge the splits of a query row, the others add up the
 // weights of 1,024 rows of a set, each with the LSE of its (at most R) query rows made from the splits' sums again.  One launch instead of
-// two, and neither part waits for the other.  4.5 us behind a token over 4,097 rows (a launch and two trips to memory), 7.2 behind eight over
-// 18,177.  R = 8, 16, 32 for the registers that the logits wait in.
+// two, and neither part waits for the other.  4.5 us behind a token over 4,097 rows (a launch and two trips to memory), 7.2 behind eight
+// over 18,177.  R = 8, 16, 32 for the registers that the logits wait in.
 template <bool F32, int D, int R>
 __global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typename Storage<F32>::T* __restrict__ O, float* __restrict__ LSE,
                                                             const float* __restrict__ logits, const int32_t* __restrict__ mix_len,
@@ -953,12 +960,13 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(Partials part, typen
 }
 
 // ------------------------------------------------------------------------------------------
-// The weights of the rows where there are many query rows: the logits once more, against the LSE.  A wave keeps 64 keys in registers as
-// the operand of the first product and goes over query rows, 64 at a time from a ring of four LDS stages, which direct loads fill three tiles
+// The weights of the rows where there are many query rows: the logits once more, against the LSE.  A wave keeps 64 keys in registers as the
+// operand of the first product and goes over query rows, 64 at a time from a ring of four LDS stages, which direct loads fill three tiles
 // ahead for the four waves of a workgroup (counted by hand); a lane's sums are of its elements of the tiles, folded over the lanes at the
 // end.  Query rows are cut into n_part parts where keys alone do not fill the chip, whose sums a last kernel adds in order.
-// Bound by the vector instructions, an exponential and a sum per element beside one product where the ring has two.  14,336 query rows and
-// 18,688 rows of 4 KV heads: 314 us, 0.83 PFLOP/s; 448 and 23,872: 28, capped 37 (43).  Each wave fed from memory by itself, without the ring: 39 where it takes
+// Bound by the vector instructions, an exponential and a sum per element beside one product where the ring has two.  What the pass adds to
+// a call in replayed graphs: 14,336 query rows and 18,688 rows of 4 KV heads 312 us, 0.83 PFLOP/s (under a profiler, 12 launches, 355 at
+// least); 448 and 23,872 26, capped 32 (41 by the exponential).  Each wave fed from memory by itself, without the ring: 39 where it took
 // 30.  Logits kept for this instead of made again would be 4 bytes an element both ways: 171 MB, 70 us, for the 448.
 // ------------------------------------------------------------------------------------------
 // Lanes whose bit N is set keep the upper half of their elements and take their partner's, the others the lower half.
@@ -1023,8 +1031,8 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
     const bool capped = r.cap2 > 0.f, biased = POS && r.slopes, ragged = key0 + 64 > len;
     const float cu = capped || biased ? 1.f : r.c2, unit_of = capped ? 1.f : r.c2;       // units of log 2 of x below; of what a bias is put to
 
-    // Tile t -> stage t % NS, the tiles in their order; rows behind the last one are it.  Token and head of a lane's first row, and of the row
-    // whose numbers it loads, are carried from tile to tile: divisions by the group took as long as the products.
+    // Tile t -> stage t % NS, the tiles in their order; rows behind the last one are it.  Token and head of a lane's first row, and of the
+    // row whose numbers it loads, are carried from tile to tile: divisions by the group took as long as the products.
     struct Place {
         int tok, hg;
         __device__ __forceinline__ void add(int toks, int hgs, int group) {
@@ -1056,7 +1064,8 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
         }
         const bool there = own_at.tok < s.T;
         const int tok = there ? own_at.tok : s.T - 1, hg = there ? own_at.hg : group - 1;
-        dma4(info, (uint32_t)(of_pos ? tok : of_slope ? hg : tok * group + hg) * 4, lds_base + C::INFO_AT + (uint32_t)((t % C::NS) * kWeightWaves + wave) * 256);
+        dma4(info, (uint32_t)(of_pos ? tok : of_slope ? hg : tok * group + hg) * 4,
+             lds_base + C::INFO_AT + (uint32_t)((t % C::NS) * kWeightWaves + wave) * 256);
         if (++issued < n_t) {
             row_at.add(tile_toks, tile_hgs, group);
             own_at.add(tile_toks, tile_hgs, group);
@@ -1150,7 +1159,7 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
                 plain(y, lse[1]);
                 continue;
             }
-            if (all && !biased) {                             // (in one stretch too it spills, with one branch for both plain logits are 2 % slower)
+            if (all && !biased) {                             // (in one stretch it spills; one branch for both: plain logits 2 % slower)
 #pragma unroll 1
                 for (int half = 0; half < 2; ++half) {
                     f32x16 x[2];
@@ -1166,7 +1175,8 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
                 row.pq = pos_of(half);
                 row.span = span_of(r, row.pq);
                 if constexpr (POS) {
-                    const bool hidden = (row.span.width == 0 || pk_max < row.span.lo || pk_min > row.span.hi()) && (pk_max < 0 || (unsigned)max(pk_min, 0) >= row.span.na);
+                    const bool hidden = (row.span.width == 0 || pk_max < row.span.lo || pk_min > row.span.hi()) &&
+                                        (pk_max < 0 || (unsigned)max(pk_min, 0) >= row.span.na);
                     if (__builtin_amdgcn_ballot_w64(!hidden) == 0) continue;
                 }
                 row.lse = lse_of(half);
@@ -1178,8 +1188,10 @@ __global__ __launch_bounds__(64 * kWeightWaves, 2) void attend_weights_kernel(Se
                 if (all) {
                     plain(x, row.lse);
                 } else {                                      // (what is not seen has weight 0, also where the LSE is no number)
-                    if (r.n_always > 0) by_position(x, [&](float y, int p) { return __builtin_amdgcn_exp2f(shown<true>(row.span, p, fmaf(y, cu, -row.lse))); });
-                    else by_position(x, [&](float y, int p) { return __builtin_amdgcn_exp2f(shown<false>(row.span, p, fmaf(y, cu, -row.lse))); });
+                    if (r.n_always > 0)
+                        by_position(x, [&](float y, int p) { return __builtin_amdgcn_exp2f(shown<true>(row.span, p, fmaf(y, cu, -row.lse))); });
+                    else
+                        by_position(x, [&](float y, int p) { return __builtin_amdgcn_exp2f(shown<false>(row.span, p, fmaf(y, cu, -row.lse))); });
 #pragma unroll
                     for (int kb = 0; kb < 2; ++kb) acc[kb] += x[kb];
                 }
@@ -1215,12 +1227,12 @@ __global__ __launch_bounds__(256) void weights_sum_kernel(const float* __restric
 }
 
 // ------------------------------------------------------------------------------------------
-// fp32 sets, on the fp32 matrix instruction: 16 stacked query rows per workgroup, whose four waves take the 32-key tiles of its split in turn;
-// operands come from memory in the order that both products use, as in the plain fp32 decode:
+// fp32 sets, on the fp32 matrix instruction: 16 stacked query rows per workgroup, whose four waves take the 32-key tiles of its split in
+// turn; operands come from memory in the order that both products use, as in the plain fp32 decode:
 //   S^T = K Q^T    lane (i = lane % 16, j = lane / 16): K[key i][16 x + 4 j + e] and Q[row i] of the same; result register r: key 4 j + r, row i
 //   O^T = V^T P^T  step r takes the keys 4 j + r, V[key 4 j + r][64 b + 4 i + e]; result register r' of (b, e): O[row i][64 b + 16 j + 4 r' + e]
-// Bound by that instruction (a 1/16 of the bf16 one's rate) where there is enough to do; three sets of 705 rows with 5 tokens of 4 heads on 2, D = 64,
-// take 6.5 us, of which launch and dependent loads are the most (row by row: 143).
+// Bound by that instruction (a 1/16 of the bf16 one's rate) where there is enough to do; three sets of 705 rows with 5 tokens of 4 heads on
+// 2, D = 64, take 6.5 us, of which launch and dependent loads are the most (row by row: 143).
 // ------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 constexpr int kF32Block = 16, kF32Tile = 32, kF32Waves = 4;
@@ -1279,7 +1291,8 @@ __global__ __launch_bounds__(64 * kF32Waves, 2) void attend_f32_kernel(Sets s, R
             if (__builtin_amdgcn_ballot_w64(any) == 0) {
                 if (kept)
 #pragma unroll
-                    for (int kb = 0; kb < 2; ++kb) *(float4*)(kept + key0 + kb * 16 + 4 * j) = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                    for (int kb = 0; kb < 2; ++kb)
+                        *(float4*)(kept + key0 + kb * 16 + 4 * j) = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
                 continue;
             }
         }
@@ -1414,8 +1427,8 @@ __global__ __launch_bounds__(64 * kF32Waves, 2) void attend_f32_kernel(Sets s, R
         weigh_set<64 * NW>(logits + (size_t)unit * n_rows * stride, stride, n_rows, len, lse_lds, weight ? weight + set : nullptr, weight_out + set);
 }
 
-// The weights of fp32 sets where there are many query rows: a wave has 32 keys and goes over blocks of 16 query rows, four waves of a workgroup
-// over parts of them, whose sums are folded through LDS.
+// The weights of fp32 sets where there are many query rows: a wave has 32 keys and goes over blocks of 16 query rows, four waves of a
+// workgroup over parts of them, whose sums are folded through LDS.
 template <int D, bool POS>
 __global__ __launch_bounds__(64 * kF32Waves, 2) void weights_f32_kernel(Sets s, Rule r, const float* __restrict__ lse2, const float* weight,
                                                                         float* weight_out) {
@@ -1500,8 +1513,8 @@ extern "C" void vxl_debug_mixed_force(int waves, int n_split, int n_part) {
     g_force_part = std::max(0, n_part);
 }
 
-// Many query rows (ring): estimates in us of a launch of workgroups of 256 and of 128 rows and so many splits: rounds over 256 compute units, 8 us
-// for one's start and end, 1.75 and 1.13 per tile (0.75 of it for D = 64), 5 and 0.4 per MB for the merge.
+// Many query rows (ring): estimates in us of a launch of workgroups of 256 and of 128 rows and so many splits: rounds over 256 compute
+// units, 8 us for one's start and end, 1.75 and 1.13 per tile (0.75 of it for D = 64), 5 and 0.4 per MB for the merge.
 static void ring_plan(MixedPlan& p, long long units, long long rows, int D, int l_cap) {
     const long long tiles = (l_cap + kKeyTile - 1) / kKeyTile;
     const int force_waves = g_force_waves, force_split = g_force_split;
@@ -1510,7 +1523,8 @@ static void ring_plan(MixedPlan& p, long long units, long long rows, int D, int 
         if (force_waves && nw != force_waves) continue;
         const long long n_rtile = (rows + 32 * nw - 1) / (32 * nw), base = units * n_rtile;
         const double tile = (nw == 8 ? 1.75 : 1.13) * (D == 64 ? 0.75 : 1.0);
-        const long long most = force_split ? std::min<long long>(tiles, force_split) : std::max<long long>(1, std::min<long long>(tiles, 512 / base));
+        const long long most = force_split ? std::min<long long>(tiles, force_split)
+                                           : std::max<long long>(1, std::min<long long>(tiles, 512 / base));
         for (long long n = force_split ? most : 1; n <= most;) {
             const long long walk = (tiles + n - 1) / n, rounds = (base * n + 255) / 256;
             const double mb = 4e-6 * units * n * rows * D;
@@ -1525,8 +1539,8 @@ static void ring_plan(MixedPlan& p, long long units, long long rows, int D, int 
     }
 }
 
-// Splits: as forced, or from `first` on up to `last` the number that an estimate in us says is faster by a tenth (from eight on the first: no more
-// than an eighth of a round is lost, and the search would take longer than it saves).
+// Splits: as forced, or from `first` on up to `last` the number that an estimate in us says is faster by a tenth (from eight on the first:
+// no more than an eighth of a round is lost, and the search would take longer than it saves).
 template <typename F>
 static int split_by_rounds(int forced, long long first, long long last, F&& us, long long most) {
     if (forced) return (int)std::min<long long>(most, forced);
@@ -1546,23 +1560,30 @@ MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
     p.stride = (l_cap + kStepTile - 1) / kStepTile * kStepTile;
     p.few = rows <= kStepRows;
     if (d->dtype == VXL_F32) {
-        // As many splits as fill the chip, each wave of one with a tile at least: up to 128 rows one workgroup, and of up to 16 query rows one launch (28 heads
-        // on 4, one token, D = 128: 128 rows 9.7 us, with the second launch 12; 192 rows 13.5 by one workgroup, 12.1 by two and the launch).
+        // As many splits as fill the chip, each wave of one with a tile at least.  Sets of up to 128 rows are one workgroup's, and with up
+        // to 16 query rows one launch's.  28 heads on 4, one token, D = 128: 128 rows 9.7 us, with the second launch 12; 192 rows 13.5 by
+        // one workgroup, 12.1 by two and the launch.
         const long long tiles = (l_cap + kF32Tile - 1) / kF32Tile, most = (tiles + kF32Waves - 1) / kF32Waves;
         const long long base = units * ((rows + kF32Block - 1) / kF32Block);
-        // More where the last round would leave many compute units idle, by estimates in us (14 heads on 2 of D = 64: 300 tokens over 5,000 rows, 1 to 5 parts
-        // 134, 109, 96, 94, 91; 80 of four queries over 3,000 84, 73, 66, 64, 62).
+        // More where the last round would leave many compute units idle, by estimates in us.  14 heads on 2 of D = 64, 1 to 5 splits:
+        //   300 tokens over 5,000 rows              134, 109, 96, 94, 91
+        //   80 tokens of four queries over 3,000    84, 73, 66, 64, 62
         p.n_split = split_by_rounds(g_force_split, std::min(most, std::max(1ll, 512 / base)), std::min(most, 2048 / base), [&](long long n) {
             const double walk = (double)((tiles + kF32Waves * n - 1) / (kF32Waves * n)), rounds = (double)((base * n + 511) / 512);
             return rounds * (5 + (d->head_dim == 64 ? 3 : 5) * walk) + (n > 1 ? 4 + units * rows / 1000. : 0);
         }, most);
     } else if (p.few) {
-        // A workgroup on every compute unit, each wave of one with a tile at least.  Short sets by one workgroup each, which needs no second
-        // launch (us, one workgroup and splits, 28 heads on 4, one token: 256 rows 9.0, 10.3, 384 rows 10.7, 10.3; four tokens 12.1, 13.9 and
-        // 14.5, 14.1; D = 64, 14 on 2, 384 rows 8.9, 9.0 and 11.5, 12.1, 512 rows 9.7, 9.2 and 12.4, 12.1).
+        // A workgroup on every compute unit, each wave of one with a tile at least.  Short sets by one workgroup each, which needs no
+        // second launch.  Us by one workgroup and by splits:          one token      four tokens
+        //   28 heads on 4, D = 128    256 rows                  9.0, 10.3      12.1, 13.9
+        //                             384 rows                 10.7, 10.3      14.5, 14.1
+        //   14 heads on 2, D = 64     384 rows                  8.9, 9.0       11.5, 12.1
+        //                             512 rows                  9.7, 9.2       12.4, 12.1
         const long long tiles = (l_cap + kStepTile - 1) / kStepTile, most = (tiles + kStepWaves - 1) / kStepWaves;
-        // More where the last round of workgroups would leave many units idle, by estimates in us (28 heads on 4, one token; 132 sets of
-        // 6,000 rows, 1 to 6 parts 119, 123, 97, 107, 95, 104; 300 of 2,500, 1 to 3 parts 112, 95, 93; 144 of 2,500 with four tokens 69, 91, 79).
+        // More where the last round of workgroups would leave many units idle, by estimates in us.  28 heads on 4, from one split on:
+        //   132 sets of 6,000 rows, one token       119, 123, 97, 107, 95, 104
+        //   300 sets of 2,500 rows, one token       112, 95, 93
+        //   144 sets of 2,500 rows, four tokens     69, 91, 79
         const long long full = std::min(most, std::max(1ll, 256 / units));
         const bool one = tiles <= (d->head_dim == 64 ? 12 : 8);
         p.n_split = split_by_rounds(g_force_split, one ? 1 : full, one ? 1 : std::min(most, 1024 / units), [&](long long n) {
@@ -1571,9 +1592,9 @@ MixedPlan mixed_plan(const vxl_attn_desc* d, int batch, int T, int l_cap) {
         }, most);
     } else if (d->dtype == VXL_BF16) {
         ring_plan(p, units, rows, d->head_dim, l_cap);
-        // Parts of the query rows, by estimates in us: rounds of two workgroups on a compute unit, but no less than the workgroup whose keys
-        // are visible in part takes (tests per element).  448 rows, 23,872 keys, 1 to 4 parts 33.7, 33.2, 32.9, 37.3; 14,336 rows, 18,688
-        // keys, 1, 3, 5, 7, 12 parts 476, 371, 351, 362, 349.
+        // Parts of the query rows, by estimates in us: rounds of two workgroups on a compute unit, but no less than the workgroup whose
+        // keys are visible in part takes (tests per element).  What the pass adds in replayed graphs: 448 rows, 23,872 keys, 1 to 4 parts
+        // 26, 32, 33, 37; 14,336 rows, 18,688 keys, 1, 3, 5, 7, 12 parts 502, 348, 315, 320, 315.
         const long long row_tiles = (rows + kWeightRows - 1) / kWeightRows, blocks = units * key_blocks;
         double best = 1e30;
         for (long long n = 1; n <= std::min<long long>(row_tiles, 16); ++n) {
@@ -1626,8 +1647,8 @@ static vxl_status launch_ring(const MixedPlan& p, const MixedCall& c, const Sets
         });
         if (st != VXL_OK) return st;
         const int n_rtile = (rows + C::ROWS - 1) / C::ROWS;
-        hipLaunchKernelGGL((attend_ring_kernel<dim, nw, pos>), placed_grid((long long)units * p.n_split * n_rtile), dim3(64 * nw), C::LDS_BYTES, s, sets,
-                           rule, part, (uint16_t*)c.O, c.LSE, lse2, units, p.n_split, n_rtile);
+        hipLaunchKernelGGL((attend_ring_kernel<dim, nw, pos>), placed_grid((long long)units * p.n_split * n_rtile), dim3(64 * nw),
+                           C::LDS_BYTES, s, sets, rule, part, (uint16_t*)c.O, c.LSE, lse2, units, p.n_split, n_rtile);
         return mixed_launched();
     };
     auto by_pos = [&](auto dim, auto nw) { return rule.q_pos ? run(dim, nw, std::true_type{}) : run(dim, nw, std::false_type{}); };
@@ -1656,8 +1677,8 @@ static vxl_status launch_finish(const MixedPlan& p, const MixedCall& c, const Pa
     return mixed_launched();
 }
 
-// Keys and values of more bytes than the L2s have between them are read past the caches: 298 MB 66 -> 60 us; 8 MB, which the next call finds in
-// them, are not.
+// Keys and values of more bytes than the L2s have between them are read past the caches: 246 MB (302 of capacity, which is what is known
+// here) 66 -> 60 us; 8 MB, which the next call finds in them, are not.
 constexpr size_t kPastCachesBytes = 32u << 20;
 static vxl_status launch_step(const MixedPlan& p, const MixedCall& c, const Sets& sets, const Rule& rule, hipStream_t s) {
     const vxl_attn_desc* d = c.d;
@@ -1707,8 +1728,8 @@ static vxl_status launch_weights(const MixedPlan& p, const MixedCall& c, const S
             return VXL_OK;
         });
         if (st != VXL_OK) return st;
-        hipLaunchKernelGGL((attend_weights_kernel<dim, pos>), folded_grid((long long)units * p.n_part * n_blocks), dim3(64 * kWeightWaves), lds, s, sets,
-                           rule, lse2, c.weight, c.weight_out, part_w, units, p.n_part);
+        hipLaunchKernelGGL((attend_weights_kernel<dim, pos>), folded_grid((long long)units * p.n_part * n_blocks), dim3(64 * kWeightWaves),
+                           lds, s, sets, rule, lse2, c.weight, c.weight_out, part_w, units, p.n_part);
         return mixed_launched();
     };
     auto by_pos = [&](auto dim) { return rule.q_pos ? run(dim, std::true_type{}) : run(dim, std::false_type{}); };
@@ -1725,15 +1746,15 @@ static vxl_status launch_f32(const MixedPlan& p, const MixedCall& c, const Sets&
     const Partials part{(float*)(c.ws + p.part_o), (float2*)(c.ws + p.part_ml)};
     float *logits = p.few && c.weight_out ? (float*)(c.ws + p.logits) : nullptr, *lse2 = (float*)(c.ws + p.lse2);
     auto run = [&](auto dim, auto pos) {
-        hipLaunchKernelGGL((attend_f32_kernel<dim, pos>), placed_grid((long long)units * p.n_split * n_rtile), dim3(64 * kF32Waves), 0, s, sets, rule, part,
-                           (float*)c.O, c.LSE, lse2, logits, p.stride, units, p.n_split, n_rtile, c.weight, c.weight_out);
+        hipLaunchKernelGGL((attend_f32_kernel<dim, pos>), placed_grid((long long)units * p.n_split * n_rtile), dim3(64 * kF32Waves), 0, s,
+                           sets, rule, part, (float*)c.O, c.LSE, lse2, logits, p.stride, units, p.n_split, n_rtile, c.weight, c.weight_out);
         vxl_status st = mixed_launched();
         if (st != VXL_OK) return st;
         if (p.few) return p.n_split == 1 && n_rtile == 1 ? st : launch_finish<true, dim>(p, c, part, logits, s);
         if (p.n_split > 1) st = launch_merge(p, c, s);
         if (st != VXL_OK || !c.weight_out) return st;
-        hipLaunchKernelGGL((weights_f32_kernel<dim, pos>), dim3((c.l_cap + kF32Tile - 1) / kF32Tile, units), dim3(64 * kF32Waves), 0, s, sets, rule, lse2,
-                           c.weight, c.weight_out);
+        hipLaunchKernelGGL((weights_f32_kernel<dim, pos>), dim3((c.l_cap + kF32Tile - 1) / kF32Tile, units), dim3(64 * kF32Waves), 0, s,
+                           sets, rule, lse2, c.weight, c.weight_out);
         return mixed_launched();
     };
     auto by_pos = [&](auto dim) { return rule.q_pos ? run(dim, std::true_type{}) : run(dim, std::false_type{}); };
@@ -1759,8 +1780,10 @@ vxl_status launch_mixed_attend(const MixedPlan& p, const MixedCall& c, bool forc
     const vxl_score_rule none{};
     const vxl_score_rule& u = c.rule ? *c.rule : none;
     const float in = u.softcap > 0.f ? c.scale / u.softcap : 0.f, in2 = in * in;
-    const float few = in < 0x1p-20f ? 0x1p-6f : in < 0x1p16f ? 0.125f : 0.f;      // (where higher powers are lost they are not needed; coefficients are numbers)
-    const Rule rule{c.scale * kLog2e, in, u.softcap * kLog2e, in > 0.f ? few / in : 0.f, {in2 * (-1.f / 3), in2 * in2 * (2.f / 15), in2 * in2 * in2 * (-17.f / 315)},
+    // |u| below which the series holds: where higher powers of the scale are lost they are not needed, and all coefficients are numbers.
+    const float few = in < 0x1p-20f ? 0x1p-6f : in < 0x1p16f ? 0.125f : 0.f;
+    const Rule rule{c.scale * kLog2e, in, u.softcap * kLog2e,
+                    in > 0.f ? few / in : 0.f, {in2 * (-1.f / 3), in2 * in2 * (2.f / 15), in2 * in2 * in2 * (-17.f / 315)},
                     2 * kLog2e * in, -2 * kLog2e * u.softcap,
                     u.causal, u.window, u.n_always, u.slopes, c.q_pos, c.row_pos};
     const Sets sets{c.Qd, c.Kmix, c.Vmix, c.mix_len, c.T, d->n_q_heads, d->n_kv_heads, c.l_cap};

@@ -32,23 +32,26 @@ struct Move {
     bool in_place;
 };
 
-// The n-th largest preference is found by counting, eleven bits at a time from the top: the bin of the bits so far that holds it, and how many
-// of that bin's rows are still among the n.  Rows above the last bin are kept, and of those in it the lowest.  Rows below n that are not
-// kept are holes, rows from n on that are kept movers; there are as many of one as of the other, and the i-th hole takes the i-th mover.
+// The n-th largest preference is found by counting, eleven bits at a time from the top: the bin of the bits so far that holds it, and how
+// many of that bin's rows are still among the n.  Rows above the last bin are kept, and of those in it the lowest.  Rows below n that are
+// not kept are holes, rows from n on that are kept movers; there are as many of one as of the other, and the i-th hole takes the i-th
+// mover.
 constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 2048;
 __device__ __forceinline__ constexpr int shift_of(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
 __device__ __forceinline__ constexpr int bins_of(int pass) { return pass == 2 ? 1024 : kBins; }
 __device__ __forceinline__ int bin_of(uint32_t x, int pass) { return (int)(x >> shift_of(pass)) & (bins_of(pass) - 1); }
 // (whether its bits above this pass's are those found)
-__device__ __forceinline__ bool of_bin(uint32_t x, int pass, uint32_t upper) { return pass == 0 || x >> (shift_of(pass) + (pass == 2 ? 10 : 11)) == upper; }
+__device__ __forceinline__ bool of_bin(uint32_t x, int pass, uint32_t upper) {
+    return pass == 0 || x >> (shift_of(pass) + (pass == 2 ? 10 : 11)) == upper;
+}
 
 struct Found {
     uint32_t upper;            // the bits found so far
     int left;                  // rows of that bin that are among the n
     int rows;                  // rows of that bin
 };
-// Sums over the lanes up to this one, in the order of lanes (shifts inside rows of 16 lanes, then the last lane of a row, of two, to those behind:
-// a few cycles each, where a shuffle goes through the LDS).
+// Sums over the lanes up to this one, in the order of lanes (shifts inside rows of 16 lanes, then the last lane of a row, of two, to those
+// behind: a few cycles each, where a shuffle goes through the LDS).
 __device__ __forceinline__ int scan_lanes(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
     x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
@@ -107,12 +110,13 @@ __device__ __forceinline__ void move_row(const Cut& c, const Move& m, size_t fro
 
 // ------------------------------------------------------------------------------------------
 // Sets of up to 16,384 rows: a thread has PER rows' preferences in registers (wave w the rows [64 PER w, 64 PER (w + 1)), lanes side by
-// side), a workgroup a whole set.  Bound by latency: launch, one trip to memory, and the barriers of two or three passes (the last one is left
-// out when all of the bin's rows are kept, which is so where weights differ).  Out of place every workgroup of a set selects for itself and
-// moves its share, which saves the second launch; in place the rows' places are written down for the kernel behind.
-// 4 KV heads, 2,304 rows to 2,048: 8.8 us; 16 sets of 7,001 fp32 rows to 1,777: 12.8.  Two groups of workgroups a compute unit could hold (512 / units):
-// 23.8.  Counting a wave's most frequent bin by one lane: 28.  PER = 32 (20,000 rows): 33.8 and 48.7 us for a quarter and nearly all kept, the
-// launches below 34.2 and 43.1.
+// side), a workgroup a whole set.  Bound by latency: launch, one trip to memory, and the barriers of two or three passes (the last one is
+// left out when all of the bin's rows are kept, which is so where weights differ).  Out of place every workgroup of a set selects for
+// itself and moves its share, which saves the second launch; in place the rows' places are written down for the kernel behind.
+// 4 KV heads, 2,304 rows to 2,048: 8.8 us (in place 8.2 and 2.3 for the moves, with the second launch 10.9 in a replayed graph, out of
+// place 9.2); 16 sets of up to 7,001 fp32 rows to 1,777: 13.4 (9.7 and 5.0; 13.9 either way).  Two groups of workgroups a compute unit
+// could hold (512 / units): 23.8.  Counting a wave's most frequent bin by one lane: 28.  PER = 32 (20,000 rows): 33.8 and 48.7 us for a
+// quarter and nearly all kept, the launches below 34.2 and 43.1.
 // ------------------------------------------------------------------------------------------
 template <int PER, int ROW16, bool MOVES>
 __global__ __launch_bounds__(kThreads) void evict_set_kernel(Cut c, Move m, int32_t* __restrict__ places, int32_t* __restrict__ n_out) {
@@ -235,10 +239,11 @@ __global__ __launch_bounds__(kThreads) void evict_set_kernel(Cut c, Move m, int3
 }
 
 // ------------------------------------------------------------------------------------------
-// Longer sets: each in parts of `part_rows` rows below n and of as many from n on (so that a part has holes or movers, never both), at most kParts
-// of them, a workgroup each.  Every pass is a launch: the counts of a part's bins are written down, the next launch adds those of all
-// parts, finds the bin and counts on.  The last one knows from the counts how many rows every part before it keeps.
-// 131,328 rows of 4 KV heads to 16,384: 4.4, 7.4 and 7.4 us for the passes, 12.7 for the places, 12.6 for the moves, which copy 64 MB.
+// Longer sets: each in parts of `part_rows` rows below n and of as many from n on (so that a part has holes or movers, never both), at most
+// kParts of them, a workgroup each.  Every pass is a launch: the counts of a part's bins are written down, the next launch adds those of
+// all parts, finds the bin and counts on.  The last one knows from the counts how many rows every part before it keeps.
+// 131,328 rows of 4 KV heads to 16,384: 4.5, 7.3 and 7.3 us for the passes, 12.8 for the places, 12.6 for the moves, which copy 64 MB (in
+// place 11.6: seven of eight kept rows change place); in replayed graphs 48.7 out of place, 46.9 in place.
 // ------------------------------------------------------------------------------------------
 constexpr int kParts = 20;
 struct State {                 // of a set between the launches, in the workspace
@@ -444,8 +449,8 @@ __global__ __launch_bounds__(256) void evict_move_kernel(Cut c, Move m, const in
     }
 }
 
-// Rows of a set that one workgroup holds in registers, and of a part of a longer one: a set has at most two parts more than part_rows go into it,
-// one for its end and one where n cuts one in two.
+// Rows of a set that one workgroup holds in registers, and of a part of a longer one: a set has at most two parts more than part_rows go
+// into it, one for its end and one where n cuts one in two.
 constexpr int kSetRows = 16 * kThreads;
 int part_rows_of(int l_cap) { return std::max(8 * kThreads, (int)(((long long)l_cap + kParts - 3) / (kParts - 2))); }
 
@@ -466,7 +471,8 @@ vxl_status launch_mixed_evict(const EvictPlan& p, const EvictCall& e, hipStream_
     const int units = e.batch * d->n_kv_heads;
     int32_t *map = (int32_t*)(e.ws + p.map), *n = (int32_t*)(e.ws + p.n);
     const Cut c{e.weight, e.row_pos, e.mix_len, e.newest, d->n_kv_heads, e.l_cap, e.keep, e.n_first, e.n_recent};
-    const Move m{(const uint4*)e.Kmix, (const uint4*)e.Vmix, (uint4*)e.Kout, (uint4*)e.Vout, e.weight_out, e.pos_out, e.kept, e.out_cap, e.Kout == e.Kmix};
+    const Move m{(const uint4*)e.Kmix, (const uint4*)e.Vmix, (uint4*)e.Kout, (uint4*)e.Vout, e.weight_out, e.pos_out,
+                 e.kept, e.out_cap, e.Kout == e.Kmix};
     const int most = std::max(1, std::min(e.keep, e.l_cap));
     return by_storage(d, [&](auto f32, auto dim) {
         constexpr int ROW16 = dim * (f32 ? 4 : 2) / 16;

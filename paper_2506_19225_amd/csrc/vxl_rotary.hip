@@ -8,13 +8,13 @@ namespace vxl {
 
 namespace {
 
-// A row is D / (2 VEC) items of two chunks of VEC elements each: rotated (chunks i and i + rotary_dim / 2, or two neighbours
-// whose elements are pairs among themselves) or copied.  A thread has one item of a token for its heads hg, hg + HG, ..., so
-// the sines and cosines of its pairs are made once (in registers, from an angle in 64 bits) and used for all of them.
-// HBM bound where there is much to do: 131,328 tokens of 28 + 4 heads, D = 128, bf16, 437 us, 4.9 TB/s read and written, a copy's rate; a launch
-// and three dependent loads where there is little: 3.2 us.
-// Threads that a launch of few tokens has at least, the heads of a token shared by several of them.  Us in a replayed graph with 2^15, 2^16, 2^17:
-// 512 new tokens 7.1, 5.7, 5.7; 1,000 tokens of a prompt 6.6, 6.4, 7.3, 4,000 19.5, 15.7, 15.9.
+// A row is D / (2 VEC) items of two chunks of VEC elements each: rotated (chunks i and i + rotary_dim / 2, or two neighbours whose elements
+// are pairs among themselves) or copied.  A thread has one item of a token for its heads hg, hg + HG, ..., so the sines and cosines of its
+// pairs are made once (in registers, from an angle in 64 bits) and used for all of them.
+// HBM bound where there is much to do: 131,328 tokens of 28 + 4 heads, D = 128, bf16, 437 us, 4.9 TB/s read and written, a copy's rate; a
+// launch and three dependent loads where there is little: 3.2 us.
+// Threads that a launch of few tokens has at least, the heads of a token shared by several of them.  Us in a replayed graph with 2^15,
+// 2^16, 2^17: 512 new tokens 7.1, 5.7, 5.7; 1,000 tokens of a prompt 6.6, 6.4, 7.3, 4,000 19.5, 15.7, 15.9.
 constexpr long long kThreadsWanted = 1 << 16;
 struct Where {                 // element strides between heads and tokens of source and destination
     long long head, tok;
@@ -167,8 +167,9 @@ vxl_status launch(const vxl_attn_desc* d, const vxl_rotary* r, RotateArgs a, hip
         constexpr int VEC = f32 ? 4 : 8;
         using Wide = std::integral_constant<int, VEC>;
         using One = std::integral_constant<int, 1>;
-        if (r->interleaved) return r->rotary_dim % VEC == 0 && r->rotary_dim % (2 * VEC) == 0 ? run(Wide{}, std::false_type{}) : run(One{}, std::false_type{});
-        return r->rotary_dim % (2 * VEC) == 0 ? run(Wide{}, std::true_type{}) : run(One{}, std::true_type{});
+        const bool wide = r->rotary_dim % (2 * VEC) == 0;
+        if (r->interleaved) return wide ? run(Wide{}, std::false_type{}) : run(One{}, std::false_type{});
+        return wide ? run(Wide{}, std::true_type{}) : run(One{}, std::true_type{});
     });
 }
 
