@@ -39,10 +39,11 @@ struct State {
 // Kinds of an argument: a layout's c_void_p (or a number or None, the library's to refuse); the descriptor; a quantised cache
 // (its tensors as they are at the call, and its format) or None, a null pointer; a tensor (its
 // data pointer; a contiguous CUDA tensor or AssertionError) or None, a null pointer; a number.  Python does not pass
-// kNumel, the number of elements of the tensor before it (0 for None), and size(i, d), dimension d of its argument i.
+// kNumel, the number of elements of the tensor before it (0 for None), kCount, the same but -1 for None, and size(i, d), dimension d of
+// its argument i.
 // The calls on rotary positions and growing sets hold their tensors to more: of the descriptor's type, float32 or int32 (the workspace: of
 // any), on one device, the current one; beside them a rotary or a rule, or None, a null pointer.
-enum Kind { kLayout, kDesc, kCache, kTensor, kInt, kRotary, kRule, kOfDesc, kFloats, kInts, kWorkspace, kNumel, kSize };
+enum Kind { kLayout, kDesc, kCache, kTensor, kInt, kRotary, kRule, kOfDesc, kFloats, kInts, kWorkspace, kNumel, kCount, kSize };
 constexpr int size(int arg, int dim) { return kSize | arg << 8 | dim << 16; }
 
 // A number that an object answers with (a new reference, or null where it raised).
@@ -266,7 +267,7 @@ bool rule_of(const State& st, Frame& f, PyObject* o, long long* out) {
     long long slopes, n;
     if (!struct_of(st, f, o, st.rule_type, st.slopes, at::kFloat, "float32", &f.rule, &slopes, &n)) return false;
     f.rule.slopes = (const float*)slopes;
-    if (slopes && f.desc && n != f.desc->n_q_heads) { PyErr_SetString(PyExc_ValueError, "a slope per query head expected"); return false; }
+    if (f.held[f.n_held - 1] != Py_None && f.desc && n != f.desc->n_q_heads) { PyErr_SetString(PyExc_ValueError, "a slope per query head expected"); return false; }
     *out = (long long)&f.rule;
     return true;
 }
@@ -279,6 +280,7 @@ bool convert(const State& st, PyObject* const* args, Frame& f, long long* out) {
     int* const next = &f.next;
     if constexpr ((KIND & 255) == kSize) return size_of(args[KIND >> 8 & 255], KIND >> 16, out);
     else if constexpr (KIND == kNumel) return numel_of(args[*next - 1], out);
+    else if constexpr (KIND == kCount) return args[*next - 1] == Py_None ? (*out = -1, true) : numel_of(args[*next - 1], out);
     else if constexpr (KIND == kLayout) return layout_of(st, args[(*next)++], out);
     else if constexpr (KIND == kDesc) {
         if (!desc_of(st, args[(*next)++], out)) return false;
@@ -443,11 +445,11 @@ PyObject* bilevel_decode_kvq(PyObject* self, PyObject* const* args, Py_ssize_t n
     });
 }
 
-// Whether a tensor (0 elements: there is none) has as many elements as the call takes off it.
+// Whether a tensor (-1 elements: there is none) has as many elements as the call takes off it.
 bool has(long long numel, std::initializer_list<long long> dims) {
     __int128 n = 1;
     for (long long x : dims) n *= x;
-    return numel == 0 || n == numel;
+    return numel < 0 || n == numel;
 }
 // Whether one of queries or keys holds the rows of n tokens, by the descriptor's layout.  Without strides heads lie n tokens apart, so that several
 // of them in a tensor of more tokens would be taken for rows of others.
@@ -468,15 +470,15 @@ PyObject* rotate(PyObject* self, PyObject* const* args, Py_ssize_t n) {
         const long long tokens = a[3];
         if (args[2] == Py_None || !in_32_bits(tokens)) return VXL_ERR_INVALID_ARG;          // (no positions are not positions of no tokens)
         for (int i : {4, 6, 8, 10})
-            if (a[i] && !holds_rows(desc(a[0]), tokens, a[i + 1], i == 4 || i == 8)) return VXL_ERR_INVALID_ARG;
+            if (args[i / 2 + 1] != Py_None && !holds_rows(desc(a[0]), tokens, a[i + 1], i == 4 || i == 8)) return VXL_ERR_INVALID_ARG;
         return lib.rotate(desc(a[0]), ptr<vxl_rotary>(a[1]), ptr<int32_t>(a[2]), (int32_t)tokens, ptr<void>(a[4]), ptr<void>(a[6]),
                           ptr<void>(a[8]), ptr<void>(a[10]), (vxl_stream)a[12]);
     });
 }
 // (batch and new tokens: of positions; rows: of kmix)
 PyObject* mixed_append(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-    return call<kDesc, kRotary, kInts, size(2, 0), size(2, 1), kOfDesc, kNumel, kOfDesc, kNumel, kOfDesc, kNumel, kOfDesc, kNumel, kOfDesc, kNumel,
-                kOfDesc, kNumel, size(7, 2), kInts, kNumel, kInts, kNumel, kFloats, kNumel>(
+    return call<kDesc, kRotary, kInts, size(2, 0), size(2, 1), kOfDesc, kCount, kOfDesc, kCount, kOfDesc, kCount, kOfDesc, kCount, kOfDesc, kCount,
+                kOfDesc, kCount, size(7, 2), kInts, kCount, kInts, kCount, kFloats, kCount>(
         self, args, n, [](const State& lib, const long long* a) {
         const vxl_attn_desc* d = desc(a[0]);
         const long long batch = a[3], tokens = a[4], cap = a[17], hkv = d->n_kv_heads;
@@ -493,8 +495,8 @@ PyObject* mixed_append(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 }
 // (batch and tokens: of qd; rows: of kmix)
 PyObject* mixed_attend(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-    return call<kDesc, kRule, kOfDesc, size(2, 0), size(2, 1), kNumel, kInts, kNumel, kOfDesc, size(4, 2), kNumel, kOfDesc, kNumel, kInts, kNumel,
-                kInts, kNumel, kOfDesc, kNumel, kFloats, kNumel, kFloats, kNumel, kFloats, kNumel, kWorkspace, kNumel>(
+    return call<kDesc, kRule, kOfDesc, size(2, 0), size(2, 1), kCount, kInts, kCount, kOfDesc, size(4, 2), kCount, kOfDesc, kCount, kInts, kCount,
+                kInts, kCount, kOfDesc, kCount, kFloats, kCount, kFloats, kCount, kFloats, kCount, kWorkspace, kNumel>(
         self, args, n, [](const State& lib, const long long* a) {
         const vxl_attn_desc* d = desc(a[0]);
         const long long batch = a[3], tokens = a[4], cap = a[9], hkv = d->n_kv_heads, hq = d->n_q_heads;
@@ -511,8 +513,8 @@ PyObject* mixed_attend(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 }
 // (batch and rows: of kmix; rows of the result: of kout)
 PyObject* mixed_evict(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-    return call<kDesc, kOfDesc, size(1, 0), size(1, 2), kNumel, kOfDesc, kNumel, kInts, kNumel, kFloats, kNumel, kInts, kNumel, kInts, kNumel, kInt,
-                kInt, kInt, kOfDesc, size(10, 2), kNumel, kOfDesc, kNumel, kFloats, kNumel, kInts, kNumel, kInts, kNumel, kWorkspace, kNumel>(
+    return call<kDesc, kOfDesc, size(1, 0), size(1, 2), kCount, kOfDesc, kCount, kInts, kCount, kFloats, kCount, kInts, kCount, kInts, kCount, kInt,
+                kInt, kInt, kOfDesc, size(10, 2), kCount, kOfDesc, kCount, kFloats, kCount, kInts, kCount, kInts, kCount, kWorkspace, kNumel>(
         self, args, n, [](const State& lib, const long long* a) {
         const vxl_attn_desc* d = desc(a[0]);
         const long long batch = a[2], cap = a[3], to = a[19], hkv = d->n_kv_heads, dim = d->head_dim;

@@ -58,6 +58,26 @@ def test_rotation_without_positions():
         assert refused(rotate, at=None, **kw) == vxl.VXL_ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("call,optional", [(rotate, "k ko"), (append, "pos w"), (attend, "lse w w2"), (attend, "at pos"), (evict, "new")])
+def test_tensors_of_nothing_are_not_none(call, optional):
+    """A tensor without elements in the place of one that may be None: refused, not left out."""
+    import inspect
+    have = {k: p.default for k, p in inspect.signature(call).parameters.items()}
+    rest = {rotate: {}, append: {}, attend: dict(rule=None), evict: dict(recent=0)}[call]
+    names = optional.split()
+    assert refused(call, **rest, **{name: None for name in names}) == vxl.VXL_ERR_HIP
+    for some in [names] + [[name] for name in names]:
+        for shape in ((0,), have[some[0]].shape[:-1] + (0,)):
+            with pytest.raises((vxl.VxlError, IndexError)) as e:
+                call(**rest, **{name: Typed(shape, have[name].dtype, 0) for name in some})
+            assert not isinstance(e.value, vxl.VxlError) or e.value.status == vxl.VXL_ERR_INVALID_ARG, some
+
+
+def test_slopes_of_no_head():
+    with pytest.raises(ValueError, match="slope per query head"):
+        attend(rule=vxl.ScoreRule(slopes=Typed((0,), torch.float32, 0)))
+
+
 @pytest.mark.filterwarnings("ignore:Accessing the data pointer of FakeTensor")
 @pytest.mark.parametrize("call", [attend, evict])
 def test_a_workspace_of_another_device(call, monkeypatch):
