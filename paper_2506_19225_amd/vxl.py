@@ -455,7 +455,8 @@ class ScoreRule:
 
 
 def rotate(desc: AttnDesc, rotary: Rotary, positions, q, k, q_out, k_out, stream=None):
-    """vxl_rotate: positions int32 [N]; q/q_out and k/k_out (or None, both) in the descriptor's layouts, in place or not."""
+    """vxl_rotate: positions int32 [N]; q/q_out and k/k_out (or None, both) in the descriptor's layouts, in place or not.  Without strides
+    tensors of several heads hold N tokens exactly, with them N or more."""
     st = (_native or native()).rotate(desc, rotary, positions, q, k, q_out, k_out, stream)
     _check(st, "vxl_rotate")
     return q_out, k_out
@@ -463,8 +464,9 @@ def rotate(desc: AttnDesc, rotary: Rotary, positions, q, k, q_out, k_out, stream
 
 def mixed_append(desc: AttnDesc, rotary: Optional[Rotary], positions, q, k, v, qd, kmix, vmix, mix_len, row_pos=None, row_weight=None,
                  stream=None):
-    """vxl_mixed_append: positions int32 [B,T]; q, k, v of B * T tokens in the descriptor's layouts; qd [B,T,Hq,D]; kmix/vmix
-    [B,Hkv,Lcap,D]; mix_len int32 [B], the new rows among them; row_pos int32, row_weight float32 [B,Hkv,Lcap]."""
+    """vxl_mixed_append: positions int32 [B,T]; q, k, v of B * T tokens in the descriptor's layouts, as rotate's; qd [B,T,Hq,D]; kmix/vmix
+    [B,Hkv,Lcap,D]; mix_len int32 [B], the new rows among them; row_pos int32, row_weight float32 [B,Hkv,Lcap].  Behind a gather:
+    row_pos = src_idx[:, None].expand(B, Hkv, Lcap).contiguous(), row_weight = 0, mix_len += T."""
     st = (_native or native()).mixed_append(desc, rotary, positions, q, k, v, qd, kmix, vmix, mix_len, row_pos, row_weight, stream)
     _check(st, "vxl_mixed_append")
     return qd
